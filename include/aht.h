@@ -407,6 +407,53 @@ aht_status aht_s5_step(aht_s5* s, const uint8_t* obs, const uint8_t* reset, cons
                        int64_t n, float* state, float* logits, float* values);
 aht_status aht_s5_sync(aht_s5* s);
 
+/* ---- Gated linear recurrence over a trajectory (the sequence core of a recurrent ego) ---
+ * A real diagonal recurrence with input-dependent decay (De et al. 2024, "Griffin", the
+ * real-gated linear recurrent unit), over the [T][N] steps that aht_rollout collects, with
+ * the state cleared where an episode begins.  Per env n and channel d:
+ *   s = 8 softplus(lam),  rho = sigmoid(r_t),  iota = sigmoid(i_t),
+ *   a_t = exp(-s rho),  beta_t = sqrt(1 - a_t^2),
+ *   h_t = a_t h_{t-1} + beta_t iota_t x_t,   without the first term where reset_t is set.
+ * A reset drops the earlier state whatever it holds, NaN included.  Env n has lengths[n]
+ * steps (clamped to 0..T; NULL: all T): from there on h is written as 0, the inputs are not
+ * used (they may hold anything), the state stays and the gradients are 0.
+ * x, r, i, h and their gradients are fp32 or bf16, element (t, n, d) of a sequence at
+ * data[t * st + n * sn + d]: time-major, env-major and slices of one fused projection are
+ * all strides.  Gates, state and sums are fp32; each output is rounded once.  Outputs must
+ * not overlap inputs or one another (h_last may be h0).  Lanes (n, d) are independent and
+ * every sum has a fixed order: the same call gives the same bits.
+ * T = 1 is the serving step: h0 and h_last are the carried state.  Calls are asynchronous
+ * on cuda_stream (NULL = default), allocate nothing and may be captured into a graph. */
+#define AHT_GLR_SEGMENT 8       /* steps between two checkpoints of the state */
+#define AHT_GLR_MAX_D (1 << 20)
+typedef struct aht_seq {
+  void* data;
+  int64_t st, sn;               /* elements between steps / between envs */
+} aht_seq;
+typedef struct aht_glr_args {
+  int32_t dtype;                /* AHT_FP32 or AHT_BF16: x, r, i, h, dh, dx, dr, di */
+  int32_t D;                    /* channels, 1..AHT_GLR_MAX_D */
+  int64_t T, N;                 /* steps (0 or more), envs (1 or more) */
+  aht_seq x, r, i;
+  const float* lam;             /* [D] */
+  const uint8_t* reset;         /* [T][N] 1: an episode begins with step t; or NULL */
+  const int32_t* lengths;       /* [N] or NULL */
+} aht_glr_args;
+/* Elements of the fp32 checkpoint array [ceil(T / AHT_GLR_SEGMENT)][N][D] that the forward
+ * pass leaves for the backward pass, and bytes of the backward pass's workspace. */
+int64_t aht_glr_ckpt_elems(int64_t T, int64_t N, int32_t D);
+int64_t aht_glr_workspace(int64_t T, int64_t N, int32_t D);
+/* h0 f32 [N][D] (NULL: zeros) -> h (NULL: not written), h_last f32 [N][D] (NULL: not
+ * written; may be h0), ckpt f32 (NULL when no backward pass follows). */
+aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq* h, float* h_last, float* ckpt,
+                           void* cuda_stream);
+/* Gradients of a loss whose gradients are dh (of h; NULL: 0) and dh_last (f32 [N][D] of
+ * h_last; NULL: 0), at the arguments and checkpoints of the forward call: dx, dr, di, and,
+ * where not NULL, dlam f32 [D] (summed over steps and envs) and dh0 f32 [N][D]. */
+aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_seq* dh, const float* dh_last,
+                            const aht_seq* dx, const aht_seq* dr, const aht_seq* di, float* dlam, float* dh0,
+                            void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
 /* Stateless GAE (App. C "PPO ego"), time-major [T][n_envs] device arrays:
  *   delta_t = r_t + gamma (1 - d_t) V_{t+1} - V_t,
  *   A_t = delta_t + gamma lambda (1 - d_t) A_{t+1},  V_T = v_last,  A_T = 0,

@@ -27,7 +27,8 @@ EXPORTED = ["aht_create", "aht_destroy", "aht_reset", "aht_rollout", "aht_xplay_
             "aht_xp_stats", "aht_learner_create", "aht_learner_destroy", "aht_learner_n_params",
             "aht_ppo_update", "aht_ppo_grad", "aht_learner_get", "aht_learner_set",
             "aht_learner_push", "aht_learner_sync", "aht_rollout_ippo", "aht_rollout_resample",
-            "aht_s5_create", "aht_s5_destroy", "aht_s5_step", "aht_s5_sync", "aht_traj_copy"]
+            "aht_s5_create", "aht_s5_destroy", "aht_s5_step", "aht_s5_sync", "aht_traj_copy",
+            "aht_glr_ckpt_elems", "aht_glr_workspace", "aht_glr_forward", "aht_glr_backward"]
 
 
 class AhtError(RuntimeError):
@@ -118,6 +119,15 @@ def load() -> C.CDLL:
             L.aht_s5_step.restype = C.c_int
             L.aht_s5_sync.argtypes = [vp]
             L.aht_s5_sync.restype = C.c_int
+            L.aht_glr_ckpt_elems.argtypes = [i64, i64, i32]
+            L.aht_glr_ckpt_elems.restype = i64
+            L.aht_glr_workspace.argtypes = [i64, i64, i32]
+            L.aht_glr_workspace.restype = i64
+            L.aht_glr_forward.argtypes = [C.POINTER(GlrArgs), vp, C.POINTER(Seq), vp, vp, vp]
+            L.aht_glr_forward.restype = C.c_int
+            L.aht_glr_backward.argtypes = [C.POINTER(GlrArgs), vp, C.POINTER(Seq), vp, C.POINTER(Seq), C.POINTER(Seq),
+                                           C.POINTER(Seq), vp, vp, vp, i64, vp]
+            L.aht_glr_backward.restype = C.c_int
             L.aht_rollout_resample.argtypes = [vp, i32, C.POINTER(i32), i32, i32, C.POINTER(Traj), vp]
             L.aht_xplay_matrix.argtypes = [vp, C.POINTER(i32), i32, C.POINTER(i32), i32, i32, i32, C.POINTER(XplayOut)]
             L.aht_gae.argtypes = [vp, vp, vp, vp, i64, i32, C.c_float, C.c_float, vp, vp, vp]
@@ -661,3 +671,92 @@ def aht_s5_step(pol: S5Policy, obs, reset, state, logits, values, legal=None):
 
 def aht_s5_sync(pol: S5Policy):
     _check(load().aht_s5_sync(pol.handle))
+
+
+# ---- gated linear recurrence over a trajectory ------------------------------------------
+AHT_GLR_SEGMENT = 8
+
+
+class Seq(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("st", C.c_int64), ("sn", C.c_int64)]
+
+
+class GlrArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("D", C.c_int32), ("T", C.c_int64), ("N", C.c_int64),
+                ("x", Seq), ("r", Seq), ("i", Seq), ("lam", C.c_void_p), ("reset", C.c_void_p),
+                ("lengths", C.c_void_p)]
+
+
+def _seq(t, shape, dtype, name, written=False):
+    """A [T][N][D] tensor with contiguous channels and any step and env strides."""
+    if t is None:
+        return Seq(None, 0, 0)
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    T, N, D = shape
+    if t.numel() and D > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} must have contiguous channels (stride 1 in its last dimension)")
+    st, sn = (t.stride(0) if T > 1 else 0), (t.stride(1) if N > 1 else 0)
+    if written and t.numel():
+        # every element an address of its own: the strides nest around a row of D channels
+        dims = sorted((s, k) for s, k in ((st, T), (sn, N)) if k > 1)
+        extent = D
+        for s, k in dims:
+            if s < extent:
+                raise ValueError(f"{name} is written: its steps and envs must not overlap in memory")
+            extent = s * (k - 1) + extent
+    return Seq(t.data_ptr(), st, sn)
+
+
+def _glr_args(x, r, i, lam, reset, lengths):
+    if not isinstance(x, torch.Tensor) or x.dim() != 3:
+        raise ValueError("x must be a [T][N][D] tensor")
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"x must be float32 or bfloat16, got {x.dtype}")
+    T, N, D = x.shape
+    dt = x.dtype
+    return (T, N, D), dt, GlrArgs(
+        AHT_FP32 if dt == torch.float32 else AHT_BF16, D, T, N, _seq(x, x.shape, dt, "x"), _seq(r, x.shape, dt, "r"),
+        _seq(i, x.shape, dt, "i"), _ptr(lam, torch.float32, (D,), "lam"),
+        _ptr(reset, torch.uint8, (T, N), "reset"), _ptr(lengths, torch.int32, (N,), "lengths"))
+
+
+def aht_glr_ckpt_shape(T, N, D):
+    """Shape of the f32 checkpoint tensor that the forward pass leaves for the backward."""
+    return (-(-T // AHT_GLR_SEGMENT), N, D)
+
+
+def aht_glr_workspace(T, N, D) -> int:
+    """Bytes of aht_glr_backward's workspace."""
+    return int(load().aht_glr_workspace(T, N, D))
+
+
+def aht_glr_forward(x, r, i, lam, h=None, reset=None, lengths=None, h0=None, h_last=None, ckpt=None, stream=None):
+    """h_t = a_t h_{t-1} + beta_t sigmoid(i_t) x_t over x, r, i [T][N][D] (see include/aht.h);
+    T = 1 with h0 and h_last the same tensor is the serving step."""
+    shape, dt, a = _glr_args(x, r, i, lam, reset, lengths)
+    T, N, D = shape
+    f32 = torch.float32
+    hs = _seq(h, shape, dt, "h", written=True)
+    _check(load().aht_glr_forward(C.byref(a), _ptr(h0, f32, (N, D), "h0"), C.byref(hs),
+                                  _ptr(h_last, f32, (N, D), "h_last"),
+                                  _ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt"), _stream(stream)))
+
+
+def aht_glr_backward(x, r, i, lam, ckpt, dh, dx, dr, di, dlam=None, workspace=None, reset=None, lengths=None,
+                     dh_last=None, dh0=None, stream=None):
+    """Gradients of aht_glr_forward into dx, dr, di (and dlam, dh0) from dh and dh_last."""
+    shape, dt, a = _glr_args(x, r, i, lam, reset, lengths)
+    T, N, D = shape
+    f32 = torch.float32
+    s = {k: _seq(t, shape, dt, k, written=k != "dh") for k, t in (("dh", dh), ("dx", dx), ("dr", dr), ("di", di))}
+    ws = _ptr(workspace, torch.uint8, None, "workspace")
+    _check(load().aht_glr_backward(C.byref(a), _ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt"),
+                                   C.byref(s["dh"]), _ptr(dh_last, f32, (N, D), "dh_last"), C.byref(s["dx"]),
+                                   C.byref(s["dr"]), C.byref(s["di"]), _ptr(dlam, f32, (D,), "dlam"),
+                                   _ptr(dh0, f32, (N, D), "dh0"), ws, 0 if workspace is None else workspace.numel(),
+                                   _stream(stream)))
