@@ -454,6 +454,50 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
                             const aht_seq* dx, const aht_seq* dr, const aht_seq* di, float* dlam, float* dh0,
                             void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
+/* ---- Orthogonalised matrix updates (optimiser of a policy's hidden matrices) ------------
+ * The Muon update (Jordan et al. 2024) of a fixed set of weight matrices W [rows][cols]:
+ *   M <- momentum M + G,   U = G + momentum M (nesterov) or M,
+ *   O = orthogonalisation of U,
+ *   W <- (1 - lr weight_decay) W - lr sqrt(max(1, rows / cols)) O,
+ * where O replaces U's singular values by values near 1: X = U / (||U||_F + eps), then
+ * `steps` times X <- a X + b (X X^T) X + c (X X^T)^2 X with (a, b, c) = (3.4445, -4.7750,
+ * 2.0315).  Products are accurate to fp32 (operands carried as two fp16, fp32 accumulation);
+ * W and M are fp32, G fp32 or bf16, each output is rounded once.  A zero U gives O = 0; a
+ * NaN or infinity in a gradient makes that matrix's update NaN and touches no other.  Every
+ * sum has a fixed order: the same call gives the same bits.
+ * Matrices are row-major with row strides ld (>= cols, in elements); those of one call must
+ * not overlap.  Vectors, embeddings and output layers are the business of another optimiser. */
+#define AHT_MUON_MAX_MATRICES 48
+#define AHT_MUON_MAX_DIM 16384
+typedef struct aht_muon_config {
+  float momentum;               /* [0, 1) (0.95) */
+  float weight_decay;           /* >= 0 (0.01) */
+  float eps;                    /* > 0 (1e-7) */
+  int32_t nesterov;             /* 0 or 1 (1) */
+  int32_t steps;                /* 1..32 (5) */
+} aht_muon_config;
+typedef struct aht_muon_matrix {  /* device arrays of one matrix */
+  float* W;
+  float* M;
+  const void* G;
+  int32_t ldw, ldm, ldg;
+} aht_muon_matrix;
+typedef struct aht_muon aht_muon; /* opaque, library-owned */
+/* Allocates the workspace for n matrices of these sizes (about 8 bytes per element plus 8
+ * per element of the short side's square, sides rounded up to 128); work runs on
+ * cuda_stream (NULL = default).  The other calls allocate nothing. */
+aht_status aht_muon_create(int32_t n, const int32_t* rows, const int32_t* cols, const aht_muon_config* cfg,
+                           void* cuda_stream, aht_muon** out);
+void aht_muon_destroy(aht_muon* s);
+/* One update of every matrix (host array of n).  Asynchronous; aht_muon_sync reports device
+ * errors (AHT_ETIMEOUT if a bounded wait of a product expired). */
+aht_status aht_muon_step(aht_muon* s, const aht_muon_matrix* mats, int32_t grad_dtype, float lr);
+/* out[k] = orthogonalisation of in[k] (host arrays of n device pointers and row strides;
+ * both fp32 or both bf16; out[k] may be in[k]). */
+aht_status aht_muon_orthogonalize(aht_muon* s, const void* const* in, const int32_t* ld_in, void* const* out,
+                                  const int32_t* ld_out, int32_t dtype);
+aht_status aht_muon_sync(aht_muon* s);
+
 /* Stateless GAE (App. C "PPO ego"), time-major [T][n_envs] device arrays:
  *   delta_t = r_t + gamma (1 - d_t) V_{t+1} - V_t,
  *   A_t = delta_t + gamma lambda (1 - d_t) A_{t+1},  V_T = v_last,  A_T = 0,

@@ -28,7 +28,8 @@ EXPORTED = ["aht_create", "aht_destroy", "aht_reset", "aht_rollout", "aht_xplay_
             "aht_ppo_update", "aht_ppo_grad", "aht_learner_get", "aht_learner_set",
             "aht_learner_push", "aht_learner_sync", "aht_rollout_ippo", "aht_rollout_resample",
             "aht_s5_create", "aht_s5_destroy", "aht_s5_step", "aht_s5_sync", "aht_traj_copy",
-            "aht_glr_ckpt_elems", "aht_glr_workspace", "aht_glr_forward", "aht_glr_backward"]
+            "aht_glr_ckpt_elems", "aht_glr_workspace", "aht_glr_forward", "aht_glr_backward", "aht_muon_create", "aht_muon_destroy",
+            "aht_muon_step", "aht_muon_orthogonalize", "aht_muon_sync"]
 
 
 class AhtError(RuntimeError):
@@ -128,6 +129,14 @@ def load() -> C.CDLL:
             L.aht_glr_backward.argtypes = [C.POINTER(GlrArgs), vp, C.POINTER(Seq), vp, C.POINTER(Seq), C.POINTER(Seq),
                                            C.POINTER(Seq), vp, vp, vp, i64, vp]
             L.aht_glr_backward.restype = C.c_int
+            L.aht_muon_create.argtypes = [i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(MuonConfig), vp, C.POINTER(vp)]
+            L.aht_muon_destroy.argtypes = [vp]
+            L.aht_muon_destroy.restype = None
+            L.aht_muon_step.argtypes = [vp, C.POINTER(MuonMatrix), i32, C.c_float]
+            L.aht_muon_orthogonalize.argtypes = [vp, C.POINTER(vp), C.POINTER(i32), C.POINTER(vp), C.POINTER(i32), i32]
+            L.aht_muon_sync.argtypes = [vp]
+            for f in ("aht_muon_create", "aht_muon_step", "aht_muon_orthogonalize", "aht_muon_sync"):
+                getattr(L, f).restype = C.c_int
             L.aht_rollout_resample.argtypes = [vp, i32, C.POINTER(i32), i32, i32, C.POINTER(Traj), vp]
             L.aht_xplay_matrix.argtypes = [vp, C.POINTER(i32), i32, C.POINTER(i32), i32, i32, i32, C.POINTER(XplayOut)]
             L.aht_gae.argtypes = [vp, vp, vp, vp, i64, i32, C.c_float, C.c_float, vp, vp, vp]
@@ -760,3 +769,101 @@ def aht_glr_backward(x, r, i, lam, ckpt, dh, dx, dr, di, dlam=None, workspace=No
                                    C.byref(s["dr"]), C.byref(s["di"]), _ptr(dlam, f32, (D,), "dlam"),
                                    _ptr(dh0, f32, (N, D), "dh0"), ws, 0 if workspace is None else workspace.numel(),
                                    _stream(stream)))
+
+
+# ---- orthogonalised matrix updates -------------------------------------------------------
+class MuonConfig(C.Structure):
+    _fields_ = [("momentum", C.c_float), ("weight_decay", C.c_float), ("eps", C.c_float),
+                ("nesterov", C.c_int32), ("steps", C.c_int32)]
+
+
+class MuonMatrix(C.Structure):
+    _fields_ = [("W", C.c_void_p), ("M", C.c_void_p), ("G", C.c_void_p), ("ldw", C.c_int32),
+                ("ldm", C.c_int32), ("ldg", C.c_int32)]
+
+
+MUON_DEFAULTS = dict(momentum=0.95, weight_decay=0.01, eps=1e-7, nesterov=1, steps=5)
+
+
+class Muon:
+    """Owns an aht_muon handle (aht_muon_destroy on close / garbage collection)."""
+
+    def __init__(self, handle, shapes):
+        self.handle, self.shapes = handle, shapes
+
+    def close(self):
+        if self.handle:
+            load().aht_muon_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def aht_muon_create(shapes, stream=None, **cfg) -> Muon:
+    """shapes: [(rows, cols), ...] of the matrices every later call updates; cfg: MUON_DEFAULTS."""
+    c = dict(MUON_DEFAULTS)
+    c.update(cfg)
+    conf = MuonConfig(**c)
+    shapes = [(int(r), int(k)) for r, k in shapes]
+    n = len(shapes)
+    rows, cols = (C.c_int32 * n)(*[r for r, _ in shapes]), (C.c_int32 * n)(*[k for _, k in shapes])
+    h = C.c_void_p()
+    _check(load().aht_muon_create(n, rows, cols, C.byref(conf), _stream(stream), C.byref(h)))
+    return Muon(h, shapes)
+
+
+def _matrices(opt, ts, dtype, name):
+    """The matrices of a call: pointers and row strides."""
+    ts = list(ts)
+    if len(ts) != len(opt.shapes):
+        raise ValueError(f"{name}: {len(opt.shapes)} matrices expected, got {len(ts)}")
+    out = []
+    for k, (t, shape) in enumerate(zip(ts, opt.shapes)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name}[{k}] must be a CUDA tensor")
+        if t.dtype != dtype:
+            raise TypeError(f"{name}[{k}] must be {dtype}, got {t.dtype}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}[{k}] must have shape {shape}, got {tuple(t.shape)}")
+        rows, cols = shape
+        ld = t.stride(0) if rows > 1 else cols
+        if (cols > 1 and t.stride(1) != 1) or ld < cols:
+            raise ValueError(f"{name}[{k}] must be row-major (its rows contiguous and apart)")
+        if ld >= 1 << 31:
+            raise ValueError(f"{name}[{k}]: row stride above 2^31 - 1")
+        out.append((t.data_ptr(), ld))
+    return out
+
+
+def _matrix_dtype(ts, name):
+    if not len(ts) or not isinstance(ts[0], torch.Tensor) or ts[0].dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name} must be float32 or bfloat16 tensors")
+    return ts[0].dtype, AHT_FP32 if ts[0].dtype == torch.float32 else AHT_BF16
+
+
+def aht_muon_step(opt: Muon, weights, momenta, grads, lr):
+    """One update of ``weights`` and ``momenta`` (f32, in place) from ``grads`` (f32 or bf16)."""
+    grads = list(grads)
+    dt, code = _matrix_dtype(grads, "grads")
+    W, M = _matrices(opt, weights, torch.float32, "weights"), _matrices(opt, momenta, torch.float32, "momenta")
+    G = _matrices(opt, grads, dt, "grads")
+    arr = (MuonMatrix * len(W))(*[MuonMatrix(w, m, g, lw, lm, lg) for (w, lw), (m, lm), (g, lg) in zip(W, M, G)])
+    _check(load().aht_muon_step(opt.handle, arr, code, lr))
+
+
+def aht_muon_orthogonalize(opt: Muon, mats, outs):
+    """outs[k] = orthogonalisation of mats[k] (all f32 or all bf16; outs may be mats)."""
+    mats = list(mats)
+    dt, code = _matrix_dtype(mats, "mats")
+    A, B = _matrices(opt, mats, dt, "mats"), _matrices(opt, outs, dt, "outs")
+    n = len(A)
+    ptr, ld = (lambda v: (C.c_void_p * n)(*[p for p, _ in v])), (lambda v: (C.c_int32 * n)(*[s for _, s in v]))
+    _check(load().aht_muon_orthogonalize(opt.handle, ptr(A), ld(A), ptr(B), ld(B), code))
+
+
+def aht_muon_sync(opt: Muon):
+    _check(load().aht_muon_sync(opt.handle))
