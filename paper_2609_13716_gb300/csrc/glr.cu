@@ -1,29 +1,47 @@
 // glr.cu -- the gated linear recurrence over a collected trajectory (include/aht.h states
 // the model): forward over T steps, one serving step (T = 1), and the backward pass.
 //
-// A lane is one channel d of one env n; its T steps are a chain, lanes are independent.
-// One thread runs one lane here; consecutive threads take consecutive channels, so a warp
-// reads contiguous rows.  State, gates and sums are fp32 whatever the tensors' type; each
-// output is rounded once.
+// A lane is one channel d of one env n; its T steps are a chain, lanes are independent.  A
+// thread owns V neighbouring channels of one env (one 4- or 8-byte load per row) and a
+// segment of S consecutive steps; a warp's row is contiguous.  The loads of the next segment
+// are issued before the present one is computed, so the copies run during the arithmetic.
+//   - Many lanes: a warp walks its lanes' whole chain, segment after segment.
+//   - Few lanes: WT warps of a CTA, and CL CTAs of a cluster, take consecutive segments of
+//     the same lanes.  A segment is an affine map of the state it receives, h -> A h + H;
+//     the maps are composed over the warps in shared memory and over the CTAs in distributed
+//     shared memory, then every thread applies its own from the state that reaches it.  All
+//     inputs are read once, and no CTA waits for one outside its cluster.
+// The backward pass is the same scan from the end for p = dL/dh of the state a step
+// receives, p -> A p + P with the same A.
+//
+// State, gates and sums are fp32 whatever the tensors' type; each output is rounded once.
+// Where a map has A = 0 (a reset, or a decay that underflowed) it drops what it receives,
+// NaN and infinity included.
 //
 // The backward pass needs the state before every step.  The forward pass leaves it as fp32
 // checkpoints every kSeg = 8 steps (0.5 B per element; the rounded h would cost 2-4 B and
 // carry bf16 rounding into every gradient), and the backward pass rebuilds the seven states
 // between two checkpoints in registers.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "kernels.h"
+#include "tc_common.cuh"
 
 namespace aht {
 aht_status set_last_error(aht_status s, const char* msg);  // the message of aht_last_error
 }  // namespace aht
 
 using namespace aht;
+namespace cg = cooperative_groups;
 
 namespace {
 
 constexpr int kSeg = AHT_GLR_SEGMENT;  // steps between two checkpoints
 constexpr float kGateScale = 8.0f;     // s = 8 softplus(lam)
+constexpr int kMaxCluster = 8;
 
 struct Seq {
   void* p;
@@ -39,53 +57,291 @@ struct GlrDev {
   const int32_t* lengths;
 };
 
-template <typename E>
-__device__ __forceinline__ float ld(const Seq& s, int64_t t, int64_t n, int64_t d) {
-  const E* p = static_cast<const E*>(s.p) + t * s.st + n * s.sn + d;
-  return (float)__ldg(p);
-}
-template <typename E>
-__device__ __forceinline__ void st(const Seq& s, int64_t t, int64_t n, int64_t d, float v) {
-  static_cast<E*>(s.p)[t * s.st + n * s.sn + d] = (E)v;
-}
+// ---- V neighbouring channels as one load or store -----------------------------------------
+template <int kBytes> struct Word;
+template <> struct Word<2> { using T = uint16_t; };
+template <> struct Word<4> { using T = uint32_t; };
+template <> struct Word<8> { using T = uint2; };
+template <> struct Word<16> { using T = uint4; };
+
+template <typename E, int V>
+struct Vec {
+  using W = typename Word<(int)sizeof(E) * V>::T;
+  union {
+    W w;
+    E e[V];
+  };
+  __device__ __forceinline__ Vec() {}
+  __device__ __forceinline__ void load(const void* p) { w = __ldcs(static_cast<const W*>(p)); }
+  __device__ __forceinline__ void store(void* p) const { __stcs(static_cast<W*>(p), w); }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int v = 0; v < V; ++v) e[v] = E(0.0f);
+  }
+  __device__ __forceinline__ float get(int v) const { return (float)e[v]; }
+  __device__ __forceinline__ void set(int v, float f) { e[v] = (E)f; }
+};
 
 __device__ __forceinline__ float softplus_f(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))); }
 __device__ __forceinline__ float sigmoid_f(float x) { return 1.0f / (1.0f + expf(-x)); }
 
-// The gates of one element: q = s rho, a = exp(-q) = 1 + em, beta^2 = 1 - a^2 = -em (2 + em)
-// (no cancellation as a -> 1).
-struct Gates {
-  float rho, iota, q, a, beta2;
+constexpr float kLog2e = 1.4426950408889634f;
+// 1 / (1 + 2^(-x log2 e)): the hardware exp2 and reciprocal, 2^-22 relative each; 0 and 1 at
+// the infinities.
+__device__ __forceinline__ float sigmoid_q(float x) {
+  return tc::rcp_approx(1.0f + tc::ex2_approx(-kLog2e * x));
+}
+// exp(-q) - 1 for q >= 0: below 1/4 its series -q (1 - q/2 + q^2/6 - ... + q^6/5040) (the
+// next term is below 2^-26 there), above it 2^(-q log2 e) - 1 (no cancellation).
+__device__ __forceinline__ float decay_m1(float q) {
+  float s = fmaf(q, 1.0f / 5040.0f, -1.0f / 720.0f);
+  s = fmaf(q, s, 1.0f / 120.0f);
+  s = fmaf(q, s, -1.0f / 24.0f);
+  s = fmaf(q, s, 1.0f / 6.0f);
+  s = fmaf(q, s, -0.5f);
+  s = fmaf(q, s, 1.0f);
+  const float big = tc::ex2_approx(-kLog2e * q) - 1.0f;
+  return q < 0.25f ? -q * s : big;
+}
+__device__ __forceinline__ float sqrt_q(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// A y + b, or b alone where A is 0.
+__device__ __forceinline__ float apply(float A, float y, float b) { return A == 0.0f ? b : fmaf(A, y, b); }
+
+// Where a warp works: its env, its channels, its segment of a window of steps.
+struct Place {
+  int64_t n, d;     // env, first channel of this thread
+  bool on;          // the thread has channels
+  int64_t len;      // steps of env n
+  __device__ __forceinline__ Place(const GlrDev& a, int64_t unit, int tiles, int lane, int V, bool any) {
+    n = unit / tiles;
+    d = ((unit - n * tiles) * 32 + lane) * V;
+    on = any && d < a.D;
+    len = any && a.lengths ? max((int64_t)0, min(a.T, (int64_t)a.lengths[n])) : any ? a.T : 0;
+  }
 };
-__device__ __forceinline__ Gates gates(float s, float r, float i) {
-  Gates g;
-  g.rho = sigmoid_f(r);
-  g.iota = sigmoid_f(i);
-  g.q = s * g.rho;
-  const float em = expm1f(-g.q);
-  g.a = 1.0f + em;
-  g.beta2 = -em * (2.0f + em);
-  return g;
+
+// The rows of a segment, one after another.  The asm keeps the compiler from carrying a
+// pointer per row and tensor through the loop over windows (over 100 registers).
+struct Walk {
+  char* p;
+  int64_t step;
+  __device__ __forceinline__ Walk(const Seq& s, const void* lane0, int esz, int64_t t) {
+    step = s.st * esz;
+    p = static_cast<char*>(const_cast<void*>(lane0)) + t * step;
+    asm volatile("" : "+l"(p), "+l"(step));
+  }
+  __device__ __forceinline__ char* next() {
+    char* q = p;
+    p += step;
+    return q;
+  }
+  __device__ __forceinline__ char* next_back() {
+    char* q = p;
+    p -= step;
+    return q;
+  }
+};
+
+// Bit k: step t0 + k begins an episode (t0 + k < len), for k < S <= 32; one byte per lane.
+template <int S>
+__device__ __forceinline__ uint32_t reset_bits(const GlrDev& a, const Place& at, int64_t t0, int lane) {
+  if (!a.reset) return 0;
+  const bool r = lane < S && t0 + lane < at.len && __ldg(a.reset + (t0 + lane) * a.N + at.n) != 0;
+  return __ballot_sync(0xFFFFFFFFu, r);
 }
 
-template <typename E>
-__global__ void glr_fwd(const GlrDev a, const float* h0, const Seq h, float* h_last, float* ckpt) {
-  const int64_t lane = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, lanes = a.N * a.D;
-  if (lane >= lanes) return;
-  const int64_t n = lane / a.D, d = lane - n * a.D;
-  const float s = kGateScale * softplus_f(a.lam[d]);
-  const int64_t len = a.lengths ? max((int64_t)0, min(a.T, (int64_t)a.lengths[n])) : a.T;
-  float y = h0 ? h0[lane] : 0.0f;
-  for (int64_t t = 0; t < a.T; ++t) {
-    if (ckpt && t % kSeg == 0) ckpt[(t / kSeg) * lanes + lane] = y;
-    if (t < len) {
-      const Gates g = gates(s, ld<E>(a.r, t, n, d), ld<E>(a.i, t, n, d));
-      const float b = sqrtf(g.beta2) * g.iota * ld<E>(a.x, t, n, d);
-      y = a.reset && a.reset[t * a.N + n] ? b : fmaf(g.a, y, b);
+// The map that reaches segment (rank, wt) of a window, from the maps (A, H) that every
+// segment publishes, and the composition of the whole window.  Segments run in the order of
+// the scan (for the backward pass the caller numbers them from the end).
+template <int V, int WT, bool kCluster>
+struct Exchange {
+  struct Shared {
+    float a[2][WT][32][V], h[2][WT][32][V];                       // maps of the CTA's warps
+    float ca[2][kMaxCluster][32][V], ch[2][kMaxCluster][32][V];   // maps of the cluster's CTAs
+  };
+  // carry: the state before the window, in; after the window, out.  in: the state before
+  // this segment.
+  __device__ __forceinline__ static void run(Shared& sh, int buf, int rank, int n_rank, int wt, int lane,
+                                             const float (&A)[V], const float (&H)[V], float (&carry)[V],
+                                             float (&in)[V]) {
+    if (WT == 1 && !kCluster) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        in[v] = carry[v];
+        carry[v] = apply(A[v], carry[v], H[v]);
+      }
+      return;
     }
-    if (h.p) st<E>(h, t, n, d, t < len ? y : 0.0f);
+    float pa[V], ph[V], ta[V], th[V];  // composition before this warp, and of all warps
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      sh.a[buf][wt][lane][v] = A[v];
+      sh.h[buf][wt][lane][v] = H[v];
+      pa[v] = ta[v] = 1.0f;
+      ph[v] = th[v] = 0.0f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WT; ++w)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (w == wt) {
+          pa[v] = ta[v];
+          ph[v] = th[v];
+        }
+        const float wa = sh.a[buf][w][lane][v];
+        th[v] = apply(wa, th[v], sh.h[buf][w][lane][v]);
+        ta[v] = wa == 0.0f ? 0.0f : ta[v] * wa;
+      }
+    if (kCluster) {
+      cg::cluster_group cl = cg::this_cluster();
+      // warp wt hands the CTA's map to the CTAs wt, wt + WT, ...
+      for (int dst = wt; dst < n_rank; dst += WT) {
+        float* ra = cl.map_shared_rank(&sh.ca[buf][rank][lane][0], dst);
+        float* rh = cl.map_shared_rank(&sh.ch[buf][rank][lane][0], dst);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          ra[v] = ta[v];
+          rh[v] = th[v];
+        }
+      }
+      cl.sync();
+#pragma unroll
+      for (int v = 0; v < V; ++v) in[v] = carry[v];
+      for (int c = 0; c < n_rank; ++c)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if (c == rank) in[v] = carry[v];
+          carry[v] = apply(sh.ca[buf][c][lane][v], carry[v], sh.ch[buf][c][lane][v]);
+        }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        in[v] = carry[v];
+        carry[v] = apply(ta[v], carry[v], th[v]);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) in[v] = apply(pa[v], in[v], ph[v]);
   }
-  if (h_last) h_last[lane] = y;
+};
+
+// CTAs of kWarps warps: WT of them share lanes, kWarps / WT lane groups.
+template <typename E, int V, int S, int WT, int kWarps, bool kCluster>
+__global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
+    glr_fwd(const __grid_constant__ GlrDev a, const float* h0, const __grid_constant__ Seq h, float* h_last,
+            float* ckpt, int n_rank) {
+  using X = Exchange<V, WT, kCluster>;
+  __shared__ typename X::Shared sh;
+  constexpr int WL = kWarps / WT;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wt = warp % WT;
+  const int rank = kCluster ? (int)(blockIdx.x % n_rank) : 0;
+  const int tiles = (a.D + 32 * V - 1) / (32 * V);
+  const int64_t unit = (int64_t)(kCluster ? blockIdx.x / n_rank : blockIdx.x) * WL + warp / WT;
+  const Place at(a, unit, tiles, lane, V, unit < a.N * tiles);
+  const int64_t lanes = a.N * a.D, me = at.n * a.D + at.d;
+  const int seg = rank * WT + wt;
+  const int64_t window = (int64_t)(kCluster ? n_rank : 1) * WT * S;
+
+  float s[V], carry[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    s[v] = at.on ? kGateScale * softplus_f(a.lam[at.d + v]) : 0.0f;
+    carry[v] = at.on && h0 ? h0[me + v] : 0.0f;
+  }
+  Vec<E, V> nx[S], nr[S], ni[S];
+  uint32_t nrs = 0;
+  const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
+  const E* pr = static_cast<const E*>(a.r.p) + at.n * a.r.sn + at.d;
+  const E* pi = static_cast<const E*>(a.i.p) + at.n * a.i.sn + at.d;
+  const E* ph = static_cast<const E*>(h.p) + at.n * h.sn + at.d;
+  auto fetch = [&](int64_t t0) {
+    Walk wr(a.r, pr, sizeof(E), t0), wi(a.i, pi, sizeof(E), t0), wx(a.x, px, sizeof(E), t0);
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      nx[k].zero();
+      nr[k].zero();
+      ni[k].zero();
+      const char *qr = wr.next(), *qi = wi.next(), *qx = wx.next();
+      if (at.on && t0 + k < at.len) {
+        nr[k].load(qr);
+        ni[k].load(qi);
+        nx[k].load(qx);
+      }
+    }
+    nrs = reset_bits<S>(a, at, t0, lane);
+  };
+  fetch((int64_t)seg * S);
+  int buf = 0;
+  for (int64_t w0 = 0; w0 < a.T; w0 += window, buf ^= 1) {
+    const int64_t t0 = w0 + (int64_t)seg * S;
+    float da[S][V], b[S][V];
+    float A[V], H[V], y[V];
+    const uint32_t rs = nrs;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      A[v] = 1.0f;
+      H[v] = 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < S; ++k)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float em = decay_m1(s[v] * sigmoid_q(nr[k].get(v)));
+        da[k][v] = 1.0f + em;
+        b[k][v] = sqrt_q(-em * (2.0f + em)) * (sigmoid_q(ni[k].get(v)) * nx[k].get(v));
+      }
+    if (w0 + window < a.T) fetch(t0 + window);
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      const bool live = t0 + k < at.len, cut = (rs >> k) & 1u;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        da[k][v] = live ? (cut ? 0.0f : da[k][v]) : 1.0f;
+        b[k][v] = live ? b[k][v] : 0.0f;
+        if (WT > 1 || kCluster) {
+          A[v] = cut ? 0.0f : A[v] * da[k][v];
+          H[v] = cut ? b[k][v] : fmaf(da[k][v], H[v], b[k][v]);
+        }
+      }
+    }
+    if (WT > 1 || kCluster) {
+      X::run(sh, buf, rank, n_rank, wt, lane, A, H, carry, y);
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) y[v] = carry[v];
+    }
+    Walk wh(h, ph, sizeof(E), t0);
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      const int64_t t = t0 + k;
+      char* q = wh.next();
+      if (ckpt && at.on && t < a.T && (S == kSeg ? k == 0 : (t % kSeg) == 0)) {
+        float* c = ckpt + (t / kSeg) * lanes + me;
+#pragma unroll
+        for (int v = 0; v < V; ++v) c[v] = y[v];
+      }
+      Vec<E, V> o;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        y[v] = apply(da[k][v], y[v], b[k][v]);
+        o.set(v, t < at.len ? y[v] : 0.0f);
+      }
+      if (h.p && at.on && t < a.T) o.store(q);
+    }
+    if (WT == 1 && !kCluster) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) carry[v] = y[v];
+    }
+  }
+  if (h_last && at.on && seg == 0) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) h_last[me + v] = carry[v];
+  }
 }
 
 struct GlrGrad {
@@ -94,76 +350,169 @@ struct GlrGrad {
   const float* dh_last;
   Seq dx, dr, di;
   float* dh0;
-  float* part;  // [N][D] sums of w over the steps of a lane
+  float* part;  // [segments of a window][N][D] sums of w over a thread's steps
 };
 
-template <typename E>
-__global__ void glr_bwd(const GlrDev a, const GlrGrad b) {
-  const int64_t lane = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, lanes = a.N * a.D;
-  if (lane >= lanes) return;
-  const int64_t n = lane / a.D, d = lane - n * a.D;
-  const float s = kGateScale * softplus_f(a.lam[d]);
-  const int64_t len = a.lengths ? max((int64_t)0, min(a.T, (int64_t)a.lengths[n])) : a.T;
-  float p = b.dh_last ? b.dh_last[lane] : 0.0f;  // gradient of the state a step leaves
-  float sum = 0.0f, comp = 0.0f;
-  for (int64_t seg = (a.T + kSeg - 1) / kSeg - 1; seg >= 0; --seg) {
-    float before[kSeg];
-    float y = b.ckpt[seg * lanes + lane];
-    const int64_t t0 = seg * kSeg;
+template <typename E, int V, int WT, int kWarps, bool kCluster>
+__global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
+    glr_bwd(const __grid_constant__ GlrDev a, const __grid_constant__ GlrGrad b, int n_rank) {
+  using X = Exchange<V, WT, kCluster>;
+  __shared__ typename X::Shared sh;
+  constexpr int S = kSeg, WL = kWarps / WT;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wt = warp % WT;
+  const int rank = kCluster ? (int)(blockIdx.x % n_rank) : 0;
+  const int tiles = (a.D + 32 * V - 1) / (32 * V);
+  const int64_t unit = (int64_t)(kCluster ? blockIdx.x / n_rank : blockIdx.x) * WL + warp / WT;
+  const Place at(a, unit, tiles, lane, V, unit < a.N * tiles);
+  const int64_t lanes = a.N * a.D, me = at.n * a.D + at.d;
+  const int n_seg = (kCluster ? n_rank : 1) * WT, seg = rank * WT + wt;  // seg 0: the latest steps
+  const int64_t window = (int64_t)n_seg * S;
+  const int64_t last = (a.T + window - 1) / window * window - (int64_t)(seg + 1) * S;  // its first t0
+
+  float s[V], carry[V], sum[V], comp[V];
 #pragma unroll
-    for (int k = 0; k < kSeg; ++k) {
-      const int64_t t = t0 + k;
-      before[k] = 0.0f;
-      if (t < len) {
-        const bool rs = a.reset && a.reset[t * a.N + n];
-        before[k] = rs ? 0.0f : y;
-        const Gates g = gates(s, ld<E>(a.r, t, n, d), ld<E>(a.i, t, n, d));
-        const float in = sqrtf(g.beta2) * g.iota * ld<E>(a.x, t, n, d);
-        y = rs ? in : fmaf(g.a, y, in);
-      }
-    }
-    float part = 0.0f;
-#pragma unroll
-    for (int k = kSeg - 1; k >= 0; --k) {
-      const int64_t t = t0 + k;
-      if (t >= a.T) continue;
-      float dx = 0.0f, dr = 0.0f, di = 0.0f;
-      if (t < len) {
-        const bool rs = a.reset && a.reset[t * a.N + n];
-        const float x = ld<E>(a.x, t, n, d);
-        const Gates g = gates(s, ld<E>(a.r, t, n, d), ld<E>(a.i, t, n, d));
-        const float beta = sqrtf(g.beta2);
-        const float G = (b.dh.p ? ld<E>(b.dh, t, n, d) : 0.0f) + p;
-        dx = G * beta * g.iota;
-        di = dx * x * (1.0f - g.iota);
-        // w = q a dL/da; q / beta -> 0 with q (beta^2 ~ 2 q)
-        const float qb = g.beta2 > 0.0f ? g.q / beta : 0.0f;
-        const float w = g.a * G * (g.q * before[k] - qb * g.a * g.iota * x);
-        dr = -(1.0f - g.rho) * w;
-        part += w;
-        p = rs ? 0.0f : g.a * G;
-      }
-      st<E>(b.dx, t, n, d, dx);
-      st<E>(b.dr, t, n, d, dr);
-      st<E>(b.di, t, n, d, di);
-    }
-    const float yk = part - comp, sk = sum + yk;  // compensated over the segments
-    comp = (sk - sum) - yk;
-    sum = sk;
+  for (int v = 0; v < V; ++v) {
+    s[v] = at.on ? kGateScale * softplus_f(a.lam[at.d + v]) : 0.0f;
+    carry[v] = at.on && b.dh_last ? b.dh_last[me + v] : 0.0f;
+    sum[v] = comp[v] = 0.0f;
   }
-  if (b.part) b.part[lane] = sum;
-  if (b.dh0) b.dh0[lane] = p;
+  Vec<E, V> nx[S], nr[S], ni[S], ng[S];
+  float nc[V];
+  uint32_t nrs = 0;
+  const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
+  const E* pr = static_cast<const E*>(a.r.p) + at.n * a.r.sn + at.d;
+  const E* pi = static_cast<const E*>(a.i.p) + at.n * a.i.sn + at.d;
+  const E* pg = static_cast<const E*>(b.dh.p) + at.n * b.dh.sn + at.d;
+  const E* pdx = static_cast<const E*>(b.dx.p) + at.n * b.dx.sn + at.d;
+  const E* pdr = static_cast<const E*>(b.dr.p) + at.n * b.dr.sn + at.d;
+  const E* pdi = static_cast<const E*>(b.di.p) + at.n * b.di.sn + at.d;
+  auto fetch = [&](int64_t t0) {
+    Walk wr(a.r, pr, sizeof(E), t0), wi(a.i, pi, sizeof(E), t0), wx(a.x, px, sizeof(E), t0), wg(b.dh, pg, sizeof(E), t0);
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      nx[k].zero();
+      nr[k].zero();
+      ni[k].zero();
+      ng[k].zero();
+      const char *qr = wr.next(), *qi = wi.next(), *qx = wx.next(), *qg = wg.next();
+      if (at.on && t0 + k < at.len) {
+        nr[k].load(qr);
+        ni[k].load(qi);
+        nx[k].load(qx);
+        if (b.dh.p) ng[k].load(qg);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) nc[v] = at.on && t0 < at.len ? __ldcs(b.ckpt + (t0 / kSeg) * lanes + me + v) : 0.0f;
+    nrs = reset_bits<S>(a, at, t0, lane);
+  };
+  if (a.T > 0) fetch(last);
+  int buf = 0;
+  for (int64_t t0 = last, w = (a.T + window - 1) / window; w > 0; --w, t0 -= window, buf ^= 1) {
+    float em[S][V], rho[S][V], iota[S][V], prev[S][V], A[V], P[V], p[V];
+    Vec<E, V> x[S], g[S];
+    const uint32_t rs = nrs;
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = nc[v];
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      x[k] = nx[k];
+      g[k] = ng[k];
+      const bool cut = (rs >> k) & 1u;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        rho[k][v] = sigmoid_q(nr[k].get(v));
+        iota[k][v] = sigmoid_q(ni[k].get(v));
+        em[k][v] = decay_m1(s[v] * rho[k][v]);
+        const float in = sqrt_q(-em[k][v] * (2.0f + em[k][v])) * (iota[k][v] * x[k].get(v));
+        prev[k][v] = cut ? 0.0f : p[v];
+        p[v] = cut ? in : fmaf(1.0f + em[k][v], p[v], in);
+      }
+    }
+    if (w > 1) fetch(t0 - window);
+    if (WT > 1 || kCluster) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        A[v] = 1.0f;
+        P[v] = 0.0f;
+      }
+#pragma unroll
+      for (int k = S - 1; k >= 0; --k) {
+        const bool cut = (rs >> k) & 1u;
+        if (t0 + k < at.len) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const float d = 1.0f + em[k][v];
+            P[v] = cut ? 0.0f : d * (g[k].get(v) + P[v]);
+            A[v] = cut ? 0.0f : A[v] * d;
+          }
+        }
+      }
+      X::run(sh, buf, rank, n_rank, wt, lane, A, P, carry, p);
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) p[v] = carry[v];
+    }
+    float part[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) part[v] = 0.0f;
+    Walk wdx(b.dx, pdx, sizeof(E), t0 + S - 1), wdr(b.dr, pdr, sizeof(E), t0 + S - 1), wdi(b.di, pdi, sizeof(E), t0 + S - 1);
+#pragma unroll
+    for (int k = S - 1; k >= 0; --k) {
+      const int64_t t = t0 + k;
+      const bool cut = (rs >> k) & 1u, live = t < at.len;
+      Vec<E, V> ox, orr, oi;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float xx = x[k].get(v), io = iota[k][v], e = em[k][v], d = 1.0f + e;
+        const float G = g[k].get(v) + p[v];
+        const float b2 = -e * (2.0f + e), q = s[v] * rho[k][v];
+        const float inv = rsqrtf(b2);
+        const float u = G * io;                             // dL/d(beta x)
+        const float dx = b2 > 0.0f ? u * (b2 * inv) : 0.0f;
+        // w = q a dL/da; q / beta -> 0 with q (beta^2 ~ 2 q)
+        const float qb = b2 > 0.0f ? q * inv * d : 0.0f;
+        const float wv = d * (q * G * prev[k][v] - qb * u * xx);
+        ox.set(v, live ? dx : 0.0f);
+        oi.set(v, live ? dx * xx * (1.0f - io) : 0.0f);
+        orr.set(v, live ? (rho[k][v] - 1.0f) * wv : 0.0f);
+        part[v] += live ? wv : 0.0f;
+        p[v] = live ? (cut ? 0.0f : d * G) : p[v];
+      }
+      char *qx = wdx.next_back(), *qr = wdr.next_back(), *qi = wdi.next_back();
+      if (at.on && t < a.T) {
+        ox.store(qx);
+        orr.store(qr);
+        oi.store(qi);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float yk = part[v] - comp[v], sk = sum[v] + yk;  // compensated over the segments
+      comp[v] = (sk - sum[v]) - yk;
+      sum[v] = sk;
+      if (WT == 1 && !kCluster) carry[v] = p[v];
+    }
+  }
+  if (!at.on) return;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    if (b.part) b.part[seg * lanes + me + v] = sum[v];
+    if (b.dh0 && seg == 0) b.dh0[me + v] = carry[v];
+  }
 }
 
-// dlam[d] = -(sum over rows of part[row][d]) sigmoid(lam) / softplus(lam), rows in a fixed
-// order: 32 row-threads per channel, then a tree.  The ratio tends to 1 as lam -> -inf.
+// Sums over rows of part[rows][D] in a fixed order: CTA (x, y) takes 32 channels and the
+// rows y, y + gridDim.y, ... ; 32 row-threads per channel, then a tree.  kLast also applies
+// dlam[d] = -sum sigmoid(lam) / softplus(lam) (the ratio tends to 1 as lam -> -inf).
+template <bool kLast>
 __global__ void glr_dlam(const float* __restrict__ part, int64_t rows, int32_t D, const float* __restrict__ lam,
-                         float* __restrict__ dlam) {
+                         float* __restrict__ out) {
   __shared__ float sh[32][33];
   const int d = blockIdx.x * 32 + threadIdx.x;
   float sum = 0.0f, comp = 0.0f;
   if (d < D)
-    for (int64_t r = threadIdx.y; r < rows; r += 32) {
+    for (int64_t r = blockIdx.y * 32 + threadIdx.y; r < rows; r += 32 * gridDim.y) {
       const float yk = part[r * D + d] - comp, sk = sum + yk;
       comp = (sk - sum) - yk;
       sum = sk;
@@ -174,8 +523,12 @@ __global__ void glr_dlam(const float* __restrict__ part, int64_t rows, int32_t D
     if (threadIdx.y < k) sh[threadIdx.y][threadIdx.x] += sh[threadIdx.y + k][threadIdx.x];
   }
   if (threadIdx.y == 0 && d < D) {
-    const float l = lam[d], sp = softplus_f(l);
-    dlam[d] = -sh[0][threadIdx.x] * (sp > 0.0f ? sigmoid_f(l) / sp : 1.0f);
+    float v = sh[0][threadIdx.x];
+    if (kLast) {
+      const float l = lam[d], sp = softplus_f(l);
+      v = -v * (sp > 0.0f ? sigmoid_f(l) / sp : 1.0f);
+    }
+    out[(int64_t)blockIdx.y * D + d] = v;
   }
 }
 
@@ -187,6 +540,8 @@ aht_status check(const aht_glr_args* a) {
     return set_last_error(AHT_EINVAL, "sizes: T >= 0, N >= 1, 1 <= D <= AHT_GLR_MAX_D");
   if (a->N > (int64_t(1) << 37) / a->D || (a->T > 0 && a->N > (int64_t(1) << 46) / a->D / a->T))
     return set_last_error(AHT_EINVAL, "N * D must be at most 2^37 and T * N * D at most 2^46");
+  if (a->N > (int64_t(1) << 32) / ((a->D + 31) / 32))  // CTAs of a launch
+    return set_last_error(AHT_EINVAL, "N * ceil(D / 32) must be at most 2^32");
   if (!a->lam) return set_last_error(AHT_EINVAL, "lam is NULL");
   if (a->T > 0 && (!a->x.data || !a->r.data || !a->i.data)) return set_last_error(AHT_EINVAL, "NULL input sequence");
   return AHT_OK;
@@ -197,13 +552,74 @@ GlrDev dev(const aht_glr_args* a) {
   return GlrDev{a->D, a->T, a->N, seq(a->x), seq(a->r), seq(a->i), a->lam, a->reset, a->lengths};
 }
 
-aht_status launched() {
-  const cudaError_t e = cudaGetLastError();
+aht_status launched(cudaError_t e) {
   return e == cudaSuccess ? AHT_OK : set_last_error(AHT_ECUDA, cudaGetErrorString(e));
 }
 
-constexpr int kBlock = 128;
-unsigned blocks_of(const aht_glr_args* a) { return (unsigned)((a->N * a->D + kBlock - 1) / kBlock); }
+// Whether V channels of every row of a sequence start on a boundary of their size.
+bool aligned(const Seq& s, int esz, int V, int64_t T, int64_t N) {
+  const uintptr_t bytes = (uintptr_t)esz * V;
+  return !s.p || ((uintptr_t)s.p % bytes == 0 && (T <= 1 || s.st % V == 0) && (N <= 1 || s.sn % V == 0));
+}
+
+// How the lanes and steps of a call are split.
+struct Split {
+  int wt, cl;      // warps of a CTA and CTAs of a cluster along time
+  int64_t units;   // groups of 32 V lanes of one env
+  int segs() const { return wt * cl; }
+};
+
+constexpr int kFill = 152 * 12;  // warps that keep every SM's loads in flight
+
+Split split_of(int64_t T, int64_t N, int32_t D, int V) {
+  Split p{1, 1, N * ((D + 32 * V - 1) / (32 * V))};
+  if (p.units >= kFill || T <= 2 * kSeg) return p;
+  p.wt = 8;
+  while (p.cl < kMaxCluster && p.units * p.wt * p.cl < kFill && (int64_t)p.wt * p.cl * 2 * kSeg <= T) p.cl *= 2;
+  return p;
+}
+
+template <typename K, typename... Args>
+aht_status launch(K kernel, int64_t blocks, int threads, int cl, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(blocks * cl));
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {(unsigned)cl, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = cl > 1 ? 1 : 0;
+  return launched(cudaLaunchKernelEx(&cfg, kernel, args...));
+}
+
+template <typename E, int V>
+aht_status forward(const aht_glr_args* a, const float* h0, const Seq& h, float* h_last, float* ckpt, cudaStream_t s) {
+  const Split p = split_of(a->T, a->N, a->D, V);
+  const GlrDev d = dev(a);
+  const int64_t four = (p.units + 3) / 4;
+  if (a->T <= 1) return launch(glr_fwd<E, V, 1, 1, 4, false>, four, 128, 1, s, d, h0, h, h_last, ckpt, 1);
+  if (p.wt == 1) return launch(glr_fwd<E, V, kSeg, 1, 4, false>, four, 128, 1, s, d, h0, h, h_last, ckpt, 1);
+  if (p.cl == 1) return launch(glr_fwd<E, V, kSeg, 8, 8, false>, p.units, 256, 1, s, d, h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, kSeg, 8, 8, true>, p.units, 256, p.cl, s, d, h0, h, h_last, ckpt, p.cl);
+}
+
+template <typename E, int V>
+aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStream_t s) {
+  const Split p = split_of(a->T, a->N, a->D, V);
+  const GlrDev d = dev(a);
+  *rows = p.segs();
+  if (p.wt == 1) return launch(glr_bwd<E, V, 1, 4, false>, (p.units + 3) / 4, 128, 1, s, d, g, 1);
+  if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false>, p.units, 256, 1, s, d, g, 1);
+  return launch(glr_bwd<E, V, 8, 8, true>, p.units, 256, p.cl, s, d, g, p.cl);
+}
+
+constexpr int kSumRows = 64;  // row groups of the first pass of dlam's sum
+
+int64_t part_floats(int64_t T, int64_t N, int32_t D) {
+  const int64_t s = std::max(split_of(T, N, D, 1).segs(), std::max(split_of(T, N, D, 2).segs(), split_of(T, N, D, 4).segs()));
+  return s * N * D;
+}
 
 }  // namespace
 
@@ -214,7 +630,7 @@ int64_t aht_glr_ckpt_elems(int64_t T, int64_t N, int32_t D) {
 }
 
 int64_t aht_glr_workspace(int64_t T, int64_t N, int32_t D) {
-  return T < 0 || N < 0 || D < 0 ? 0 : N * D * (int64_t)sizeof(float);
+  return T < 0 || N < 1 || D < 1 ? 0 : (part_floats(T, N, D) + (int64_t)kSumRows * D) * (int64_t)sizeof(float);
 }
 
 aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq* h, float* h_last, float* ckpt,
@@ -223,11 +639,16 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
   const Seq out = h ? seq(*h) : Seq{nullptr, 0, 0};
   if (!out.p && !h_last) return set_last_error(AHT_EINVAL, "neither h nor h_last is asked for");
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const int esz = a->dtype == AHT_FP32 ? 4 : 2;
+  auto fits = [&](int V) {
+    return a->D % V == 0 && aligned(seq(a->x), esz, V, a->T, a->N) && aligned(seq(a->r), esz, V, a->T, a->N) &&
+           aligned(seq(a->i), esz, V, a->T, a->N) && aligned(out, esz, V, a->T, a->N);
+  };
   if (a->dtype == AHT_FP32)
-    glr_fwd<float><<<blocks_of(a), kBlock, 0, s>>>(dev(a), h0, out, h_last, ckpt);
-  else
-    glr_fwd<__nv_bfloat16><<<blocks_of(a), kBlock, 0, s>>>(dev(a), h0, out, h_last, ckpt);
-  return launched();
+    return fits(2) && a->D >= 64 && split_of(a->T, a->N, a->D, 2).wt == 1 ? forward<float, 2>(a, h0, out, h_last, ckpt, s)
+                   : forward<float, 1>(a, h0, out, h_last, ckpt, s);
+  return fits(2) ? forward<__nv_bfloat16, 2>(a, h0, out, h_last, ckpt, s)
+                 : forward<__nv_bfloat16, 1>(a, h0, out, h_last, ckpt, s);
 }
 
 aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_seq* dh, const float* dh_last,
@@ -240,17 +661,32 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
   if (dlam && (!workspace || workspace_bytes < aht_glr_workspace(a->T, a->N, a->D)))
     return set_last_error(AHT_EINVAL, "workspace is NULL or smaller than aht_glr_workspace");
   const Seq none{nullptr, 0, 0};
+  float* part = dlam ? static_cast<float*>(workspace) : nullptr;
   const GlrGrad g{ckpt,    dh ? seq(*dh) : none, dh_last, dx ? seq(*dx) : none, dr ? seq(*dr) : none,
-                  di ? seq(*di) : none, dh0, dlam ? static_cast<float*>(workspace) : nullptr};
+                  di ? seq(*di) : none, dh0, part};
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const int esz = a->dtype == AHT_FP32 ? 4 : 2;
+  bool two = a->D % 2 == 0;
+  for (const Seq& q : {seq(a->x), seq(a->r), seq(a->i), g.dh, g.dx, g.dr, g.di})
+    two = two && aligned(q, esz, 2, a->T, a->N);
+  int segs = 1;
+  aht_status e;
   if (a->dtype == AHT_FP32)
-    glr_bwd<float><<<blocks_of(a), kBlock, 0, s>>>(dev(a), g);
+    e = backward<float, 1>(a, g, &segs, s);
   else
-    glr_bwd<__nv_bfloat16><<<blocks_of(a), kBlock, 0, s>>>(dev(a), g);
-  if (aht_status e = launched()) return e;
-  if (!dlam) return AHT_OK;
-  glr_dlam<<<(a->D + 31) / 32, dim3(32, 32), 0, s>>>(g.part, a->N, a->D, a->lam, dlam);
-  return launched();
+    e = two ? backward<__nv_bfloat16, 2>(a, g, &segs, s) : backward<__nv_bfloat16, 1>(a, g, &segs, s);
+  if (e != AHT_OK || !dlam) return e;
+  const int64_t rows = (int64_t)segs * a->N;
+  const dim3 grid((a->D + 31) / 32), block(32, 32);
+  if (rows <= 512) {
+    glr_dlam<true><<<grid, block, 0, s>>>(part, rows, a->D, a->lam, dlam);
+    return launched(cudaGetLastError());
+  }
+  float* first = part + part_floats(a->T, a->N, a->D);
+  glr_dlam<false><<<dim3(grid.x, kSumRows), block, 0, s>>>(part, rows, a->D, a->lam, first);
+  if (aht_status e2 = launched(cudaGetLastError())) return e2;
+  glr_dlam<true><<<grid, block, 0, s>>>(first, kSumRows, a->D, a->lam, dlam);
+  return launched(cudaGetLastError());
 }
 
 }  // extern "C"
