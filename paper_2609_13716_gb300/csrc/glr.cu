@@ -26,6 +26,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "tc_common.cuh"
@@ -85,27 +86,47 @@ struct Vec {
 __device__ __forceinline__ float softplus_f(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))); }
 __device__ __forceinline__ float sigmoid_f(float x) { return 1.0f / (1.0f + expf(-x)); }
 
+// ---- gates, two elements at a time (packed fp32 pairs) -------------------------------------
 constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ uint64_t both(float c) { return tc::f2_pack(c, c); }
+
 // 1 / (1 + 2^(-x log2 e)): the hardware exp2 and reciprocal, 2^-22 relative each; 0 and 1 at
 // the infinities.
-__device__ __forceinline__ float sigmoid_q(float x) {
-  return tc::rcp_approx(1.0f + tc::ex2_approx(-kLog2e * x));
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t x) {
+  float a, b;
+  tc::f2_unpack(tc::f2_mul(x, both(-kLog2e)), a, b);
+  tc::f2_unpack(tc::f2_add(tc::f2_pack(tc::ex2_approx(a), tc::ex2_approx(b)), both(1.0f)), a, b);
+  return tc::f2_pack(tc::rcp_approx(a), tc::rcp_approx(b));
 }
-// exp(-q) - 1 for q >= 0: below 1/4 its series -q (1 - q/2 + q^2/6 - ... + q^6/5040) (the
-// next term is below 2^-26 there), above it 2^(-q log2 e) - 1 (no cancellation).
-__device__ __forceinline__ float decay_m1(float q) {
-  float s = fmaf(q, 1.0f / 5040.0f, -1.0f / 720.0f);
-  s = fmaf(q, s, 1.0f / 120.0f);
-  s = fmaf(q, s, -1.0f / 24.0f);
-  s = fmaf(q, s, 1.0f / 6.0f);
-  s = fmaf(q, s, -0.5f);
-  s = fmaf(q, s, 1.0f);
-  const float big = tc::ex2_approx(-kLog2e * q) - 1.0f;
-  return q < 0.25f ? -q * s : big;
+// exp(z) - 1 for z <= 0: down to -1/4 its series z (1 + z/2 + z^2/6 + ... + z^6/5040) (the
+// next term is below 2^-26 there), beyond it 2^(z log2 e) - 1 (no cancellation).  kSmall: no
+// z of the warp lies beyond.
+template <bool kSmall>
+__device__ __forceinline__ uint64_t decay_m1(uint64_t z) {
+  uint64_t s = tc::f2_fma(z, both(1.0f / 5040.0f), both(1.0f / 720.0f));
+  s = tc::f2_fma(z, s, both(1.0f / 120.0f));
+  s = tc::f2_fma(z, s, both(1.0f / 24.0f));
+  s = tc::f2_fma(z, s, both(1.0f / 6.0f));
+  s = tc::f2_fma(z, s, both(0.5f));
+  s = tc::f2_mul(z, tc::f2_fma(z, s, both(1.0f)));
+  if (kSmall) return s;
+  float z0, z1, s0, s1, a, b;
+  tc::f2_unpack(z, z0, z1);
+  tc::f2_unpack(s, s0, s1);
+  tc::f2_unpack(tc::f2_mul(z, both(kLog2e)), a, b);
+  tc::f2_unpack(tc::f2_add(tc::f2_pack(tc::ex2_approx(a), tc::ex2_approx(b)), both(-1.0f)), a, b);
+  return tc::f2_pack(z0 > -0.25f ? s0 : a, z1 > -0.25f ? s1 : b);
 }
+// beta^2 = 1 - a^2 = em (-2 - em)
+__device__ __forceinline__ uint64_t beta_sq(uint64_t em) { return tc::f2_mul(em, tc::f2_fma(em, both(-1.0f), both(-2.0f))); }
 __device__ __forceinline__ float sqrt_q(float x) {
   float y;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rsqrt_q(float x) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 // A y + b, or b alone where A is 0.
@@ -237,6 +258,8 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
             float* ckpt, int n_rank) {
   using X = Exchange<V, WT, kCluster>;
   __shared__ typename X::Shared sh;
+  constexpr int kE = S * V;
+  static_assert(kE % 2 == 0 && (S >= kSeg ? S == kSeg : kSeg % S == 0), "pairs of elements; segments within checkpoints");
   constexpr int WL = kWarps / WT;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wt = warp % WT;
   const int rank = kCluster ? (int)(blockIdx.x % n_rank) : 0;
@@ -247,12 +270,15 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   const int seg = rank * WT + wt;
   const int64_t window = (int64_t)(kCluster ? n_rank : 1) * WT * S;
 
-  float s[V], carry[V];
+  float m[V], carry[V];  // m = -s
+  bool small = true;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    s[v] = at.on ? kGateScale * softplus_f(a.lam[at.d + v]) : 0.0f;
+    m[v] = at.on ? -kGateScale * softplus_f(a.lam[at.d + v]) : 0.0f;
+    small = small && m[v] > -0.25f;
     carry[v] = at.on && h0 ? h0[me + v] : 0.0f;
   }
+  small = __all_sync(0xFFFFFFFFu, small);
   Vec<E, V> nx[S], nr[S], ni[S];
   uint32_t nrs = 0;
   const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
@@ -279,59 +305,92 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   int buf = 0;
   for (int64_t w0 = 0; w0 < a.T; w0 += window, buf ^= 1) {
     const int64_t t0 = w0 + (int64_t)seg * S;
-    float da[S][V], b[S][V];
-    float A[V], H[V], y[V];
     const uint32_t rs = nrs;
+    // a full segment without a reset needs no masks
+    const bool plain = rs == 0 && t0 + S <= at.len;
+    float da[kE], b[kE];  // decay and input of element k V + v
+    float y[V];
+    auto gate = [&](auto small_c) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      A[v] = 1.0f;
-      H[v] = 0.0f;
-    }
-#pragma unroll
-    for (int k = 0; k < S; ++k)
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float em = decay_m1(s[v] * sigmoid_q(nr[k].get(v)));
-        da[k][v] = 1.0f + em;
-        b[k][v] = sqrt_q(-em * (2.0f + em)) * (sigmoid_q(ni[k].get(v)) * nx[k].get(v));
+      for (int e = 0; e < kE; e += 2) {
+        const int k0 = e / V, v0 = e % V, k1 = (e + 1) / V, v1 = (e + 1) % V;
+        const uint64_t rho = sigmoid2(tc::f2_pack(nr[k0].get(v0), nr[k1].get(v1)));
+        const uint64_t em = decay_m1<decltype(small_c)::value>(tc::f2_mul(tc::f2_pack(m[v0], m[v1]), rho));
+        const uint64_t iota = sigmoid2(tc::f2_pack(ni[k0].get(v0), ni[k1].get(v1)));
+        float b0, b1;
+        tc::f2_unpack(beta_sq(em), b0, b1);
+        const uint64_t ix = tc::f2_mul(iota, tc::f2_pack(nx[k0].get(v0), nx[k1].get(v1)));
+        tc::f2_unpack(tc::f2_mul(tc::f2_pack(sqrt_q(b0), sqrt_q(b1)), ix), b[e], b[e + 1]);
+        tc::f2_unpack(tc::f2_add(em, both(1.0f)), da[e], da[e + 1]);
       }
+    };
+    if (small) gate(std::true_type());
+    else gate(std::false_type());
     if (w0 + window < a.T) fetch(t0 + window);
+    if (!plain) {
 #pragma unroll
-    for (int k = 0; k < S; ++k) {
-      const bool live = t0 + k < at.len, cut = (rs >> k) & 1u;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        da[k][v] = live ? (cut ? 0.0f : da[k][v]) : 1.0f;
-        b[k][v] = live ? b[k][v] : 0.0f;
-        if (WT > 1 || kCluster) {
-          A[v] = cut ? 0.0f : A[v] * da[k][v];
-          H[v] = cut ? b[k][v] : fmaf(da[k][v], H[v], b[k][v]);
-        }
+      for (int e = 0; e < kE; ++e) {
+        const int k = e / V;
+        const bool live = t0 + k < at.len;
+        da[e] = live ? ((rs >> k) & 1u ? 0.0f : da[e]) : 1.0f;
+        b[e] = live ? b[e] : 0.0f;
       }
     }
     if (WT > 1 || kCluster) {
+      float A[V], H[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        A[v] = da[v];
+        H[v] = b[v];
+      }
+      if (plain) {
+#pragma unroll
+        for (int e = V; e < kE; ++e) {
+          H[e % V] = fmaf(da[e], H[e % V], b[e]);
+          A[e % V] *= da[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = V; e < kE; ++e) {
+          H[e % V] = apply(da[e], H[e % V], b[e]);
+          A[e % V] = da[e] == 0.0f ? 0.0f : A[e % V] * da[e];
+        }
+      }
       X::run(sh, buf, rank, n_rank, wt, lane, A, H, carry, y);
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) y[v] = carry[v];
     }
+    if (ckpt && at.on && t0 < a.T && (S >= kSeg || t0 % kSeg == 0)) {
+      float* c = ckpt + (t0 / kSeg) * lanes + me;
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] = y[v];
+    }
     Walk wh(h, ph, sizeof(E), t0);
+    if (plain) {
 #pragma unroll
-    for (int k = 0; k < S; ++k) {
-      const int64_t t = t0 + k;
-      char* q = wh.next();
-      if (ckpt && at.on && t < a.T && (S == kSeg ? k == 0 : (t % kSeg) == 0)) {
-        float* c = ckpt + (t / kSeg) * lanes + me;
+      for (int k = 0; k < S; ++k) {
+        Vec<E, V> o;
 #pragma unroll
-        for (int v = 0; v < V; ++v) c[v] = y[v];
+        for (int v = 0; v < V; ++v) {
+          y[v] = fmaf(da[k * V + v], y[v], b[k * V + v]);
+          o.set(v, y[v]);
+        }
+        char* q = wh.next();
+        if (h.p && at.on) o.store(q);
       }
-      Vec<E, V> o;
+    } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        y[v] = apply(da[k][v], y[v], b[k][v]);
-        o.set(v, t < at.len ? y[v] : 0.0f);
+      for (int k = 0; k < S; ++k) {
+        Vec<E, V> o;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          y[v] = apply(da[k * V + v], y[v], b[k * V + v]);
+          o.set(v, t0 + k < at.len ? y[v] : 0.0f);
+        }
+        char* q = wh.next();
+        if (h.p && at.on && t0 + k < a.T) o.store(q);
       }
-      if (h.p && at.on && t < a.T) o.store(q);
     }
     if (WT == 1 && !kCluster) {
 #pragma unroll
@@ -353,12 +412,13 @@ struct GlrGrad {
   float* part;  // [segments of a window][N][D] sums of w over a thread's steps
 };
 
-template <typename E, int V, int WT, int kWarps, bool kCluster>
+// kAhead: the next segment is loaded while the present one is computed (registers allowing).
+template <typename E, int V, int WT, int kWarps, bool kCluster, bool kAhead>
 __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     glr_bwd(const __grid_constant__ GlrDev a, const __grid_constant__ GlrGrad b, int n_rank) {
   using X = Exchange<V, WT, kCluster>;
   __shared__ typename X::Shared sh;
-  constexpr int S = kSeg, WL = kWarps / WT;
+  constexpr int S = kSeg, WL = kWarps / WT, kE = S * V;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wt = warp % WT;
   const int rank = kCluster ? (int)(blockIdx.x % n_rank) : 0;
   const int tiles = (a.D + 32 * V - 1) / (32 * V);
@@ -369,13 +429,16 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   const int64_t window = (int64_t)n_seg * S;
   const int64_t last = (a.T + window - 1) / window * window - (int64_t)(seg + 1) * S;  // its first t0
 
-  float s[V], carry[V], sum[V], comp[V];
+  float m[V], carry[V], sum[V], comp[V];
+  bool small = true;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    s[v] = at.on ? kGateScale * softplus_f(a.lam[at.d + v]) : 0.0f;
+    m[v] = at.on ? -kGateScale * softplus_f(a.lam[at.d + v]) : 0.0f;
+    small = small && m[v] > -0.25f;
     carry[v] = at.on && b.dh_last ? b.dh_last[me + v] : 0.0f;
     sum[v] = comp[v] = 0.0f;
   }
+  small = __all_sync(0xFFFFFFFFu, small);
   Vec<E, V> nx[S], nr[S], ni[S], ng[S];
   float nc[V];
   uint32_t nrs = 0;
@@ -388,6 +451,8 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   const E* pdi = static_cast<const E*>(b.di.p) + at.n * b.di.sn + at.d;
   auto fetch = [&](int64_t t0) {
     Walk wr(a.r, pr, sizeof(E), t0), wi(a.i, pi, sizeof(E), t0), wx(a.x, px, sizeof(E), t0), wg(b.dh, pg, sizeof(E), t0);
+#pragma unroll
+    for (int v = 0; v < V; ++v) nc[v] = at.on && t0 < at.len ? __ldcs(b.ckpt + (t0 / kSeg) * lanes + me + v) : 0.0f;
 #pragma unroll
     for (int k = 0; k < S; ++k) {
       nx[k].zero();
@@ -402,50 +467,69 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         if (b.dh.p) ng[k].load(qg);
       }
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) nc[v] = at.on && t0 < at.len ? __ldcs(b.ckpt + (t0 / kSeg) * lanes + me + v) : 0.0f;
     nrs = reset_bits<S>(a, at, t0, lane);
   };
-  if (a.T > 0) fetch(last);
+  if (kAhead && a.T > 0) fetch(last);
   int buf = 0;
   for (int64_t t0 = last, w = (a.T + window - 1) / window; w > 0; --w, t0 -= window, buf ^= 1) {
-    float em[S][V], rho[S][V], iota[S][V], prev[S][V], A[V], P[V], p[V];
+    if (!kAhead) fetch(t0);
+    float em[kE], rho[kE], iota[kE], prev[kE], p[V];
     Vec<E, V> x[S], g[S];
     const uint32_t rs = nrs;
+    const bool plain = rs == 0 && t0 + S <= at.len;  // no masks needed
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = nc[v];
 #pragma unroll
     for (int k = 0; k < S; ++k) {
       x[k] = nx[k];
       g[k] = ng[k];
-      const bool cut = (rs >> k) & 1u;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        rho[k][v] = sigmoid_q(nr[k].get(v));
-        iota[k][v] = sigmoid_q(ni[k].get(v));
-        em[k][v] = decay_m1(s[v] * rho[k][v]);
-        const float in = sqrt_q(-em[k][v] * (2.0f + em[k][v])) * (iota[k][v] * x[k].get(v));
-        prev[k][v] = cut ? 0.0f : p[v];
-        p[v] = cut ? in : fmaf(1.0f + em[k][v], p[v], in);
-      }
     }
-    if (w > 1) fetch(t0 - window);
+    // gates; prev holds beta iota x until the states are rebuilt
+    auto gate = [&](auto small_c) {
+#pragma unroll
+      for (int e = 0; e < kE; e += 2) {
+        const int k0 = e / V, v0 = e % V, k1 = (e + 1) / V, v1 = (e + 1) % V;
+        const uint64_t rh = sigmoid2(tc::f2_pack(nr[k0].get(v0), nr[k1].get(v1)));
+        const uint64_t z = decay_m1<decltype(small_c)::value>(tc::f2_mul(tc::f2_pack(m[v0], m[v1]), rh));
+        const uint64_t io = sigmoid2(tc::f2_pack(ni[k0].get(v0), ni[k1].get(v1)));
+        float b0, b1;
+        tc::f2_unpack(beta_sq(z), b0, b1);
+        const uint64_t ix = tc::f2_mul(io, tc::f2_pack(x[k0].get(v0), x[k1].get(v1)));
+        tc::f2_unpack(tc::f2_mul(tc::f2_pack(sqrt_q(b0), sqrt_q(b1)), ix), prev[e], prev[e + 1]);
+        tc::f2_unpack(rh, rho[e], rho[e + 1]);
+        tc::f2_unpack(io, iota[e], iota[e + 1]);
+        tc::f2_unpack(z, em[e], em[e + 1]);
+      }
+    };
+    if (small) gate(std::true_type());
+    else gate(std::false_type());
+    if (kAhead && w > 1) fetch(t0 - window);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const int k = e / V, v = e % V;
+      const float in = prev[e];
+      if (!plain && ((rs >> k) & 1u)) p[v] = 0.0f;
+      prev[e] = p[v];
+      p[v] = fmaf(p[v], em[e], p[v]) + in;
+    }
     if (WT > 1 || kCluster) {
+      float A[V], P[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         A[v] = 1.0f;
         P[v] = 0.0f;
       }
 #pragma unroll
-      for (int k = S - 1; k >= 0; --k) {
-        const bool cut = (rs >> k) & 1u;
-        if (t0 + k < at.len) {
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            const float d = 1.0f + em[k][v];
-            P[v] = cut ? 0.0f : d * (g[k].get(v) + P[v]);
-            A[v] = cut ? 0.0f : A[v] * d;
-          }
+      for (int e = kE - 1; e >= 0; --e) {
+        const int k = e / V, v = e % V;
+        const float d = 1.0f + em[e];
+        if (plain) {
+          P[v] = d * (g[k].get(v) + P[v]);
+          A[v] *= d;
+        } else if (t0 + k < at.len) {
+          const bool cut = (rs >> k) & 1u;
+          P[v] = cut ? 0.0f : d * (g[k].get(v) + P[v]);
+          A[v] = cut ? 0.0f : A[v] * d;
         }
       }
       X::run(sh, buf, rank, n_rank, wt, lane, A, P, carry, p);
@@ -457,35 +541,41 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
 #pragma unroll
     for (int v = 0; v < V; ++v) part[v] = 0.0f;
     Walk wdx(b.dx, pdx, sizeof(E), t0 + S - 1), wdr(b.dr, pdr, sizeof(E), t0 + S - 1), wdi(b.di, pdi, sizeof(E), t0 + S - 1);
+    auto grads = [&](auto plain_c) {
+      constexpr bool kPlain = decltype(plain_c)::value;
 #pragma unroll
-    for (int k = S - 1; k >= 0; --k) {
-      const int64_t t = t0 + k;
-      const bool cut = (rs >> k) & 1u, live = t < at.len;
-      Vec<E, V> ox, orr, oi;
+      for (int k = S - 1; k >= 0; --k) {
+        const bool live = kPlain || t0 + k < at.len, cut = !kPlain && ((rs >> k) & 1u);
+        Vec<E, V> ox, orr, oi;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float xx = x[k].get(v), io = iota[k][v], e = em[k][v], d = 1.0f + e;
-        const float G = g[k].get(v) + p[v];
-        const float b2 = -e * (2.0f + e), q = s[v] * rho[k][v];
-        const float inv = rsqrtf(b2);
-        const float u = G * io;                             // dL/d(beta x)
-        const float dx = b2 > 0.0f ? u * (b2 * inv) : 0.0f;
-        // w = q a dL/da; q / beta -> 0 with q (beta^2 ~ 2 q)
-        const float qb = b2 > 0.0f ? q * inv * d : 0.0f;
-        const float wv = d * (q * G * prev[k][v] - qb * u * xx);
-        ox.set(v, live ? dx : 0.0f);
-        oi.set(v, live ? dx * xx * (1.0f - io) : 0.0f);
-        orr.set(v, live ? (rho[k][v] - 1.0f) * wv : 0.0f);
-        part[v] += live ? wv : 0.0f;
-        p[v] = live ? (cut ? 0.0f : d * G) : p[v];
+        for (int v = 0; v < V; ++v) {
+          const int e = k * V + v;
+          const float xx = x[k].get(v), io = iota[e], z = em[e], d = 1.0f + z;
+          const float G = g[k].get(v) + p[v];
+          const float b2 = z * (-2.0f - z), nq = m[v] * rho[e];     // nq = -q
+          // 1 / beta, finite where beta = 0: dx is 0 there, and q / beta -> 0 with q
+          const float inv = rsqrt_q(fmaxf(b2, 1e-37f));
+          const float u = G * io;                                   // dL/d(beta x)
+          const float dx = u * (b2 * inv);
+          // w = -q a dL/da = a (-q G prev + (q / beta) a u x)
+          const float wv = d * (nq * (G * prev[e] - (inv * d) * (u * xx)));
+          const float dr = wv - rho[e] * wv, di = (dx * xx) * (1.0f - io);
+          ox.set(v, live ? dx : 0.0f);
+          oi.set(v, live ? di : 0.0f);
+          orr.set(v, live ? dr : 0.0f);
+          part[v] += live ? wv : 0.0f;
+          p[v] = live ? (cut ? 0.0f : d * G) : p[v];
+        }
+        char *qx = wdx.next_back(), *qr = wdr.next_back(), *qi = wdi.next_back();
+        if (at.on && (kPlain || t0 + k < a.T)) {
+          ox.store(qx);
+          orr.store(qr);
+          oi.store(qi);
+        }
       }
-      char *qx = wdx.next_back(), *qr = wdr.next_back(), *qi = wdi.next_back();
-      if (at.on && t < a.T) {
-        ox.store(qx);
-        orr.store(qr);
-        oi.store(qi);
-      }
-    }
+    };
+    if (plain) grads(std::true_type());
+    else grads(std::false_type());
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const float yk = part[v] - comp[v], sk = sum[v] + yk;  // compensated over the segments
@@ -497,7 +587,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   if (!at.on) return;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if (b.part) b.part[seg * lanes + me + v] = sum[v];
+    if (b.part) b.part[seg * lanes + me + v] = -sum[v];
     if (b.dh0 && seg == 0) b.dh0[me + v] = carry[v];
   }
 }
@@ -593,15 +683,20 @@ aht_status launch(K kernel, int64_t blocks, int threads, int cl, cudaStream_t s,
   return launched(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
+// Many lanes (or T = 1): a warp per group of 32 V lanes.
+template <typename E, int V, int S>
+aht_status forward_wide(const aht_glr_args* a, const float* h0, const Seq& h, float* h_last, float* ckpt, cudaStream_t s) {
+  const int64_t four = (split_of(a->T, a->N, a->D, V).units + 3) / 4;
+  constexpr int kShort = V > 1 ? 1 : 2;  // steps of a segment when T = 1 (elements go in pairs)
+  if (a->T <= 1) return launch(glr_fwd<E, V, kShort, 1, 4, false>, four, 128, 1, s, dev(a), h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, S, 1, 4, false>, four, 128, 1, s, dev(a), h0, h, h_last, ckpt, 1);
+}
+// Few lanes: 8 warps and p.cl CTAs along time.
 template <typename E, int V>
-aht_status forward(const aht_glr_args* a, const float* h0, const Seq& h, float* h_last, float* ckpt, cudaStream_t s) {
-  const Split p = split_of(a->T, a->N, a->D, V);
-  const GlrDev d = dev(a);
-  const int64_t four = (p.units + 3) / 4;
-  if (a->T <= 1) return launch(glr_fwd<E, V, 1, 1, 4, false>, four, 128, 1, s, d, h0, h, h_last, ckpt, 1);
-  if (p.wt == 1) return launch(glr_fwd<E, V, kSeg, 1, 4, false>, four, 128, 1, s, d, h0, h, h_last, ckpt, 1);
-  if (p.cl == 1) return launch(glr_fwd<E, V, kSeg, 8, 8, false>, p.units, 256, 1, s, d, h0, h, h_last, ckpt, 1);
-  return launch(glr_fwd<E, V, kSeg, 8, 8, true>, p.units, 256, p.cl, s, d, h0, h, h_last, ckpt, p.cl);
+aht_status forward_long(const aht_glr_args* a, const Split& p, const float* h0, const Seq& h, float* h_last, float* ckpt,
+                        cudaStream_t s) {
+  if (p.cl == 1) return launch(glr_fwd<E, V, kSeg, 8, 8, false>, p.units, 256, 1, s, dev(a), h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, kSeg, 8, 8, true>, p.units, 256, p.cl, s, dev(a), h0, h, h_last, ckpt, p.cl);
 }
 
 template <typename E, int V>
@@ -609,9 +704,10 @@ aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStre
   const Split p = split_of(a->T, a->N, a->D, V);
   const GlrDev d = dev(a);
   *rows = p.segs();
-  if (p.wt == 1) return launch(glr_bwd<E, V, 1, 4, false>, (p.units + 3) / 4, 128, 1, s, d, g, 1);
-  if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false>, p.units, 256, 1, s, d, g, 1);
-  return launch(glr_bwd<E, V, 8, 8, true>, p.units, 256, p.cl, s, d, g, p.cl);
+  constexpr bool kAhead = V == 1;
+  if (p.wt == 1) return launch(glr_bwd<E, V, 1, 4, false, kAhead>, (p.units + 3) / 4, 128, 1, s, d, g, 1);
+  if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kAhead>, p.units, 256, 1, s, d, g, 1);
+  return launch(glr_bwd<E, V, 8, 8, true, kAhead>, p.units, 256, p.cl, s, d, g, p.cl);
 }
 
 constexpr int kSumRows = 64;  // row groups of the first pass of dlam's sum
@@ -644,11 +740,19 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
     return a->D % V == 0 && aligned(seq(a->x), esz, V, a->T, a->N) && aligned(seq(a->r), esz, V, a->T, a->N) &&
            aligned(seq(a->i), esz, V, a->T, a->N) && aligned(out, esz, V, a->T, a->N);
   };
-  if (a->dtype == AHT_FP32)
-    return fits(2) && a->D >= 64 && split_of(a->T, a->N, a->D, 2).wt == 1 ? forward<float, 2>(a, h0, out, h_last, ckpt, s)
-                   : forward<float, 1>(a, h0, out, h_last, ckpt, s);
-  return fits(2) ? forward<__nv_bfloat16, 2>(a, h0, out, h_last, ckpt, s)
-                 : forward<__nv_bfloat16, 1>(a, h0, out, h_last, ckpt, s);
+  auto wide = [&](int V) { return a->T <= 1 || split_of(a->T, a->N, a->D, V).wt == 1; };
+  if (a->dtype == AHT_FP32) {
+    if (fits(4) && a->D >= 128 && wide(4)) return forward_wide<float, 4, 4>(a, h0, out, h_last, ckpt, s);
+    if (wide(1)) return forward_wide<float, 1, kSeg>(a, h0, out, h_last, ckpt, s);
+    return forward_long<float, 1>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
+  }
+  if (fits(4) && a->D >= 128 && wide(4)) return forward_wide<__nv_bfloat16, 4, 4>(a, h0, out, h_last, ckpt, s);
+  if (fits(2)) {
+    if (wide(2)) return forward_wide<__nv_bfloat16, 2, kSeg>(a, h0, out, h_last, ckpt, s);
+    return forward_long<__nv_bfloat16, 2>(a, split_of(a->T, a->N, a->D, 2), h0, out, h_last, ckpt, s);
+  }
+  if (wide(1)) return forward_wide<__nv_bfloat16, 1, kSeg>(a, h0, out, h_last, ckpt, s);
+  return forward_long<__nv_bfloat16, 1>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
 }
 
 aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_seq* dh, const float* dh_last,
