@@ -197,37 +197,53 @@ struct Exchange {
       }
       return;
     }
-    float pa[V], ph[V], ta[V], th[V];  // composition before this warp, and of all warps
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       sh.a[buf][wt][lane][v] = A[v];
       sh.h[buf][wt][lane][v] = H[v];
-      pa[v] = ta[v] = 1.0f;
-      ph[v] = th[v] = 0.0f;
     }
     __syncthreads();
+    float pa[V], ph[V], wa[WT][V], wh[WT][V];  // pa, ph: composition before this warp
 #pragma unroll
     for (int w = 0; w < WT; ++w)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        if (w == wt) {
-          pa[v] = ta[v];
-          ph[v] = th[v];
-        }
-        const float wa = sh.a[buf][w][lane][v];
-        th[v] = apply(wa, th[v], sh.h[buf][w][lane][v]);
-        ta[v] = wa == 0.0f ? 0.0f : ta[v] * wa;
+        wa[w][v] = sh.a[buf][w][lane][v];
+        wh[w][v] = sh.h[buf][w][lane][v];
       }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      pa[v] = 1.0f;
+      ph[v] = 0.0f;
+    }
+    auto then = [&](float (&ca)[V], float (&ch)[V], int w) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        ch[v] = apply(wa[w][v], ch[v], wh[w][v]);
+        ca[v] = wa[w][v] == 0.0f ? 0.0f : ca[v] * wa[w][v];
+      }
+    };
+#pragma unroll
+    for (int w = 0; w < WT; ++w)
+      if (w < wt) then(pa, ph, w);
     if (kCluster) {
       cg::cluster_group cl = cg::this_cluster();
-      // warp wt hands the CTA's map to the CTAs wt, wt + WT, ...
-      for (int dst = wt; dst < n_rank; dst += WT) {
-        float* ra = cl.map_shared_rank(&sh.ca[buf][rank][lane][0], dst);
-        float* rh = cl.map_shared_rank(&sh.ch[buf][rank][lane][0], dst);
+      if (wt == WT - 1) {  // the last warp has the CTA's map: to every CTA of the cluster
+        float ta[V], th[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          ra[v] = ta[v];
-          rh[v] = th[v];
+          ta[v] = pa[v];
+          th[v] = ph[v];
+        }
+        then(ta, th, WT - 1);
+        for (int dst = 0; dst < n_rank; ++dst) {
+          float* ra = cl.map_shared_rank(&sh.ca[buf][rank][lane][0], dst);
+          float* rh = cl.map_shared_rank(&sh.ch[buf][rank][lane][0], dst);
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            ra[v] = ta[v];
+            rh[v] = th[v];
+          }
         }
       }
       cl.sync();
@@ -241,10 +257,11 @@ struct Exchange {
         }
     } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        in[v] = carry[v];
-        carry[v] = apply(ta[v], carry[v], th[v]);
-      }
+      for (int v = 0; v < V; ++v) in[v] = carry[v];
+#pragma unroll
+      for (int w = 0; w < WT; ++w)
+#pragma unroll
+        for (int v = 0; v < V; ++v) carry[v] = apply(wa[w][v], carry[v], wh[w][v]);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) in[v] = apply(pa[v], in[v], ph[v]);
@@ -259,7 +276,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   using X = Exchange<V, WT, kCluster>;
   __shared__ typename X::Shared sh;
   constexpr int kE = S * V;
-  static_assert(kE % 2 == 0 && (S >= kSeg ? S == kSeg : kSeg % S == 0), "pairs of elements; segments within checkpoints");
+  static_assert(kE % 2 == 0 && (S % kSeg == 0 || kSeg % S == 0), "pairs of elements; segments and checkpoints nest");
   constexpr int WL = kWarps / WT;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wt = warp % WT;
   const int rank = kCluster ? (int)(blockIdx.x % n_rank) : 0;
@@ -361,15 +378,18 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
 #pragma unroll
       for (int v = 0; v < V; ++v) y[v] = carry[v];
     }
-    if (ckpt && at.on && t0 < a.T && (S >= kSeg || t0 % kSeg == 0)) {
-      float* c = ckpt + (t0 / kSeg) * lanes + me;
+    auto save = [&](int k) {  // the state before step t0 + k
+      if (ckpt && at.on && t0 + k < a.T && (S >= kSeg ? k % kSeg == 0 : k == 0 && t0 % kSeg == 0)) {
+        float* c = ckpt + ((t0 + k) / kSeg) * lanes + me;
 #pragma unroll
-      for (int v = 0; v < V; ++v) c[v] = y[v];
-    }
+        for (int v = 0; v < V; ++v) c[v] = y[v];
+      }
+    };
     Walk wh(h, ph, sizeof(E), t0);
     if (plain) {
 #pragma unroll
       for (int k = 0; k < S; ++k) {
+        if (k % kSeg == 0) save(k);
         Vec<E, V> o;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -382,6 +402,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     } else {
 #pragma unroll
       for (int k = 0; k < S; ++k) {
+        if (k % kSeg == 0) save(k);
         Vec<E, V> o;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -692,11 +713,11 @@ aht_status forward_wide(const aht_glr_args* a, const float* h0, const Seq& h, fl
   return launch(glr_fwd<E, V, S, 1, 4, false>, four, 128, 1, s, dev(a), h0, h, h_last, ckpt, 1);
 }
 // Few lanes: 8 warps and p.cl CTAs along time.
-template <typename E, int V>
+template <typename E, int V, int S>
 aht_status forward_long(const aht_glr_args* a, const Split& p, const float* h0, const Seq& h, float* h_last, float* ckpt,
                         cudaStream_t s) {
-  if (p.cl == 1) return launch(glr_fwd<E, V, kSeg, 8, 8, false>, p.units, 256, 1, s, dev(a), h0, h, h_last, ckpt, 1);
-  return launch(glr_fwd<E, V, kSeg, 8, 8, true>, p.units, 256, p.cl, s, dev(a), h0, h, h_last, ckpt, p.cl);
+  if (p.cl == 1) return launch(glr_fwd<E, V, S, 8, 8, false>, p.units, 256, 1, s, dev(a), h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, S, 8, 8, true>, p.units, 256, p.cl, s, dev(a), h0, h, h_last, ckpt, p.cl);
 }
 
 template <typename E, int V>
@@ -740,19 +761,22 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
     return a->D % V == 0 && aligned(seq(a->x), esz, V, a->T, a->N) && aligned(seq(a->r), esz, V, a->T, a->N) &&
            aligned(seq(a->i), esz, V, a->T, a->N) && aligned(out, esz, V, a->T, a->N);
   };
+  // groups of 32 V channels that leave at most one thread in `of` without channels
+  auto fills = [&](int V, int of) { return (a->D + 32 * V - 1) / (32 * V) * 32 * V <= a->D + a->D / of; };
   auto wide = [&](int V) { return a->T <= 1 || split_of(a->T, a->N, a->D, V).wt == 1; };
   if (a->dtype == AHT_FP32) {
-    if (fits(4) && a->D >= 128 && wide(4)) return forward_wide<float, 4, 4>(a, h0, out, h_last, ckpt, s);
+    if (fits(4) && fills(4, 8) && wide(4)) return forward_wide<float, 4, 4>(a, h0, out, h_last, ckpt, s);
+    if (fits(2) && fills(2, 3) && wide(2)) return forward_wide<float, 2, kSeg>(a, h0, out, h_last, ckpt, s);
     if (wide(1)) return forward_wide<float, 1, kSeg>(a, h0, out, h_last, ckpt, s);
-    return forward_long<float, 1>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
+    return forward_long<float, 1, 2 * kSeg>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
   }
-  if (fits(4) && a->D >= 128 && wide(4)) return forward_wide<__nv_bfloat16, 4, 4>(a, h0, out, h_last, ckpt, s);
+  if (fits(4) && fills(4, 8) && wide(4)) return forward_wide<__nv_bfloat16, 4, 4>(a, h0, out, h_last, ckpt, s);
   if (fits(2)) {
     if (wide(2)) return forward_wide<__nv_bfloat16, 2, kSeg>(a, h0, out, h_last, ckpt, s);
-    return forward_long<__nv_bfloat16, 2>(a, split_of(a->T, a->N, a->D, 2), h0, out, h_last, ckpt, s);
+    return forward_long<__nv_bfloat16, 2, kSeg>(a, split_of(a->T, a->N, a->D, 2), h0, out, h_last, ckpt, s);
   }
   if (wide(1)) return forward_wide<__nv_bfloat16, 1, kSeg>(a, h0, out, h_last, ckpt, s);
-  return forward_long<__nv_bfloat16, 1>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
+  return forward_long<__nv_bfloat16, 1, 2 * kSeg>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
 }
 
 aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_seq* dh, const float* dh_last,
