@@ -20,6 +20,7 @@
 // r / 8) at ((c / 8) * 16 + r / 8) * 128, 32 KB contiguous, so a block moves by one bulk
 // copy and serves as a K-major operand (rows as M or N, columns as K) or as an MN-major one
 // (columns as M or N, rows as K).
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -41,20 +42,25 @@ namespace {
 
 constexpr int kB = 128;                        // block edge
 constexpr uint32_t kBlk = kB * kB * 2;         // bytes of one fp16 block
-constexpr int kSlots = 6;                      // blocks in flight per CTA
+constexpr uint32_t kHalf = kBlk / 2;           // 64 of K of one block
+constexpr uint32_t kStage = 4 * kHalf;         // lo of B, hi and lo of A, hi of B
+constexpr int kStages = 3;
+constexpr int kAcc = 4;                        // accumulators in tensor memory
 constexpr int kGemmThreads = 320;              // producer, MMA, 8 epilogue warps
 constexpr int kEpiThreads = 256;
 constexpr float kA = 3.4445f, kBq = -4.7750f, kC = 2.0315f;  // Jordan et al. 2024
 constexpr float kSX = 16384.0f, kSA = 16384.0f, kSB = 8192.0f;
-constexpr int kNormBlocks = 64;                // partial sums of squares per matrix
+constexpr int kNormBlocks = 256;               // most partial sums of squares per matrix
+constexpr int kMaxSteps = 32;
 
 struct Mat {
   int32_t rows, cols, m, n, mb, nb, tall;
+  int32_t norm_blocks;                         // partial sums of squares
   int64_t x[2], a, b;                          // byte offsets of the hi blocks
   int64_t x_lo, s_lo;                          // from a hi block to its lo block
 };
 
-enum Phase : int { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
+enum Phase : int { kGram = 0, kPoly = 1, kApply = 2 };
 
 // The caller's arrays of one call, by value (at most AHT_MUON_MAX_MATRICES).
 struct Ptrs {
@@ -68,7 +74,10 @@ struct Common {
   const Mat* mats;
   uint8_t* ws;
   double* norm;                                // [n_mats][kNormBlocks]
+  uint32_t* done;                              // [n_mats][3 phases][kMaxSteps] finished tiles
   uint32_t* status;
+  const int4* items;                           // (matrix, phase, I, J) of one step
+  int32_t n_items, steps;
   int32_t bf16_in, bf16_out, update, nesterov;
   float mu, eps, decay, lr;                    // decay = 1 - lr * weight_decay
 };
@@ -80,16 +89,19 @@ __device__ __forceinline__ float load_in(const Common& c, const Ptrs& p, int k, 
 }
 
 // ---- momentum and the sum of squares of U ------------------------------------------------
+// Also clears the tile counters of the call.
 __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Common c, const __grid_constant__ Ptrs p) {
   const int k = blockIdx.y;
   const Mat m = c.mats[k];
-  const int64_t total = (int64_t)m.rows * m.cols;
+  if ((int)blockIdx.x >= m.norm_blocks) return;
+  if (blockIdx.x == 0 && threadIdx.x < 3 * kMaxSteps) c.done[k * 3 * kMaxSteps + threadIdx.x] = 0;
+  const uint32_t total = (uint32_t)m.rows * (uint32_t)m.cols;  // at most 2^28
   double sum = 0.0;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)kNormBlocks * 256) {
-    const int64_t r = e / m.cols, col = e - r * m.cols;
+  for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += m.norm_blocks * 256) {
+    const uint32_t r = e / (uint32_t)m.cols, col = e - r * (uint32_t)m.cols;
     float u = load_in(c, p, k, r, col);
     if (c.update) {
-      float* mp = p.mom[k] + r * p.ld_mom[k] + col;
+      float* mp = p.mom[k] + (int64_t)r * p.ld_mom[k] + col;
       const float mom = fmaf(c.mu, *mp, u);
       *mp = mom;
       u = c.nesterov ? fmaf(c.mu, mom, u) : mom;
@@ -130,26 +142,23 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
   const Mat m = c.mats[k];
   const int64_t chunks = (int64_t)m.mb * m.nb * 2048;
   if ((int64_t)blockIdx.x * 256 >= chunks) return;
-  __shared__ double sh[kNormBlocks];
-  __shared__ float inv_s;
-  if (threadIdx.x < kNormBlocks) sh[threadIdx.x] = c.norm[k * kNormBlocks + threadIdx.x];
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double s = 0.0;
-    for (int i = 0; i < kNormBlocks; ++i) s += sh[i];
-    inv_s = (float)(1.0 / (sqrt(s) + (double)c.eps));
+  __shared__ double sh[256];
+  sh[threadIdx.x] = (int)threadIdx.x < m.norm_blocks ? c.norm[k * kNormBlocks + threadIdx.x] : 0.0;
+  for (int s = 128; s > 0; s >>= 1) {
+    __syncthreads();
+    if (threadIdx.x < s) sh[threadIdx.x] += sh[threadIdx.x + s];
   }
   __syncthreads();
-  const float inv = inv_s;
+  const float inv = (float)(1.0 / (sqrt(sh[0]) + (double)c.eps));
   uint8_t* x = c.ws + m.x[0];
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < chunks; q += (int64_t)gridDim.x * 256) {
-    const int64_t blk = q >> 11;
+    const int blk = (int)(q >> 11);
     const int r = (int)(q & 127), cb = (int)(q >> 7) & 15;
-    const int64_t i = (blk / m.nb) * kB + r, j0 = (blk % m.nb) * kB + 8 * cb;
+    const int bi = blk / m.nb, i = bi * kB + r, j0 = (blk - bi * m.nb) * kB + 8 * cb;
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int64_t j = j0 + e;
+      const int j = j0 + e;
       v[e] = 0.0f;
       if (i < m.m && j < m.n) {
         const int64_t row = m.tall ? j : i, col = m.tall ? i : j;
@@ -163,7 +172,7 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
     }
     uint4 hi, lo;
     split8(v, hi, lo);
-    uint8_t* at = x + blk * kBlk + chunk_at(r, cb);
+    uint8_t* at = x + (int64_t)blk * kBlk + chunk_at(r, cb);
     *reinterpret_cast<uint4*>(at) = hi;
     *reinterpret_cast<uint4*>(at + m.x_lo) = lo;
   }
@@ -173,55 +182,79 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
 // Block (I, k) of a symmetric matrix as an operand with rows I: stored when I <= k, else
 // block (k, I) with the other major.
 struct Operand {
-  const uint8_t* p;    // hi block
+  int64_t at;          // byte offset of the hi block in the workspace
   int64_t lo;          // offset of its lo block
   bool mn;             // MN-major
 };
-__device__ __forceinline__ Operand sym(const uint8_t* s, int64_t lo, int mb, int I, int k) {
+__device__ __forceinline__ Operand sym(int64_t s, int64_t lo, int mb, int I, int k) {
   const bool up = I <= k;
   return Operand{s + ((int64_t)(up ? I : k) * mb + (up ? k : I)) * kBlk, lo, !up};
 }
 
-template <int kPhase>
-__device__ __forceinline__ void operands(const Common& c, const Mat& m, int cur, int I, int J, int k, Operand& A,
-                                         Operand& B) {
-  const uint8_t* x = c.ws + m.x[cur];
-  if (kPhase == kGram) {
+__device__ __forceinline__ void operands(int phase, const Mat& m, int cur, int I, int J, int k, Operand& A, Operand& B) {
+  const int64_t x = cur ? m.x[1] : m.x[0];
+  if (phase == kGram) {
     A = Operand{x + ((int64_t)I * m.nb + k) * kBlk, m.x_lo, false};
     B = Operand{x + ((int64_t)J * m.nb + k) * kBlk, m.x_lo, false};
-  } else if (kPhase == kPoly) {
-    A = sym(c.ws + m.a, m.s_lo, m.mb, I, k);
-    B = sym(c.ws + m.a, m.s_lo, m.mb, J, k);
+  } else if (phase == kPoly) {
+    A = sym(m.a, m.s_lo, m.mb, I, k);
+    B = sym(m.a, m.s_lo, m.mb, J, k);
   } else {
-    A = sym(c.ws + m.b, m.s_lo, m.mb, I, k);
+    A = sym(m.b, m.s_lo, m.mb, I, k);
     B = Operand{x + ((int64_t)k * m.nb + J) * kBlk, m.x_lo, true};
   }
 }
 
-__device__ __forceinline__ uint64_t block_desc(uint32_t addr, bool mn) {
-  return mn ? tc::smem_desc(addr, 128u, 2048u) : tc::smem_desc(addr, 2048u, 128u);
+__device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
+  uint32_t v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_release(uint32_t* p) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory");
+}
+// Orders this thread's ordinary accesses to global memory with bulk copies, both ways.
+__device__ __forceinline__ void fence_proxy_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+
+// The 64 rows r0.. of a block (all its columns): core matrices [16 column groups][8 row
+// groups], 16 KB.
+__device__ __forceinline__ void rows_g2s(void* dst, const CUtensorMap* map, int64_t block, int r0, uint64_t* mbar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          tc::smem_u32(dst)),
+      "l"(map), "r"(0), "r"(r0 >> 3), "r"((int)(block * 16)), "r"(tc::smem_u32(mbar))
+      : "memory");
 }
 
-// A persistent kernel over the tiles (matrix, I, J) of a phase.  Warp 0 streams blocks into
-// the slots (per k: hi of A, hi of B, lo of B, lo of A; a tile whose operands are the same
-// block loads it once), warp 1 issues the MMAs into one of two accumulators, warps 2-9 run
-// the epilogue of the other.
-template <int kPhase>
+// One persistent cooperative kernel runs every product of the call: the items (step, phase,
+// matrix, I, J) in that order, item g on CTA g mod grid.  An item begins when the tiles that
+// it reads are complete (counters per matrix, phase and step), so matrices advance
+// independently and a CTA without work in one matrix's phase goes on with another's.  An
+// item only waits for earlier ones and all CTAs are resident, so the earliest unfinished item
+// always runs.
+//
+// Warp 0 streams stages of 64 of K, the hi and lo halves of a block of A and of B (A alone
+// where they are the same block); four lanes issue one copy each, since a lane needs about 240
+// clocks per copy and a stage is 768 clocks of products.  A half with K along its columns is
+// contiguous; one with K along its rows is a 3-D tensor copy.  Warp 1 (one lane) issues the
+// products, the small ones first, 128 of K into one of four accumulators.  Warps 2-9 add each
+// accumulator to fp32 registers (the tensor core rounds its running sum towards zero: summed
+// over all of K the bias of a 1024-wide product showed as 2e-5 of the result; 128 at a time it
+// stays near 1e-6) and run the tile's epilogue.
 __global__ void __launch_bounds__(kGemmThreads, 1)
-    product(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const int4* __restrict__ tiles,
-            int n_tiles, int cur) {
+    products(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const __grid_constant__ CUtensorMap map) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t full_bar[kSlots], empty_bar[kSlots];
-  __shared__ __align__(8) uint64_t accf_bar[2], acce_bar[2], drain_bar;
+  __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages];
+  __shared__ __align__(8) uint64_t accf_bar[kAcc], acce_bar[kAcc], drain_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int s = 0; s < kSlots; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       tc::mbar_init(&full_bar[s], 1);
       tc::mbar_init(&empty_bar[s], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kAcc; ++i) {
       tc::mbar_init(&accf_bar[i], 1);
       tc::mbar_init(&acce_bar[i], kEpiThreads);
     }
@@ -229,45 +262,66 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     tc::mbar_init_fence();
     abort_flag = 0;
   }
-  if (warp == 0) tc::tmem_alloc(&tmem_slot, 256);
+  if (warp == 0) tc::tmem_alloc(&tmem_slot, 512);
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = tmem_slot;
-  int issued = 0;  // (producer) slots filled
+  int issued = 0;  // (producer) stages filled
+  const int n_all = c.n_items * c.steps;
 
   auto wait_or_abort = [&](uint64_t* bar, uint32_t parity) {
     bool ok = false;
     for (int tries = 0; tries < 1000 && !ok && !abort_flag; ++tries) ok = tc::mbar_wait(bar, parity, 2000000ull);
     return ok;
   };
-  auto steps = [&](const Mat& m) { return kPhase == kGram ? m.nb : m.mb; };
+  // the tiles an item reads are complete (bounded wait)
+  auto ready = [&](const Mat& m, int k, int phase, int it) {
+    if (phase == kGram && it == 0) return true;
+    const uint32_t tri = (uint32_t)(m.mb * (m.mb + 1) / 2);
+    const int from = phase == kGram ? kApply : phase - 1;
+    const uint32_t want = from == kApply ? (uint32_t)(m.mb * m.nb) : tri;
+    const uint32_t* at = c.done + (k * 3 + from) * kMaxSteps + (phase == kGram ? it - 1 : it);
+    if (ld_acquire(at) >= want) return true;
+    const uint64_t t0 = tc::globaltimer_ns();
+    for (uint32_t i = 0; i < (1u << 30) && !abort_flag; ++i) {
+      if (ld_acquire(at) >= want) return true;
+      if ((i & 63u) == 63u && tc::globaltimer_ns() - t0 > 2000000000ull) return false;
+    }
+    return false;
+  };
+  auto k_blocks = [&](const Mat& m, int phase) { return phase == kGram ? m.nb : m.mb; };
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (lane < 4) {
+      const bool of_a = lane == 1 || lane == 2, lo = lane == 0 || lane == 2;
+      uint8_t* dst0 = smem + lane * kHalf;
       bool ok = true;
-      auto fill = [&](const uint8_t* src) {
-        const int s = issued % kSlots, use = issued / kSlots;
-        if (use > 0 && !(ok = wait_or_abort(&empty_bar[s], (uint32_t)(use - 1) & 1u))) return;
-        tc::mbar_expect_tx(&full_bar[s], kBlk);
-        tc::bulk_g2s(smem + (size_t)s * kBlk, src, kBlk, &full_bar[s]);
-        ++issued;
-      };
-      for (int t = blockIdx.x; ok && t < n_tiles; t += gridDim.x) {
-        const int4 tile = tiles[t];
-        const Mat m = c.mats[tile.x];
-        const int K = steps(m);
+      int s = 0;
+      for (int g = blockIdx.x; ok && g < n_all; g += gridDim.x) {
+        const int it = g / c.n_items;
+        const int4 item = c.items[g - it * c.n_items];
+        const Mat m = c.mats[item.x];
+        if (!(ok = ready(m, item.x, item.y, it))) break;
+        fence_proxy_global();
+        const int K = k_blocks(m, item.y);
         for (int k = 0; ok && k < K; ++k) {
           Operand A, B;
-          operands<kPhase>(c, m, cur, tile.y, tile.z, k, A, B);
-          fill(A.p);
-          if (A.p == B.p) {
-            if (ok) fill(A.p + A.lo);
-            continue;
+          operands(item.y, m, it & 1, item.z, item.w, k, A, B);
+          const bool same = A.at == B.at;
+          const Operand& o = of_a ? A : B;
+          const int64_t off = o.at + (lo ? o.lo : 0);
+          for (int h = 0; h < 2; ++h) {
+            if (issued >= kStages && !(ok = wait_or_abort(&empty_bar[s], (uint32_t)(issued / kStages - 1) & 1u))) break;
+            if (lane == 0) tc::mbar_expect_tx(&full_bar[s], same ? 2 * kHalf : kStage);
+            if (of_a || !same) {
+              uint8_t* dst = dst0 + (size_t)s * kStage;
+              if (o.mn) rows_g2s(dst, &map, off / kBlk, 64 * h, &full_bar[s]);
+              else tc::bulk_g2s(dst, c.ws + off + h * kHalf, kHalf, &full_bar[s]);
+            }
+            ++issued;
+            if (++s == kStages) s = 0;
           }
-          if (ok) fill(B.p);
-          if (ok) fill(B.p + B.lo);
-          if (ok) fill(A.p + A.lo);
         }
       }
       if (!ok) abort_flag = 1;
@@ -276,62 +330,48 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     if (lane == 0) {
       const uint32_t idesc = (1u << 4) | ((uint32_t)(kB >> 3) << 17) | ((uint32_t)(kB >> 4) << 24);  // fp16 -> fp32
       const uint32_t base = tc::smem_u32(smem);
-      int j = 0, taken = 0;
+      int j = 0, s = 0;
+      uint32_t par = 0;
       bool ok = true;
-      auto take = [&](uint32_t& addr) {
-        const int s = taken % kSlots;
-        ok = ok && wait_or_abort(&full_bar[s], (uint32_t)(taken / kSlots) & 1u);
-        tc::fence_after_sync();
-        addr = base + (uint32_t)s * kBlk;
-        ++taken;
-        return s;
-      };
-      for (int t = blockIdx.x; ok && t < n_tiles; t += gridDim.x, ++j) {
-        const int4 tile = tiles[t];
-        const Mat m = c.mats[tile.x];
-        const int K = steps(m), acc = j & 1;
-        if (j >= 2 && !(ok = wait_or_abort(&acce_bar[acc], (uint32_t)((j >> 1) - 1) & 1u))) break;
-        tc::fence_after_sync();
-        const uint32_t D = tmem + (uint32_t)(acc * kB);
-        for (int k = 0; ok && k < K; ++k) {
-          Operand A, B;
-          operands<kPhase>(c, m, cur, tile.y, tile.z, k, A, B);
-          const uint32_t id = idesc | (A.mn ? 1u << 15 : 0u) | (B.mn ? 1u << 16 : 0u);
-          const uint32_t da = A.mn ? 16u : 256u, db = B.mn ? 16u : 256u;  // 16 of K, in 16-byte units
-          auto mma = [&](uint32_t a, uint32_t b, bool first) {
-            const uint64_t ad = block_desc(a, A.mn), bd = block_desc(b, B.mn);
-#pragma unroll
-            for (int kk = 0; kk < kB / 16; ++kk)
-              tc::mma_ss(D, ad + (uint64_t)(da * kk), bd + (uint64_t)(db * kk), id, !(first && kk == 0));
+      for (int g = blockIdx.x; ok && g < n_all; g += gridDim.x) {
+        const int it = g / c.n_items;
+        const int4 item = c.items[g - it * c.n_items];
+        const int K = item.y == kGram ? c.mats[item.x].nb : c.mats[item.x].mb;
+        const bool same = item.y != kApply && item.z == item.w;
+        for (int k = 0; ok && k < K; ++k, ++j) {
+          // the majors of operands(): a symmetric block is stored when row <= column
+          const bool a_mn = item.y != kGram && item.z > k;
+          const bool b_mn = item.y == kApply || (item.y == kPoly && item.w > k);
+          const uint32_t id = idesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+          const uint32_t da = a_mn ? 16u : 256u, db = b_mn ? 16u : 256u;  // 16 of K, in 16-byte units
+          const int acc = j % kAcc;
+          if (j >= kAcc && !(ok = wait_or_abort(&acce_bar[acc], (uint32_t)(j / kAcc - 1) & 1u))) break;
+          const uint32_t D = tmem + (uint32_t)(acc * kB);
+          auto desc = [&](uint32_t addr, bool mn) {
+            return mn ? tc::smem_desc(addr, 128u, 1024u) : tc::smem_desc(addr, 2048u, 128u);
           };
-          uint32_t a_hi, a_lo, b_hi, b_lo;
-          const int s0 = take(a_hi);
-          if (A.p == B.p) {
-            if (!ok) break;
-            mma(a_hi, a_hi, k == 0);
-            const int s1 = take(a_lo);
-            if (!ok) break;
-            mma(a_hi, a_lo, false);
-            mma(a_lo, a_hi, false);
-            tc::commit(&empty_bar[s0]);
-            tc::commit(&empty_bar[s1]);
-            continue;
+          for (int h = 0; h < 2; ++h) {
+            if (!(ok = wait_or_abort(&full_bar[s], par))) break;
+            tc::fence_after_sync();
+            const uint32_t at = base + (uint32_t)s * kStage;
+            const uint64_t a_hi = desc(at + kHalf, a_mn), a_lo = desc(at + 2 * kHalf, a_mn);
+            const uint64_t b_hi = same ? a_hi : desc(at + 3 * kHalf, b_mn), b_lo = same ? a_lo : desc(at, b_mn);
+            auto mma = [&](uint64_t a, uint64_t b, bool first) {
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)
+                tc::mma_ss(D, a + (uint64_t)(da * kk), b + (uint64_t)(db * kk), id, !(first && kk == 0));
+            };
+            mma(a_hi, b_lo, h == 0);
+            mma(a_lo, b_hi, false);
+            mma(a_hi, b_hi, false);
+            tc::commit(&empty_bar[s]);
+            if (++s == kStages) {
+              s = 0;
+              par ^= 1u;
+            }
           }
-          const int s1 = take(b_hi);
-          if (!ok) break;
-          mma(a_hi, b_hi, k == 0);
-          const int s2 = take(b_lo);
-          if (!ok) break;
-          mma(a_hi, b_lo, false);
-          tc::commit(&empty_bar[s0]);
-          tc::commit(&empty_bar[s2]);
-          const int s3 = take(a_lo);
-          if (!ok) break;
-          mma(a_lo, b_hi, false);
-          tc::commit(&empty_bar[s1]);
-          tc::commit(&empty_bar[s3]);
+          if (ok) tc::commit(&accf_bar[acc]);
         }
-        if (ok) tc::commit(&accf_bar[acc]);
       }
       if (!ok) abort_flag = 1;
     }
@@ -341,78 +381,114 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const int c_beg = ((warp - 2) >> 2) * 64;       // this warp's half of the columns
     int j = 0;
     bool ok = true;
-    for (int t = blockIdx.x; t < n_tiles; t += gridDim.x, ++j) {
-      const int4 tile = tiles[t];
-      const Mat m = c.mats[tile.x];
-      const int I = tile.y, J = tile.z, acc = j & 1;
-      bool got = false;
-      if (ok) got = wait_or_abort(&accf_bar[acc], (uint32_t)(j >> 1) & 1u);
-      ok = __all_sync(0xFFFFFFFFu, ok && got);      // warp-uniform: tensor-memory loads are collective
-      if (!ok) break;
-      tc::fence_after_sync();
-      for (int c0 = c_beg; c0 < c_beg + 64; c0 += 32) {
-        uint32_t v[32];
-        tc::ld_x32(tmem + (uint32_t)(acc * kB + c0) + lane_base, v);
-        tc::wait_ld();
-        if (kPhase == kLast) {
-          const int64_t i = (int64_t)I * kB + r, j0 = (int64_t)J * kB + c0;
-          if (i >= m.m) continue;
-          const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
+    for (int g = blockIdx.x; g < n_all; g += gridDim.x) {
+      const int it = g / c.n_items;
+      const int4 item = c.items[g - it * c.n_items];
+      const Mat& m = c.mats[item.x];
+      const int phase = item.y, I = item.z, J = item.w, K = phase == kGram ? m.nb : m.mb;
+      float f[64];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            if (j0 + e >= m.n) break;
-            const float o = __uint_as_float(v[e]) * (1.0f / (kSB * kSX));
-            const int64_t row = m.tall ? j0 + e : i, col = m.tall ? i : j0 + e;
-            const int64_t at = row * p.ld_out[tile.x] + col;
-            if (c.update) {
-              float* w = static_cast<float*>(p.out[tile.x]) + at;
-              *w = fmaf(-lr, o, c.decay * *w);
-            } else if (c.bf16_out) {
-              static_cast<__nv_bfloat16*>(p.out[tile.x])[at] = __float2bfloat16_rn(o);
-            } else {
-              static_cast<float*>(p.out[tile.x])[at] = o;
+      for (int e = 0; e < 64; ++e) f[e] = 0.0f;
+      for (int k = 0; k < K; ++k, ++j) {
+        const int acc = j % kAcc;
+        bool got = false;
+        if (ok) got = wait_or_abort(&accf_bar[acc], (uint32_t)(j / kAcc) & 1u);
+        ok = __all_sync(0xFFFFFFFFu, ok && got);    // warp-uniform: tensor-memory loads are collective
+        if (!ok) break;
+        tc::fence_after_sync();
+#pragma unroll
+        for (int c0 = 0; c0 < 64; c0 += 32) {
+          uint32_t v[32];
+          tc::ld_x32(tmem + (uint32_t)(acc * kB + c_beg + c0) + lane_base, v);
+          tc::wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) f[c0 + e] += __uint_as_float(v[e]);
+        }
+        tc::fence_before_sync();
+        tc::mbar_arrive(&acce_bar[acc]);
+      }
+      const bool last = phase == kApply && it + 1 == c.steps;
+      if (ok && last) {
+        const int i = I * kB + r, j0 = J * kB + c_beg;
+        if (i < m.m) {
+          const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
+          const int64_t ld = p.ld_out[item.x], step = m.tall ? ld : 1;
+          const int64_t at0 = m.tall ? (int64_t)j0 * ld + i : (int64_t)i * ld + j0;
+          void* out = p.out[item.x];
+          // rows of whole, aligned groups of four
+          const bool four = !m.tall && j0 + 64 <= m.n && !c.bf16_out && ((uintptr_t)out & 15) == 0 && (ld & 3) == 0;
+#pragma unroll
+          for (int e = 0; e < 64; e += 4) {
+            float o[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] = f[e + x] * (1.0f / (kSB * kSX));
+            if (four) {
+              float4* w = reinterpret_cast<float4*>(static_cast<float*>(out) + at0 + e);
+              if (c.update) {
+                const float4 old = *w;
+                *w = make_float4(fmaf(-lr, o[0], c.decay * old.x), fmaf(-lr, o[1], c.decay * old.y),
+                                 fmaf(-lr, o[2], c.decay * old.z), fmaf(-lr, o[3], c.decay * old.w));
+              } else {
+                *w = make_float4(o[0], o[1], o[2], o[3]);
+              }
+              continue;
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              if (j0 + e + x >= m.n) continue;
+              const int64_t at = at0 + (e + x) * step;
+              if (c.update) {
+                float* w = static_cast<float*>(out) + at;
+                *w = fmaf(-lr, o[x], c.decay * *w);
+              } else if (c.bf16_out) {
+                static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(o[x]);
+              } else {
+                static_cast<float*>(out)[at] = o[x];
+              }
             }
           }
-          continue;
         }
-        const int64_t blk = (kPhase == kApply ? (int64_t)I * m.nb : (int64_t)I * m.mb) + J;
-        uint8_t* out = c.ws + (kPhase == kGram ? m.a : kPhase == kPoly ? m.b : m.x[cur ^ 1]) + blk * kBlk;
-        const int64_t lo_off = kPhase == kApply ? m.x_lo : m.s_lo;
+      } else if (ok) {
+        const int64_t blk = (phase == kApply ? (int64_t)I * m.nb : (int64_t)I * m.mb) + J;
+        uint8_t* out = c.ws + (phase == kGram ? m.a : phase == kPoly ? m.b : it & 1 ? m.x[0] : m.x[1]) + blk * kBlk;
+        const int64_t lo_off = phase == kApply ? m.x_lo : m.s_lo;
+        const float scale = phase == kGram ? kSA / (kSX * kSX) : phase == kPoly ? kC * kSB / (kSA * kSA) : 1.0f / kSB;
+        const uint8_t* ap = c.ws + m.a + blk * kBlk;
+        // complete since before this tile's operands were loaded; acquired by this thread too
+        if (phase == kPoly) ld_acquire(c.done + (item.x * 3 + kGram) * kMaxSteps + it);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int cb = (c0 >> 3) + g;
-          float f[8];
-          if (kPhase == kPoly) {
-            const uint8_t* ap = c.ws + m.a + blk * kBlk + chunk_at(r, cb);
-            const uint4 ah = *reinterpret_cast<const uint4*>(ap), al = *reinterpret_cast<const uint4*>(ap + m.s_lo);
+        for (int t = 0; t < 8; ++t) {
+          const int cb = (c_beg >> 3) + t;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[8 * t + e] *= scale;
+          if (phase == kPoly) {
+            const uint4 ah = __ldcg(reinterpret_cast<const uint4*>(ap + chunk_at(r, cb)));
+            const uint4 al = __ldcg(reinterpret_cast<const uint4*>(ap + m.s_lo + chunk_at(r, cb)));
             const uint32_t hw[4] = {ah.x, ah.y, ah.z, ah.w}, lw[4] = {al.x, al.y, al.z, al.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float2 h2 = __half22float2(*reinterpret_cast<const __half2*>(&hw[e]));
               const float2 l2 = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
-              f[2 * e] = h2.x + l2.x;
-              f[2 * e + 1] = h2.y + l2.y;
+              f[8 * t + 2 * e] = fmaf(h2.x + l2.x, kBq * kSB / kSA, f[8 * t + 2 * e]);
+              f[8 * t + 2 * e + 1] = fmaf(h2.y + l2.y, kBq * kSB / kSA, f[8 * t + 2 * e + 1]);
             }
-          }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float d = __uint_as_float(v[8 * g + e]);
-            if (kPhase == kGram) f[e] = d * (kSA / (kSX * kSX));
-            if (kPhase == kPoly) {
-              f[e] = fmaf(d, kC * kSB / (kSA * kSA), f[e] * (kBq * kSB / kSA));
-              if (I == J && r == 8 * cb + e) f[e] += kA * kSB;
-            }
-            if (kPhase == kApply) f[e] = d * (1.0f / kSB);
+            for (int e = 0; e < 8; ++e)
+              if (I == J && r == 8 * cb + e) f[8 * t + e] += kA * kSB;
           }
           uint4 hi, lo;
-          split8(f, hi, lo);
+          split8(f + 8 * t, hi, lo);
           uint8_t* at = out + chunk_at(r, cb);
           *reinterpret_cast<uint4*>(at) = hi;
           *reinterpret_cast<uint4*>(at + lo_off) = lo;
         }
+        fence_proxy_global();
+        __threadfence();
       }
-      tc::fence_before_sync();
-      tc::mbar_arrive(&acce_bar[acc]);
+      // all eight warps leave together: none is left at the barrier
+      ok = !tc::bar_or(1, kEpiThreads, !ok);
+      if (!ok) break;
+      if (!last && tid == 64) add_release(c.done + (item.x * 3 + phase) * kMaxSteps + it);
     }
     if (!ok) abort_flag = 1;
   }
@@ -426,14 +502,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     tc::mbar_wait(&drain_bar, 0);
   }
   if (warp == 0 && lane == 0 && abort_flag) {
-    for (int d = issued - 1; d >= 0 && d >= issued - kSlots; --d)
-      tc::mbar_wait(&full_bar[d % kSlots], (uint32_t)(d / kSlots) & 1u);
+    for (int d = issued - 1; d >= 0 && d >= issued - kStages; --d)
+      tc::mbar_wait(&full_bar[d % kStages], (uint32_t)(d / kStages) & 1u);
   }
   tc::fence_before_sync();
   __syncthreads();
   if (warp == 0) {
     tc::fence_after_sync();
-    tc::tmem_dealloc(tmem, 256);
+    tc::tmem_dealloc(tmem, 512);
   }
 }
 
@@ -455,10 +531,12 @@ struct aht_muon {
   cudaStream_t stream = nullptr;
   aht_muon_config cfg{};
   std::vector<Mat> mats;
-  int n_sms = 0, n_sym = 0, n_full = 0;
-  int norm_chunks = 0;           // CTAs per matrix of normalise
+  int n_sms = 0, n_items = 0;
+  int norm_blocks = 0, norm_chunks = 0;  // CTAs per matrix of momentum_norm and normalise
   Mat* d_mats = nullptr;
-  int4 *sym_tiles_gram = nullptr, *sym_tiles = nullptr, *full_tiles = nullptr;
+  int4* items = nullptr;
+  uint32_t* done = nullptr;
+  CUtensorMap map{};
   uint8_t* ws = nullptr;
   double* norm = nullptr;
   uint32_t* status = nullptr;
@@ -473,38 +551,52 @@ namespace {
     if (e_ != cudaSuccess) return set_last_error(AHT_ECUDA, cudaGetErrorString(e_));  \
   } while (0)
 
-template <int kPhase>
-aht_status run_product(aht_muon* s, const Common& c, const Ptrs& p, const int4* tiles, int n, int cur) {
-  product<kPhase><<<std::min(n, s->n_sms), kGemmThreads, kSlots * kBlk, s->stream>>>(c, p, tiles, n, cur);
-  MUON_CUDA(cudaGetLastError());
-  return AHT_OK;
-}
-
 aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   MuonDeviceGuard g(s->device);
   c.mats = s->d_mats;
   c.ws = s->ws;
   c.norm = s->norm;
+  c.done = s->done;
   c.status = s->status;
+  c.items = s->items;
+  c.n_items = s->n_items;
+  c.steps = s->cfg.steps;
   c.eps = s->cfg.eps;
   c.mu = s->cfg.momentum;
   c.nesterov = s->cfg.nesterov;
   const unsigned n = (unsigned)s->mats.size();
-  momentum_norm<<<dim3(kNormBlocks, n), 256, 0, s->stream>>>(c, p);
+  momentum_norm<<<dim3((unsigned)s->norm_blocks, n), 256, 0, s->stream>>>(c, p);
   MUON_CUDA(cudaGetLastError());
   normalise<<<dim3((unsigned)s->norm_chunks, n), 256, 0, s->stream>>>(c, p);
   MUON_CUDA(cudaGetLastError());
-  for (int it = 0; it < s->cfg.steps; ++it) {
-    const int cur = it & 1;
-    if (aht_status e = run_product<kGram>(s, c, p, s->sym_tiles_gram, s->n_sym, cur)) return e;
-    if (aht_status e = run_product<kPoly>(s, c, p, s->sym_tiles, s->n_sym, cur)) return e;
-    if (it + 1 < s->cfg.steps) {
-      if (aht_status e = run_product<kApply>(s, c, p, s->full_tiles, s->n_full, cur)) return e;
-    } else {
-      if (aht_status e = run_product<kLast>(s, c, p, s->full_tiles, s->n_full, cur)) return e;
-    }
-  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)std::min(s->n_items, s->n_sms));
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = kStages * kStage;
+  cfg.stream = s->stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;  // every CTA resident: they wait for one another's tiles
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  MUON_CUDA(cudaLaunchKernelEx(&cfg, products, c, p, s->map));
   return AHT_OK;
+}
+
+// The workspace as a tensor of core matrices: [blocks * 16 column groups][16 row groups][64
+// fp16], copied in boxes of 16 column groups x 8 row groups.
+aht_status make_map(aht_muon* s, int64_t bytes) {
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  MUON_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found));
+  if (found != cudaDriverEntryPointSuccess || !fn)
+    return set_last_error(AHT_ECUDA, "the driver has no cuTensorMapEncodeTiled");
+  const cuuint64_t dims[3] = {64, 16, (cuuint64_t)(bytes / 2048)}, strides[2] = {128, 2048};
+  const cuuint32_t box[3] = {64, 8, 16}, one[3] = {1, 1, 1};
+  const CUresult e = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn)(
+      &s->map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, s->ws, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return e == CUDA_SUCCESS ? AHT_OK : set_last_error(AHT_ECUDA, "cuTensorMapEncodeTiled failed");
 }
 
 aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht_muon_config* cfg, cudaStream_t stream,
@@ -519,7 +611,7 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     at += 2 * blocks * kBlk;      // hi, then lo
     return o;
   };
-  std::vector<int4> sym, full;
+  std::vector<int4> items[3];
   for (int k = 0; k < n; ++k) {
     Mat m{};
     m.rows = rows[k];
@@ -535,26 +627,29 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     m.b = region((int64_t)m.mb * m.mb);
     m.x_lo = (int64_t)m.mb * m.nb * kBlk;
     m.s_lo = (int64_t)m.mb * m.mb * kBlk;
+    m.norm_blocks = (int)std::min<int64_t>(((int64_t)m.rows * m.cols + 2047) / 2048, kNormBlocks);
     most = std::max(most, (int64_t)m.mb * m.nb);
+    s->norm_blocks = std::max(s->norm_blocks, m.norm_blocks);
     s->mats.push_back(m);
     for (int I = 0; I < m.mb; ++I) {
-      for (int J = I; J < m.mb; ++J) sym.push_back(make_int4(k, I, J, 0));
-      for (int J = 0; J < m.nb; ++J) full.push_back(make_int4(k, I, J, 0));
+      for (int J = I; J < m.mb; ++J) {
+        items[kGram].push_back(make_int4(k, kGram, I, J));
+        items[kPoly].push_back(make_int4(k, kPoly, I, J));
+      }
+      for (int J = 0; J < m.nb; ++J) items[kApply].push_back(make_int4(k, kApply, I, J));
     }
   }
-  // the longest tiles first
-  std::vector<int4> gram = sym;
-  auto by = [&](bool n_side) {
-    return [s, n_side](const int4& x, const int4& y) {
+  // the longest tiles of a phase first
+  std::vector<int4> all;
+  for (int ph = 0; ph < 3; ++ph) {
+    std::stable_sort(items[ph].begin(), items[ph].end(), [&](const int4& x, const int4& y) {
       const Mat &a = s->mats[x.x], &b = s->mats[y.x];
-      return (n_side ? a.nb : a.mb) > (n_side ? b.nb : b.mb);
-    };
-  };
-  std::stable_sort(gram.begin(), gram.end(), by(true));
-  std::stable_sort(sym.begin(), sym.end(), by(false));
-  std::stable_sort(full.begin(), full.end(), by(false));
-  s->n_sym = (int)sym.size();
-  s->n_full = (int)full.size();
+      return (ph == kGram ? a.nb : a.mb) > (ph == kGram ? b.nb : b.mb);
+    });
+    all.insert(all.end(), items[ph].begin(), items[ph].end());
+  }
+  if (all.size() > (1u << 31) / (size_t)cfg->steps / 2) return set_last_error(AHT_EINVAL, "too many tiles in one call");
+  s->n_items = (int)all.size();
   s->norm_chunks = (int)std::min<int64_t>(most * 8, 1024);
   auto alloc = [&](void** ptr, size_t bytes) {
     if (cudaMalloc(ptr, bytes) != cudaSuccess) {
@@ -568,18 +663,13 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     return alloc(dst, bytes) && cudaMemcpy(*dst, h, bytes, cudaMemcpyHostToDevice) == cudaSuccess;
   };
   if (!up((void**)&s->d_mats, s->mats.data(), s->mats.size() * sizeof(Mat)) ||
-      !up((void**)&s->sym_tiles_gram, gram.data(), gram.size() * sizeof(int4)) ||
-      !up((void**)&s->sym_tiles, sym.data(), sym.size() * sizeof(int4)) ||
-      !up((void**)&s->full_tiles, full.data(), full.size() * sizeof(int4)) || !alloc((void**)&s->ws, (size_t)at) ||
-      !alloc((void**)&s->norm, (size_t)n * kNormBlocks * sizeof(double)) || !alloc((void**)&s->status, 4) ||
+      !up((void**)&s->items, all.data(), all.size() * sizeof(int4)) || !alloc((void**)&s->ws, (size_t)at) ||
+      !alloc((void**)&s->norm, (size_t)n * kNormBlocks * sizeof(double)) ||
+      !alloc((void**)&s->done, (size_t)n * 3 * kMaxSteps * 4) || !alloc((void**)&s->status, 4) ||
       cudaMemset(s->status, 0, 4) != cudaSuccess)
     return set_last_error(AHT_ENOMEM, "workspace allocation failed");
-  const int smem = kSlots * (int)kBlk;
-  MUON_CUDA(cudaFuncSetAttribute(product<kGram>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  MUON_CUDA(cudaFuncSetAttribute(product<kPoly>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  MUON_CUDA(cudaFuncSetAttribute(product<kApply>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  MUON_CUDA(cudaFuncSetAttribute(product<kLast>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  return AHT_OK;
+  MUON_CUDA(cudaFuncSetAttribute(products, cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * (int)kStage));
+  return make_map(s, at);
 }
 
 }  // namespace
