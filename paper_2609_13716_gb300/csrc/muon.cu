@@ -5,15 +5,16 @@
 // Each matrix is taken with its short side m as rows (a tall one transposed) and padded
 // with zeros to whole 128 x 128 blocks.  Of the three products of a step,
 //   A = X X^T,   B = a I + b A + c A A,   X' = B X,
-// the first two are symmetric: only blocks (I, J) with I <= J are computed and stored, and
-// block (J, I) is the same data read with the other operand major.
+// the first two are symmetric: blocks (I, J) with floor(I / 2) <= floor(J / 2) (row pairs on
+// or above the diagonal) are computed and stored, and block (J, I) is the same data read with
+// the other operand major.
 //
 // Precision: products accurate to fp32 on 16-bit tensor cores.  An operand is stored as
 // hi + lo, two fp16 of it scaled by a power of two (hi the nearest fp16, lo the nearest fp16
 // of the rest: 22 significant bits), and a product is hi hi + hi lo + lo hi, accumulated in
 // fp32.  fp16 suits the iteration because its operands are bounded: with ||X||_F <= 1 every
 // singular value of X stays in [0, 1.21] (the quintic's maximum over [0, 1.21]), so the
-// entries of X, A and B stay below 1.21, 1.47 and 3.45, and with the scales 2^14, 2^14 and
+// entries of X, S and B stay below 1.21, 1.47 and 3.45 in size, and with the scales 2^14, 2^14 and
 // 2^13 nothing leaves fp16's range while lo's subnormal step is 2^-39 of 1.
 //
 // Storage: block [128 rows r][128 columns c] as 256 core matrices of 8 x 8, core (c / 8,
@@ -42,20 +43,22 @@ namespace {
 
 constexpr int kB = 128;                        // block edge
 constexpr uint32_t kBlk = kB * kB * 2;         // bytes of one fp16 block
-constexpr uint32_t kHalf = kBlk / 2;           // 64 of K of one block
-constexpr uint32_t kStage = 4 * kHalf;         // lo of B, hi and lo of A, hi of B
-constexpr int kStages = 3;
+constexpr uint32_t kHalf = kBlk / 2;           // 64 of K of a block
+constexpr uint32_t kStage = 3 * kHalf;         // of A: hi, lo; of B: half of hi, half of lo
+constexpr int kStages = 4;                     // two units of 128 of K
 constexpr int kAcc = 4;                        // accumulators in tensor memory
 constexpr int kGemmThreads = 320;              // producer, MMA, 8 epilogue warps
 constexpr int kEpiThreads = 256;
 constexpr float kA = 3.4445f, kBq = -4.7750f, kC = 2.0315f;  // Jordan et al. 2024
 constexpr float kSX = 16384.0f, kSA = 16384.0f, kSB = 8192.0f;
+constexpr float kShift = kBq / (2.0f * kC), kDiag = kA - kBq * kBq / (4.0f * kC);
 constexpr int kNormBlocks = 256;               // most partial sums of squares per matrix
 constexpr int kMaxSteps = 32;
 
 struct Mat {
   int32_t rows, cols, m, n, mb, nb, tall;
   int32_t norm_blocks;                         // partial sums of squares
+  int32_t sym_tiles;                           // stored blocks of a symmetric matrix
   int64_t x[2], a, b;                          // byte offsets of the hi blocks
   int64_t x_lo, s_lo;                          // from a hi block to its lo block
 };
@@ -76,7 +79,7 @@ struct Common {
   double* norm;                                // [n_mats][kNormBlocks]
   uint32_t* done;                              // [n_mats][3 phases][kMaxSteps] finished tiles
   uint32_t* status;
-  const int4* items;                           // (matrix, phase, I, J) of one step
+  const int4* items;                           // (matrix, phase, row pair, J) of one step
   int32_t n_items, steps;
   int32_t bf16_in, bf16_out, update, nesterov;
   float mu, eps, decay, lr;                    // decay = 1 - lr * weight_decay
@@ -179,30 +182,33 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
 }
 
 // ---- the products -------------------------------------------------------------------------
-// Block (I, k) of a symmetric matrix as an operand with rows I: stored when I <= k, else
-// block (k, I) with the other major.
+// Boxes of the workspace seen as [blocks * 16 column groups][16 row groups][64 fp16]: 64
+// columns of 128 rows, 64 rows of 128 columns, 64 columns of 64 rows.
+struct Maps {
+  CUtensorMap cols, rows, quarter;
+};
+
+// Block (I, k) of a symmetric matrix as an operand with rows I: stored when floor(I / 2) <=
+// floor(k / 2), else block (k, I) with the other major.  The halves make both rows of a pair
+// take the same major, which one product instruction needs.
 struct Operand {
   int64_t at;          // byte offset of the hi block in the workspace
   int64_t lo;          // offset of its lo block
   bool mn;             // MN-major
 };
 __device__ __forceinline__ Operand sym(int64_t s, int64_t lo, int mb, int I, int k) {
-  const bool up = I <= k;
+  const bool up = (I >> 1) <= (k >> 1);
   return Operand{s + ((int64_t)(up ? I : k) * mb + (up ? k : I)) * kBlk, lo, !up};
 }
-
-__device__ __forceinline__ void operands(int phase, const Mat& m, int cur, int I, int J, int k, Operand& A, Operand& B) {
+__device__ __forceinline__ Operand operand_a(int phase, const Mat& m, int cur, int I, int k) {
+  if (phase == kGram) return Operand{(cur ? m.x[1] : m.x[0]) + ((int64_t)I * m.nb + k) * kBlk, m.x_lo, false};
+  return sym(phase == kPoly ? m.a : m.b, m.s_lo, m.mb, I, k);
+}
+__device__ __forceinline__ Operand operand_b(int phase, const Mat& m, int cur, int J, int k) {
   const int64_t x = cur ? m.x[1] : m.x[0];
-  if (phase == kGram) {
-    A = Operand{x + ((int64_t)I * m.nb + k) * kBlk, m.x_lo, false};
-    B = Operand{x + ((int64_t)J * m.nb + k) * kBlk, m.x_lo, false};
-  } else if (phase == kPoly) {
-    A = sym(m.a, m.s_lo, m.mb, I, k);
-    B = sym(m.a, m.s_lo, m.mb, J, k);
-  } else {
-    A = sym(m.b, m.s_lo, m.mb, I, k);
-    B = Operand{x + ((int64_t)k * m.nb + J) * kBlk, m.x_lo, true};
-  }
+  if (phase == kGram) return Operand{x + ((int64_t)J * m.nb + k) * kBlk, m.x_lo, false};
+  if (phase == kPoly) return sym(m.a, m.s_lo, m.mb, J, k);
+  return Operand{x + ((int64_t)k * m.nb + J) * kBlk, m.x_lo, true};
 }
 
 __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
@@ -216,71 +222,113 @@ __device__ __forceinline__ void add_release(uint32_t* p) {
 // Orders this thread's ordinary accesses to global memory with bulk copies, both ways.
 __device__ __forceinline__ void fence_proxy_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 
-// The 64 rows r0.. of a block (all its columns): core matrices [16 column groups][8 row
-// groups], 16 KB.
-__device__ __forceinline__ void rows_g2s(void* dst, const CUtensorMap* map, int64_t block, int r0, uint64_t* mbar) {
+// ---- a pair of CTAs (a cluster of two) ----
+__device__ __forceinline__ uint32_t pair_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// The address of a shared object of this CTA in CTA 0 of the pair.
+__device__ __forceinline__ uint32_t in_leader(const void* p) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(tc::smem_u32(p)));
+  return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t mbar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mbar) : "memory");
+}
+// A box of the workspace into this CTA's shared memory, counted on a barrier of either CTA.
+__device__ __forceinline__ void box_g2s(void* dst, const CUtensorMap* map, int row_group, int col_group, uint32_t mbar) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-          tc::smem_u32(dst)),
-      "l"(map), "r"(0), "r"(r0 >> 3), "r"((int)(block * 16)), "r"(tc::smem_u32(mbar))
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+      "[%5];" ::"r"(tc::smem_u32(dst)),
+      "l"(map), "r"(0), "r"(row_group), "r"(col_group), "r"(mbar)
+      : "memory");
+}
+// D[both CTAs] (+)= A B^T, M = 256 (128 rows of each CTA), N = 128 (64 columns of each CTA).
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
+}
+// The products issued so far arrive on a barrier of both CTAs when they are complete.
+__device__ __forceinline__ void commit_pair(uint64_t* mbar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+          tc::smem_u32(mbar)),
+      "h"((uint16_t)3)
       : "memory");
 }
 
-// One persistent cooperative kernel runs every product of the call: the items (step, phase,
-// matrix, I, J) in that order, item g on CTA g mod grid.  An item begins when the tiles that
-// it reads are complete (counters per matrix, phase and step), so matrices advance
-// independently and a CTA without work in one matrix's phase goes on with another's.  An
-// item only waits for earlier ones and all CTAs are resident, so the earliest unfinished item
-// always runs.
+// One persistent cooperative kernel of CTA pairs runs every product of the call: the items
+// (step, phase, matrix, row pair, J) in that order, item g on pair g mod pairs; an item is the
+// 128 x 128 tiles (I, J) and (I + 1, J), one per CTA.  An item begins when the tiles that it
+// reads are complete (counters per matrix, phase and step), so matrices advance independently
+// and a pair without work in one matrix's phase goes on with another's.  An item only waits
+// for earlier ones and all CTAs are resident, so the earliest unfinished item always runs.
 //
-// Warp 0 streams stages of 64 of K, the hi and lo halves of a block of A and of B (A alone
-// where they are the same block); four lanes issue one copy each, since a lane needs about 240
-// clocks per copy and a stage is 768 clocks of products.  A half with K along its columns is
-// contiguous; one with K along its rows is a 3-D tensor copy.  Warp 1 (one lane) issues the
-// products, the small ones first, 128 of K into one of four accumulators.  Warps 2-9 add each
-// accumulator to fp32 registers (the tensor core rounds its running sum towards zero: summed
-// over all of K the bias of a 1024-wide product showed as 2e-5 of the result; 128 at a time it
-// stays near 1e-6) and run the tile's epilogue.
+// Why pairs: a 128 x 128 product of one CTA reads its operands from shared memory at 128 B
+// per clock, all there is, and the copies that refill it (85 B per clock) took 40 % of the
+// tensor cores' time.  A pair's product reads the A rows of each CTA and half of B from each,
+// 96 B per clock, and refills 64.
+//
+// Warp 0 streams stages of 64 of K; four lanes issue a copy each, since a lane needs about
+// 240 clocks per copy and a stage is 768 clocks of products.  Both CTAs' copies count on
+// CTA 0's barrier.  Warp 1 of CTA 0 (one lane) issues the products, the small ones first, 128
+// of K into one of four accumulators.  Warps 2-9 add each accumulator to fp32 registers (the
+// tensor core rounds its running sum towards zero: summed over all of K the bias of a
+// 1024-wide product showed as 2e-5 of the result; 128 at a time it stays near 1e-6) and run
+// the tile's epilogue.
 __global__ void __launch_bounds__(kGemmThreads, 1)
-    products(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const __grid_constant__ CUtensorMap map) {
+    products(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages];
+  __shared__ __align__(8) uint64_t full_bar[kStages / 2], empty_bar[kStages];
   __shared__ __align__(8) uint64_t accf_bar[kAcc], acce_bar[kAcc], drain_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)pair_rank(), pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      tc::mbar_init(&full_bar[s], 1);
-      tc::mbar_init(&empty_bar[s], 1);
-    }
+    for (int s = 0; s < kStages; ++s) tc::mbar_init(&empty_bar[s], 1);
+    for (int s = 0; s < kStages / 2; ++s) tc::mbar_init(&full_bar[s], 1);
     for (int i = 0; i < kAcc; ++i) {
       tc::mbar_init(&accf_bar[i], 1);
-      tc::mbar_init(&acce_bar[i], kEpiThreads);
+      tc::mbar_init(&acce_bar[i], 2 * kEpiThreads / 32);  // a lane of every epilogue warp of the pair
     }
     tc::mbar_init(&drain_bar, 1);
     tc::mbar_init_fence();
     abort_flag = 0;
   }
-  if (warp == 0) tc::tmem_alloc(&tmem_slot, 512);
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tc::smem_u32(&tmem_slot)));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  }
   tc::fence_before_sync();
   __syncthreads();
+  pair_sync();
   tc::fence_after_sync();
   const uint32_t tmem = tmem_slot;
   int issued = 0;  // (producer) stages filled
   const int n_all = c.n_items * c.steps;
 
   auto wait_or_abort = [&](uint64_t* bar, uint32_t parity) {
+    if (tc::mbar_try_wait(bar, parity)) return true;
     bool ok = false;
     for (int tries = 0; tries < 1000 && !ok && !abort_flag; ++tries) ok = tc::mbar_wait(bar, parity, 2000000ull);
     return ok;
   };
+  auto wait_warp = [&](uint64_t* bar, uint32_t parity) {  // by a whole warp, which goes on or gives up together
+    return (bool)__all_sync(0xFFFFFFFFu, wait_or_abort(bar, parity));
+  };
   // the tiles an item reads are complete (bounded wait)
   auto ready = [&](const Mat& m, int k, int phase, int it) {
     if (phase == kGram && it == 0) return true;
-    const uint32_t tri = (uint32_t)(m.mb * (m.mb + 1) / 2);
     const int from = phase == kGram ? kApply : phase - 1;
-    const uint32_t want = from == kApply ? (uint32_t)(m.mb * m.nb) : tri;
+    const uint32_t want = (uint32_t)(from == kApply ? m.mb * m.nb : m.sym_tiles);
     const uint32_t* at = c.done + (k * 3 + from) * kMaxSteps + (phase == kGram ? it - 1 : it);
     if (ld_acquire(at) >= want) return true;
     const uint64_t t0 = tc::globaltimer_ns();
@@ -290,87 +338,99 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
     return false;
   };
-  auto k_blocks = [&](const Mat& m, int phase) { return phase == kGram ? m.nb : m.mb; };
 
   if (warp == 0) {
     if (lane < 4) {
-      const bool of_a = lane == 1 || lane == 2, lo = lane == 0 || lane == 2;
-      uint8_t* dst0 = smem + lane * kHalf;
+      // lane 0: hi of A, 1: lo of A, 2: this CTA's half of B's hi, 3: of its lo
+      const bool of_a = lane < 2, lo = lane & 1;
+      uint8_t* dst0 = smem + (of_a ? lane * kHalf : 2 * kHalf + (lane - 2) * (kHalf / 2));
+      const uint32_t full0 = in_leader(&full_bar[0]);
       bool ok = true;
       int s = 0;
-      for (int g = blockIdx.x; ok && g < n_all; g += gridDim.x) {
+      for (int g = pair; ok && g < n_all; g += pairs) {
         const int it = g / c.n_items;
         const int4 item = c.items[g - it * c.n_items];
         const Mat m = c.mats[item.x];
         if (!(ok = ready(m, item.x, item.y, it))) break;
         fence_proxy_global();
-        const int K = k_blocks(m, item.y);
+        const int I = min(2 * item.z + rank, m.mb - 1);  // (an odd last row is computed twice, stored once)
+        const int K = item.y == kGram ? m.nb : m.mb;
         for (int k = 0; ok && k < K; ++k) {
-          Operand A, B;
-          operands(item.y, m, it & 1, item.z, item.w, k, A, B);
-          const bool same = A.at == B.at;
-          const Operand& o = of_a ? A : B;
-          const int64_t off = o.at + (lo ? o.lo : 0);
+          const Operand o = of_a ? operand_a(item.y, m, it & 1, I, k) : operand_b(item.y, m, it & 1, item.w, k);
+          const int col0 = (int)((o.at + (lo ? o.lo : 0)) / kBlk) * 16;
           for (int h = 0; h < 2; ++h) {
             if (issued >= kStages && !(ok = wait_or_abort(&empty_bar[s], (uint32_t)(issued / kStages - 1) & 1u))) break;
-            if (lane == 0) tc::mbar_expect_tx(&full_bar[s], same ? 2 * kHalf : kStage);
-            if (of_a || !same) {
-              uint8_t* dst = dst0 + (size_t)s * kStage;
-              if (o.mn) rows_g2s(dst, &map, off / kBlk, 64 * h, &full_bar[s]);
-              else tc::bulk_g2s(dst, c.ws + off + h * kHalf, kHalf, &full_bar[s]);
+            if (lane == 0 && rank == 0 && h == 0) tc::mbar_expect_tx(&full_bar[s >> 1], 4 * kStage);
+            uint8_t* dst = dst0 + (size_t)s * kStage;
+            const uint32_t bar = full0 + (uint32_t)(s >> 1) * 8u;
+            if (of_a) {
+              if (o.mn) box_g2s(dst, &maps.rows, 8 * h, col0, bar);
+              else box_g2s(dst, &maps.cols, 0, col0 + 8 * h, bar);
+            } else {
+              if (o.mn) box_g2s(dst, &maps.quarter, 8 * h, col0 + 8 * rank, bar);
+              else box_g2s(dst, &maps.quarter, 8 * rank, col0 + 8 * h, bar);
             }
             ++issued;
             if (++s == kStages) s = 0;
           }
         }
       }
+      // the last stages' releases have landed before this CTA can leave
+      for (int d = max(0, issued - kStages); ok && d < issued; ++d)
+        ok = wait_or_abort(&empty_bar[d % kStages], (uint32_t)(d / kStages) & 1u);
       if (!ok) abort_flag = 1;
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t idesc = (1u << 4) | ((uint32_t)(kB >> 3) << 17) | ((uint32_t)(kB >> 4) << 24);  // fp16 -> fp32
+    // The tensor cores queue few products, so whatever this warp does between two of them
+    // shows: one wait per 128 of K, the wait for the accumulator in the middle of the one
+    // before, and a warp-uniform loop with one elected lane (136 instead of 242 clocks lost
+    // per 768).
+    if (rank == 0) {
+      const uint32_t idesc = (1u << 4) | ((uint32_t)(kB >> 3) << 17) | ((uint32_t)(2 * kB >> 4) << 24);  // fp16 -> fp32
       const uint32_t base = tc::smem_u32(smem);
-      int j = 0, s = 0;
-      uint32_t par = 0;
+      const bool one = tc::elect_one();
+      int j = 0;
       bool ok = true;
-      for (int g = blockIdx.x; ok && g < n_all; g += gridDim.x) {
+      for (int g = pair; ok && g < n_all; g += pairs) {
         const int it = g / c.n_items;
         const int4 item = c.items[g - it * c.n_items];
-        const int K = item.y == kGram ? c.mats[item.x].nb : c.mats[item.x].mb;
-        const bool same = item.y != kApply && item.z == item.w;
+        const int mb = c.mats[item.x].mb, K = item.y == kGram ? c.mats[item.x].nb : mb;
         for (int k = 0; ok && k < K; ++k, ++j) {
-          // the majors of operands(): a symmetric block is stored when row <= column
-          const bool a_mn = item.y != kGram && item.z > k;
-          const bool b_mn = item.y == kApply || (item.y == kPoly && item.w > k);
+          // the majors of operand_a and operand_b
+          const bool a_mn = item.y != kGram && item.z > (k >> 1);
+          const bool b_mn = item.y == kApply || (item.y == kPoly && (item.w >> 1) > (k >> 1));
           const uint32_t id = idesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
-          const uint32_t da = a_mn ? 16u : 256u, db = b_mn ? 16u : 256u;  // 16 of K, in 16-byte units
-          const int acc = j % kAcc;
-          if (j >= kAcc && !(ok = wait_or_abort(&acce_bar[acc], (uint32_t)(j / kAcc - 1) & 1u))) break;
+          const uint32_t da = a_mn ? 16u : 256u, db = b_mn ? 16u : 128u;  // 16 of K, in 16-byte units
+          const int acc = j % kAcc, s = 2 * (j & 1);
           const uint32_t D = tmem + (uint32_t)(acc * kB);
-          auto desc = [&](uint32_t addr, bool mn) {
-            return mn ? tc::smem_desc(addr, 128u, 1024u) : tc::smem_desc(addr, 2048u, 128u);
-          };
-          for (int h = 0; h < 2; ++h) {
-            if (!(ok = wait_or_abort(&full_bar[s], par))) break;
-            tc::fence_after_sync();
-            const uint32_t at = base + (uint32_t)s * kStage;
-            const uint64_t a_hi = desc(at + kHalf, a_mn), a_lo = desc(at + 2 * kHalf, a_mn);
-            const uint64_t b_hi = same ? a_hi : desc(at + 3 * kHalf, b_mn), b_lo = same ? a_lo : desc(at, b_mn);
-            auto mma = [&](uint64_t a, uint64_t b, bool first) {
+          auto a_desc = [&](uint32_t x) { return a_mn ? tc::smem_desc(x, 128u, 1024u) : tc::smem_desc(x, 2048u, 128u); };
+          auto b_desc = [&](uint32_t x) { return b_mn ? tc::smem_desc(x, 128u, 1024u) : tc::smem_desc(x, 1024u, 128u); };
+          const uint64_t a0 = a_desc(base + (uint32_t)s * kStage), b0 = b_desc(base + (uint32_t)s * kStage + 2 * kHalf);
+          constexpr uint64_t kLoA = kHalf / 16, kLoB = kHalf / 32, kNext = kStage / 16;
+          auto mma = [&](uint64_t a, uint64_t b, bool first) {
 #pragma unroll
-              for (int kk = 0; kk < 4; ++kk)
-                tc::mma_ss(D, a + (uint64_t)(da * kk), b + (uint64_t)(db * kk), id, !(first && kk == 0));
-            };
-            mma(a_hi, b_lo, h == 0);
-            mma(a_lo, b_hi, false);
-            mma(a_hi, b_hi, false);
-            tc::commit(&empty_bar[s]);
-            if (++s == kStages) {
-              s = 0;
-              par ^= 1u;
-            }
+            for (int kk = 0; kk < 4; ++kk)
+              mma_pair(D, a + (uint64_t)(da * kk), b + (uint64_t)(db * kk), id, !(first && kk == 0));
+          };
+          if (!(ok = wait_warp(&full_bar[j & 1], (uint32_t)(j >> 1) & 1u))) break;
+          if (one) {
+            mma(a0, b0 + kLoB, true);
+            mma(a0 + kLoA, b0, false);
+            mma(a0, b0, false);
+            commit_pair(&empty_bar[s]);
+            mma(a0 + kNext, b0 + kNext + kLoB, false);
+            mma(a0 + kNext + kLoA, b0 + kNext, false);
           }
-          if (ok) tc::commit(&accf_bar[acc]);
+          // the accumulator of the next 128 of K
+          const int n = j + 1;
+          if (n >= kAcc && !(ok = wait_warp(&acce_bar[n % kAcc], (uint32_t)(n / kAcc - 1) & 1u))) break;
+          tc::fence_after_sync();
+          if (one) {
+            mma(a0 + kNext, b0 + kNext, false);
+            commit_pair(&empty_bar[s + 1]);
+            commit_pair(&accf_bar[acc]);
+          }
+          __syncwarp();
         }
       }
       if (!ok) abort_flag = 1;
@@ -379,36 +439,45 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const int q = warp & 3, r = 32 * q + lane;      // row of the tile
     const uint32_t lane_base = (uint32_t)(32 * q) << 16;
     const int c_beg = ((warp - 2) >> 2) * 64;       // this warp's half of the columns
+    const uint32_t acce0 = in_leader(&acce_bar[0]);
     int j = 0;
     bool ok = true;
-    for (int g = blockIdx.x; g < n_all; g += gridDim.x) {
+    for (int g = pair; g < n_all; g += pairs) {
       const int it = g / c.n_items;
       const int4 item = c.items[g - it * c.n_items];
       const Mat& m = c.mats[item.x];
-      const int phase = item.y, I = item.z, J = item.w, K = phase == kGram ? m.nb : m.mb;
+      const int phase = item.y, I = 2 * item.z + rank, J = item.w, K = phase == kGram ? m.nb : m.mb;
+      const bool mine = I < m.mb;                   // (of an odd last row: nothing to store)
+      const int64_t blk = (phase == kApply ? (int64_t)I * m.nb : (int64_t)I * m.mb) + J;
+      uint8_t* out = c.ws + (phase == kGram ? m.a : phase == kPoly ? m.b : it & 1 ? m.x[0] : m.x[1]) + blk * kBlk +
+                     chunk_at(r, c_beg >> 3);
+      const int64_t lo_off = phase == kApply ? m.x_lo : m.s_lo;
+      const float scale = phase == kGram ? kSA / (kSX * kSX) : phase == kPoly ? kC * kSB / (kSA * kSA) : 1.0f / kSB;
+      const float diag = phase == kApply || I != J ? 0.0f : phase == kGram ? kShift * kSA : kDiag * kSB;
       float f[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) f[e] = 0.0f;
       for (int k = 0; k < K; ++k, ++j) {
         const int acc = j % kAcc;
-        bool got = false;
-        if (ok) got = wait_or_abort(&accf_bar[acc], (uint32_t)(j / kAcc) & 1u);
-        ok = __all_sync(0xFFFFFFFFu, ok && got);    // warp-uniform: tensor-memory loads are collective
-        if (!ok) break;
+        // warp-uniform: tensor-memory loads are collective
+        if (!(ok = wait_warp(&accf_bar[acc], (uint32_t)(j / kAcc) & 1u))) break;
         tc::fence_after_sync();
+        if (mine) {
 #pragma unroll
-        for (int c0 = 0; c0 < 64; c0 += 32) {
-          uint32_t v[32];
-          tc::ld_x32(tmem + (uint32_t)(acc * kB + c_beg + c0) + lane_base, v);
-          tc::wait_ld();
+          for (int c0 = 0; c0 < 64; c0 += 32) {
+            uint32_t v[32];
+            tc::ld_x32(tmem + (uint32_t)(acc * kB + c_beg + c0) + lane_base, v);
+            tc::wait_ld();
 #pragma unroll
-          for (int e = 0; e < 32; ++e) f[c0 + e] += __uint_as_float(v[e]);
+            for (int e = 0; e < 32; ++e) f[c0 + e] += __uint_as_float(v[e]);
+          }
         }
         tc::fence_before_sync();
-        tc::mbar_arrive(&acce_bar[acc]);
+        __syncwarp();
+        if (lane == 0) arrive_at(acce0 + (uint32_t)acc * 8u);
       }
       const bool last = phase == kApply && it + 1 == c.steps;
-      if (ok && last) {
+      if (ok && mine && last) {
         const int i = I * kB + r, j0 = J * kB + c_beg;
         if (i < m.m) {
           const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
@@ -448,68 +517,53 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             }
           }
         }
-      } else if (ok) {
-        const int64_t blk = (phase == kApply ? (int64_t)I * m.nb : (int64_t)I * m.mb) + J;
-        uint8_t* out = c.ws + (phase == kGram ? m.a : phase == kPoly ? m.b : it & 1 ? m.x[0] : m.x[1]) + blk * kBlk;
-        const int64_t lo_off = phase == kApply ? m.x_lo : m.s_lo;
-        const float scale = phase == kGram ? kSA / (kSX * kSX) : phase == kPoly ? kC * kSB / (kSA * kSA) : 1.0f / kSB;
-        const uint8_t* ap = c.ws + m.a + blk * kBlk;
-        // complete since before this tile's operands were loaded; acquired by this thread too
-        if (phase == kPoly) ld_acquire(c.done + (item.x * 3 + kGram) * kMaxSteps + it);
+      } else if (ok && mine) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-          const int cb = (c_beg >> 3) + t;
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[8 * t + e] *= scale;
-          if (phase == kPoly) {
-            const uint4 ah = __ldcg(reinterpret_cast<const uint4*>(ap + chunk_at(r, cb)));
-            const uint4 al = __ldcg(reinterpret_cast<const uint4*>(ap + m.s_lo + chunk_at(r, cb)));
-            const uint32_t hw[4] = {ah.x, ah.y, ah.z, ah.w}, lw[4] = {al.x, al.y, al.z, al.w};
+          if (diag != 0.0f) {  // (the tile's row r is its column r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 h2 = __half22float2(*reinterpret_cast<const __half2*>(&hw[e]));
-              const float2 l2 = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
-              f[8 * t + 2 * e] = fmaf(h2.x + l2.x, kBq * kSB / kSA, f[8 * t + 2 * e]);
-              f[8 * t + 2 * e + 1] = fmaf(h2.y + l2.y, kBq * kSB / kSA, f[8 * t + 2 * e + 1]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (I == J && r == 8 * cb + e) f[8 * t + e] += kA * kSB;
+            for (int e = 0; e < 8; ++e) f[8 * t + e] += r == c_beg + 8 * t + e ? diag : 0.0f;
           }
           uint4 hi, lo;
           split8(f + 8 * t, hi, lo);
-          uint8_t* at = out + chunk_at(r, cb);
+          uint8_t* at = out + t * 2048;  // the next group of 8 columns
           *reinterpret_cast<uint4*>(at) = hi;
           *reinterpret_cast<uint4*>(at + lo_off) = lo;
         }
-        fence_proxy_global();
-        __threadfence();
       }
       // all eight warps leave together: none is left at the barrier
       ok = !tc::bar_or(1, kEpiThreads, !ok);
       if (!ok) break;
-      if (!last && tid == 64) add_release(c.done + (item.x * 3 + phase) * kMaxSteps + it);
+      if (!last && mine && tid == 64) {  // the barrier ordered the tile's stores before these
+        fence_proxy_global();
+        add_release(c.done + (item.x * 3 + phase) * kMaxSteps + it);
+      }
     }
     if (!ok) abort_flag = 1;
   }
 
-  // the MMAs and copies this CTA issued complete (bounded), then tensor memory is freed
+  // the products and copies of the pair complete (bounded), then tensor memory is freed
   tc::fence_before_sync();
   __syncthreads();
   if (tid == 0 && abort_flag) atomicOr(c.status, kStatusTimeout);
-  if (warp == 1 && lane == 0) {
-    tc::commit(&drain_bar);
+  if (warp == 1 && lane == 0 && rank == 0) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                     tc::smem_u32(&drain_bar))
+                 : "memory");
     tc::mbar_wait(&drain_bar, 0);
   }
-  if (warp == 0 && lane == 0 && abort_flag) {
-    for (int d = issued - 1; d >= 0 && d >= issued - kStages; --d)
-      tc::mbar_wait(&full_bar[d % kStages], (uint32_t)(d / kStages) & 1u);
+  if (warp == 0 && lane == 0 && rank == 0 && abort_flag) {
+    for (int u = (issued + 1) / 2 - 1; u >= 0 && u >= (issued + 1) / 2 - 2; --u)
+      tc::mbar_wait(&full_bar[u & 1], (uint32_t)(u >> 1) & 1u);
   }
   tc::fence_before_sync();
   __syncthreads();
+  pair_sync();
   if (warp == 0) {
     tc::fence_after_sync();
-    tc::tmem_dealloc(tmem, 512);
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
   }
 }
 
@@ -536,7 +590,8 @@ struct aht_muon {
   Mat* d_mats = nullptr;
   int4* items = nullptr;
   uint32_t* done = nullptr;
-  CUtensorMap map{};
+  Maps maps{};
+  int pairs = 0;                 // CTA pairs resident at once
   uint8_t* ws = nullptr;
   double* norm = nullptr;
   uint32_t* status = nullptr;
@@ -550,6 +605,19 @@ namespace {
     cudaError_t e_ = (call);                                                           \
     if (e_ != cudaSuccess) return set_last_error(AHT_ECUDA, cudaGetErrorString(e_));  \
   } while (0)
+
+void products_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int pairs, cudaStream_t stream) {
+  cfg.gridDim = dim3(2u * (unsigned)pairs);
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = kStages * kStage;
+  cfg.stream = stream;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {2, 1, 1};
+  attr[1].id = cudaLaunchAttributeCooperative;  // every CTA resident: they wait for one another's tiles
+  attr[1].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+}
 
 aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   MuonDeviceGuard g(s->device);
@@ -570,33 +638,30 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   normalise<<<dim3((unsigned)s->norm_chunks, n), 256, 0, s->stream>>>(c, p);
   MUON_CUDA(cudaGetLastError());
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)std::min(s->n_items, s->n_sms));
-  cfg.blockDim = dim3(kGemmThreads);
-  cfg.dynamicSmemBytes = kStages * kStage;
-  cfg.stream = s->stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeCooperative;  // every CTA resident: they wait for one another's tiles
-  attr[0].val.cooperative = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  MUON_CUDA(cudaLaunchKernelEx(&cfg, products, c, p, s->map));
+  cudaLaunchAttribute attr[2];
+  products_config(cfg, attr, std::min(s->n_items, s->pairs), s->stream);
+  MUON_CUDA(cudaLaunchKernelEx(&cfg, products, c, p, s->maps));
   return AHT_OK;
 }
 
-// The workspace as a tensor of core matrices: [blocks * 16 column groups][16 row groups][64
-// fp16], copied in boxes of 16 column groups x 8 row groups.
-aht_status make_map(aht_muon* s, int64_t bytes) {
+// The boxes that the products copy (see Maps).
+aht_status make_maps(aht_muon* s, int64_t bytes) {
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult found;
   MUON_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found));
   if (found != cudaDriverEntryPointSuccess || !fn)
     return set_last_error(AHT_ECUDA, "the driver has no cuTensorMapEncodeTiled");
   const cuuint64_t dims[3] = {64, 16, (cuuint64_t)(bytes / 2048)}, strides[2] = {128, 2048};
-  const cuuint32_t box[3] = {64, 8, 16}, one[3] = {1, 1, 1};
-  const CUresult e = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn)(
-      &s->map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, s->ws, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-      CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return e == CUDA_SUCCESS ? AHT_OK : set_last_error(AHT_ECUDA, "cuTensorMapEncodeTiled failed");
+  const cuuint32_t one[3] = {1, 1, 1};
+  struct Box { CUtensorMap* map; cuuint32_t rows, cols; };
+  for (const Box& b : {Box{&s->maps.cols, 16, 8}, Box{&s->maps.rows, 8, 16}, Box{&s->maps.quarter, 8, 8}}) {
+    const cuuint32_t box[3] = {64, b.rows, b.cols};
+    const CUresult e = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn)(
+        b.map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, s->ws, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (e != CUDA_SUCCESS) return set_last_error(AHT_ECUDA, "cuTensorMapEncodeTiled failed");
+  }
+  return AHT_OK;
 }
 
 aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht_muon_config* cfg, cudaStream_t stream,
@@ -629,10 +694,11 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     m.s_lo = (int64_t)m.mb * m.mb * kBlk;
     m.norm_blocks = (int)std::min<int64_t>(((int64_t)m.rows * m.cols + 2047) / 2048, kNormBlocks);
     most = std::max(most, (int64_t)m.mb * m.nb);
+    for (int I = 0; I < m.mb; ++I) m.sym_tiles += m.mb - (I & ~1);
     s->norm_blocks = std::max(s->norm_blocks, m.norm_blocks);
     s->mats.push_back(m);
-    for (int I = 0; I < m.mb; ++I) {
-      for (int J = I; J < m.mb; ++J) {
+    for (int I = 0; 2 * I < m.mb; ++I) {
+      for (int J = 2 * I; J < m.mb; ++J) {
         items[kGram].push_back(make_int4(k, kGram, I, J));
         items[kPoly].push_back(make_int4(k, kPoly, I, J));
       }
@@ -669,7 +735,12 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
       cudaMemset(s->status, 0, 4) != cudaSuccess)
     return set_last_error(AHT_ENOMEM, "workspace allocation failed");
   MUON_CUDA(cudaFuncSetAttribute(products, cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * (int)kStage));
-  return make_map(s, at);
+  cudaLaunchConfig_t cfg2{};
+  cudaLaunchAttribute attr[2];
+  products_config(cfg2, attr, s->n_sms / 2, s->stream);
+  MUON_CUDA(cudaOccupancyMaxActiveClusters(&s->pairs, products, &cfg2));
+  if (s->pairs < 1) return set_last_error(AHT_ECUDA, "no room for a CTA pair of the products");
+  return make_maps(s, at);
 }
 
 }  // namespace
