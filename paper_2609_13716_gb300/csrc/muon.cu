@@ -47,12 +47,18 @@ constexpr uint32_t kHalf = kBlk / 2;           // 64 of K of a block
 constexpr uint32_t kStage = 3 * kHalf;         // of A: hi, lo; of B: half of hi, half of lo
 constexpr int kStages = 4;                     // two units of 128 of K
 constexpr int kAcc = 4;                        // accumulators in tensor memory
-constexpr int kGemmThreads = 320;              // producer, MMA, 8 epilogue warps
+constexpr int kGemmThreads = 352;              // copies, 8 epilogue warps, 2 that issue products
 constexpr int kEpiThreads = 256;
 constexpr float kA = 3.4445f, kBq = -4.7750f, kC = 2.0315f;  // Jordan et al. 2024
 constexpr float kSX = 16384.0f, kSA = 16384.0f, kSB = 8192.0f;
+// The tensor cores round the running sum of a product towards zero.  Over the 12 additions of
+// 64 of K, the small products first, that takes about 2e-7 off a result (a step's two last
+// products together 3e-7 to 5e-7, on full-rank, low-rank and positive matrices of 128 to
+// 2048), always downwards, and five steps multiply a common factor by about 7; every product is
+// scaled back by 2 * 2^-23.
+constexpr float kUp = 1.0f + 2.0f / 8388608.0f;
 constexpr float kShift = kBq / (2.0f * kC), kDiag = kA - kBq * kBq / (4.0f * kC);
-constexpr int kNormBlocks = 256;               // most partial sums of squares per matrix
+constexpr int kNormBlocks = 1024;              // most partial sums of squares per matrix
 constexpr int kMaxSteps = 32;
 
 struct Mat {
@@ -90,26 +96,84 @@ __device__ __forceinline__ float load_in(const Common& c, const Ptrs& p, int k, 
   return c.bf16_in ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.in[k])[at])
                    : static_cast<const float*>(p.in[k])[at];
 }
+// Whether groups of four columns of every row of the inputs are aligned loads.
+__device__ __forceinline__ bool fours(const Common& c, const Ptrs& p, int k, int cols) {
+  uintptr_t low = (uintptr_t)p.in[k] & (c.bf16_in ? 7 : 15);
+  int ld = cols | p.ld_in[k];
+  if (c.update) {
+    low |= (uintptr_t)p.mom[k] & 15;
+    ld |= p.ld_mom[k];
+  }
+  return low == 0 && (ld & 3) == 0;
+}
+__device__ __forceinline__ float4 load_in4(const Common& c, const Ptrs& p, int k, int64_t r, int64_t col) {
+  const int64_t at = r * p.ld_in[k] + col;
+  if (!c.bf16_in) return __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p.in[k]) + at));
+  const uint2 w = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p.in[k]) + at));
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                     __uint_as_float(w.y & 0xFFFF0000u));
+}
+// U of an element from the gradient (or matrix) g and the new momentum
+__device__ __forceinline__ float u_of(const Common& c, float g, float mom) {
+  return !c.update ? g : c.nesterov ? fmaf(c.mu, mom, g) : mom;
+}
 
 // ---- momentum and the sum of squares of U ------------------------------------------------
-// Also clears the tile counters of the call.
+// Also clears the tile counters of the call.  A thread takes four groups of four columns at a
+// time (their loads in flight together) where the rows allow it, else single elements.
 __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Common c, const __grid_constant__ Ptrs p) {
   const int k = blockIdx.y;
-  const Mat m = c.mats[k];
-  if ((int)blockIdx.x >= m.norm_blocks) return;
+  const Mat& m = c.mats[k];
+  const int blocks = m.norm_blocks;
+  if ((int)blockIdx.x >= blocks) return;
   if (blockIdx.x == 0 && threadIdx.x < 3 * kMaxSteps) c.done[k * 3 * kMaxSteps + threadIdx.x] = 0;
-  const uint32_t total = (uint32_t)m.rows * (uint32_t)m.cols;  // at most 2^28
+  const uint32_t rows = m.rows, cols = m.cols;  // rows * cols is at most 2^28
   double sum = 0.0;
-  for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += m.norm_blocks * 256) {
-    const uint32_t r = e / (uint32_t)m.cols, col = e - r * (uint32_t)m.cols;
-    float u = load_in(c, p, k, r, col);
-    if (c.update) {
-      float* mp = p.mom[k] + (int64_t)r * p.ld_mom[k] + col;
-      const float mom = fmaf(c.mu, *mp, u);
-      *mp = mom;
-      u = c.nesterov ? fmaf(c.mu, mom, u) : mom;
+  if (fours(c, p, k, cols)) {
+    const uint32_t c4 = cols / 4, total = rows * c4;
+    for (uint32_t e0 = blockIdx.x * 1024 + threadIdx.x; e0 < total; e0 += blocks * 1024) {
+      float4 g[4], o[4];
+      float* mp[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t e = e0 + 256 * x;
+        g[x] = o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        mp[x] = nullptr;
+        if (e < total) {
+          const uint32_t r = e / c4, col = 4 * (e - r * c4);
+          g[x] = load_in4(c, p, k, r, col);
+          if (c.update) {
+            mp[x] = p.mom[k] + (int64_t)r * p.ld_mom[k] + col;
+            o[x] = *reinterpret_cast<const float4*>(mp[x]);
+          }
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (mp[x]) {
+          o[x] = make_float4(fmaf(c.mu, o[x].x, g[x].x), fmaf(c.mu, o[x].y, g[x].y), fmaf(c.mu, o[x].z, g[x].z),
+                             fmaf(c.mu, o[x].w, g[x].w));
+          *reinterpret_cast<float4*>(mp[x]) = o[x];
+        }
+        const float ux = u_of(c, g[x].x, o[x].x), uy = u_of(c, g[x].y, o[x].y), uz = u_of(c, g[x].z, o[x].z),
+                    uw = u_of(c, g[x].w, o[x].w);
+        sum += (double)(ux * ux + uy * uy) + (double)(uz * uz + uw * uw);
+      }
     }
-    sum += (double)(u * u);
+  } else {
+    const uint32_t total = rows * cols;
+    for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += blocks * 256) {
+      const uint32_t r = e / cols, col = e - r * cols;
+      const float g = load_in(c, p, k, r, col);
+      float mom = 0.0f;
+      if (c.update) {
+        float* mp = p.mom[k] + (int64_t)r * p.ld_mom[k] + col;
+        mom = fmaf(c.mu, *mp, g);
+        *mp = mom;
+      }
+      const float u = u_of(c, g, mom);
+      sum += (double)(u * u);
+    }
   }
   __shared__ double sh[256];
   sh[threadIdx.x] = sum;
@@ -146,7 +210,9 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
   const int64_t chunks = (int64_t)m.mb * m.nb * 2048;
   if ((int64_t)blockIdx.x * 256 >= chunks) return;
   __shared__ double sh[256];
-  sh[threadIdx.x] = (int)threadIdx.x < m.norm_blocks ? c.norm[k * kNormBlocks + threadIdx.x] : 0.0;
+  double part = 0.0;
+  for (int i = threadIdx.x; i < m.norm_blocks; i += 256) part += c.norm[k * kNormBlocks + i];
+  sh[threadIdx.x] = part;
   for (int s = 128; s > 0; s >>= 1) {
     __syncthreads();
     if (threadIdx.x < s) sh[threadIdx.x] += sh[threadIdx.x + s];
@@ -154,23 +220,34 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
   __syncthreads();
   const float inv = (float)(1.0 / (sqrt(sh[0]) + (double)c.eps));
   uint8_t* x = c.ws + m.x[0];
+  const bool four = !m.tall && fours(c, p, k, m.cols);
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < chunks; q += (int64_t)gridDim.x * 256) {
     const int blk = (int)(q >> 11);
     const int r = (int)(q & 127), cb = (int)(q >> 7) & 15;
     const int bi = blk / m.nb, i = bi * kB + r, j0 = (blk - bi * m.nb) * kB + 8 * cb;
     float v[8];
+    if (four && i < m.m && j0 + 8 <= m.n) {
+      const float4 g0 = load_in4(c, p, k, i, j0), g1 = load_in4(c, p, k, i, j0 + 4);
+      float4 o0 = g0, o1 = g1;
+      if (c.update) {
+        const float4* mp = reinterpret_cast<const float4*>(p.mom[k] + (int64_t)i * p.ld_mom[k] + j0);
+        o0 = mp[0];
+        o1 = mp[1];
+      }
+      const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+      const float o[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int j = j0 + e;
-      v[e] = 0.0f;
-      if (i < m.m && j < m.n) {
-        const int64_t row = m.tall ? j : i, col = m.tall ? i : j;
-        float u = load_in(c, p, k, row, col);
-        if (c.update) {
-          const float mom = p.mom[k][row * p.ld_mom[k] + col];
-          u = c.nesterov ? fmaf(c.mu, mom, u) : mom;
+      for (int e = 0; e < 8; ++e) v[e] = (u_of(c, g[e], o[e]) * inv) * kSX;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int j = j0 + e;
+        v[e] = 0.0f;
+        if (i < m.m && j < m.n) {
+          const int64_t row = m.tall ? j : i, col = m.tall ? i : j;
+          const float mom = c.update ? p.mom[k][row * p.ld_mom[k] + col] : 0.0f;
+          v[e] = (u_of(c, load_in(c, p, k, row, col), mom) * inv) * kSX;
         }
-        v[e] = (u * inv) * kSX;
       }
     }
     uint4 hi, lo;
@@ -188,27 +265,24 @@ struct Maps {
   CUtensorMap cols, rows, quarter;
 };
 
-// Block (I, k) of a symmetric matrix as an operand with rows I: stored when floor(I / 2) <=
-// floor(k / 2), else block (k, I) with the other major.  The halves make both rows of a pair
-// take the same major, which one product instruction needs.
+// Where a lane finds its operand's block for k: from k = turn on it is K-major, blocks in a
+// row (first + k); before, it is MN-major, blocks in a column (column + k * stride).  Block
+// (I, k) of a symmetric matrix is stored when floor(I / 2) <= floor(k / 2), else it is block
+// (k, I) with the other major; the halves make both rows of a pair take the same major, which
+// one product instruction needs.
 struct Operand {
-  int64_t at;          // byte offset of the hi block in the workspace
-  int64_t lo;          // offset of its lo block
-  bool mn;             // MN-major
+  int32_t first, column, stride, turn;
+  __device__ __forceinline__ bool mn(int k) const { return k < turn; }
+  __device__ __forceinline__ int block(int k) const { return mn(k) ? column + k * stride : first + k; }
 };
-__device__ __forceinline__ Operand sym(int64_t s, int64_t lo, int mb, int I, int k) {
-  const bool up = (I >> 1) <= (k >> 1);
-  return Operand{s + ((int64_t)(up ? I : k) * mb + (up ? k : I)) * kBlk, lo, !up};
-}
-__device__ __forceinline__ Operand operand_a(int phase, const Mat& m, int cur, int I, int k) {
-  if (phase == kGram) return Operand{(cur ? m.x[1] : m.x[0]) + ((int64_t)I * m.nb + k) * kBlk, m.x_lo, false};
-  return sym(phase == kPoly ? m.a : m.b, m.s_lo, m.mb, I, k);
-}
-__device__ __forceinline__ Operand operand_b(int phase, const Mat& m, int cur, int J, int k) {
-  const int64_t x = cur ? m.x[1] : m.x[0];
-  if (phase == kGram) return Operand{x + ((int64_t)J * m.nb + k) * kBlk, m.x_lo, false};
-  if (phase == kPoly) return sym(m.a, m.s_lo, m.mb, J, k);
-  return Operand{x + ((int64_t)k * m.nb + J) * kBlk, m.x_lo, true};
+__device__ __forceinline__ Operand operand(int phase, const Mat& m, int cur, bool of_a, bool lo, int I, int J) {
+  const int row = of_a ? I : J;
+  if (phase == kGram || (phase == kApply && !of_a)) {
+    const int x = (int)(((cur ? m.x[1] : m.x[0]) + (lo ? m.x_lo : 0)) / kBlk);
+    return Operand{x + row * m.nb, x + J, m.nb, phase == kGram ? 0 : 0x7FFFFFFF};
+  }
+  const int s = (int)(((phase == kPoly ? m.a : m.b) + (lo ? m.s_lo : 0)) / kBlk);
+  return Operand{s + row * m.mb, s + row, m.mb, row & ~1};
 }
 
 __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
@@ -237,8 +311,10 @@ __device__ __forceinline__ uint32_t in_leader(const void* p) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(tc::smem_u32(p)));
   return r;
 }
+// (cta-scope release: what is handed over is tensor memory, ordered by the tcgen05 fence before
+// it; a cluster-scope release waits for the thread's stores, 600 clocks an arrival.)
 __device__ __forceinline__ void arrive_at(uint32_t mbar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mbar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(mbar) : "memory");
 }
 // A box of the workspace into this CTA's shared memory, counted on a barrier of either CTA.
 __device__ __forceinline__ void box_g2s(void* dst, const CUtensorMap* map, int row_group, int col_group, uint32_t mbar) {
@@ -278,11 +354,11 @@ __device__ __forceinline__ void commit_pair(uint64_t* mbar) {
 //
 // Warp 0 streams stages of 64 of K; four lanes issue a copy each, since a lane needs about
 // 240 clocks per copy and a stage is 768 clocks of products.  Both CTAs' copies count on
-// CTA 0's barrier.  Warp 1 of CTA 0 (one lane) issues the products, the small ones first, 128
-// of K into one of four accumulators.  Warps 2-9 add each accumulator to fp32 registers (the
-// tensor core rounds its running sum towards zero: summed over all of K the bias of a
-// 1024-wide product showed as 2e-5 of the result; 128 at a time it stays near 1e-6) and run
-// the tile's epilogue.
+// CTA 0's barrier.  Warps 1 and 10 of CTA 0 issue the products of units of 128 of K in turn,
+// the small ones first, 64 of K into one of four accumulators.  Warps 2-9 add each accumulator
+// to fp32 registers (the tensor core rounds its running sum towards zero: summed over all of K
+// the bias of a 1024-wide product showed as 2e-5 of the result, 128 at a time as 6e-6, 64 at a
+// time as 3e-6, fp32 products have 2.6e-6) and run the tile's epilogue.
 __global__ void __launch_bounds__(kGemmThreads, 1)
     products(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -299,7 +375,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       tc::mbar_init(&accf_bar[i], 1);
       tc::mbar_init(&acce_bar[i], 2 * kEpiThreads / 32);  // a lane of every epilogue warp of the pair
     }
-    tc::mbar_init(&drain_bar, 1);
+    tc::mbar_init(&drain_bar, 2);
     tc::mbar_init_fence();
     abort_flag = 0;
   }
@@ -345,8 +421,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       const bool of_a = lane < 2, lo = lane & 1;
       uint8_t* dst0 = smem + (of_a ? lane * kHalf : 2 * kHalf + (lane - 2) * (kHalf / 2));
       const uint32_t full0 = in_leader(&full_bar[0]);
+      const int half0 = of_a ? 0 : 8 * rank;      // this CTA's half of B's rows
       bool ok = true;
       int s = 0;
+      uint32_t par = 1;                           // of the release awaited (the first pass waits for none)
       for (int g = pair; ok && g < n_all; g += pairs) {
         const int it = g / c.n_items;
         const int4 item = c.items[g - it * c.n_items];
@@ -355,24 +433,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         fence_proxy_global();
         const int I = min(2 * item.z + rank, m.mb - 1);  // (an odd last row is computed twice, stored once)
         const int K = item.y == kGram ? m.nb : m.mb;
+        const Operand o = operand(item.y, m, it & 1, of_a, lo, I, item.w);
         for (int k = 0; ok && k < K; ++k) {
-          const Operand o = of_a ? operand_a(item.y, m, it & 1, I, k) : operand_b(item.y, m, it & 1, item.w, k);
-          const int col0 = (int)((o.at + (lo ? o.lo : 0)) / kBlk) * 16;
+          const bool mn = o.mn(k);
+          const int col0 = o.block(k) * 16 + (mn ? half0 : 0);
+          const CUtensorMap* map = !of_a ? &maps.quarter : mn ? &maps.rows : &maps.cols;
+#pragma unroll
           for (int h = 0; h < 2; ++h) {
-            if (issued >= kStages && !(ok = wait_or_abort(&empty_bar[s], (uint32_t)(issued / kStages - 1) & 1u))) break;
+            if (issued >= kStages && !(ok = wait_or_abort(&empty_bar[s + h], par))) break;
             if (lane == 0 && rank == 0 && h == 0) tc::mbar_expect_tx(&full_bar[s >> 1], 4 * kStage);
-            uint8_t* dst = dst0 + (size_t)s * kStage;
-            const uint32_t bar = full0 + (uint32_t)(s >> 1) * 8u;
-            if (of_a) {
-              if (o.mn) box_g2s(dst, &maps.rows, 8 * h, col0, bar);
-              else box_g2s(dst, &maps.cols, 0, col0 + 8 * h, bar);
-            } else {
-              if (o.mn) box_g2s(dst, &maps.quarter, 8 * h, col0 + 8 * rank, bar);
-              else box_g2s(dst, &maps.quarter, 8 * rank, col0 + 8 * h, bar);
-            }
+            box_g2s(dst0 + (s + h) * kStage, map, mn ? 8 * h : half0, mn ? col0 : col0 + 8 * h, full0 + (s >> 1) * 8);
             ++issued;
-            if (++s == kStages) s = 0;
           }
+          if ((s ^= 2) == 0) par ^= 1u;
         }
       }
       // the last stages' releases have landed before this CTA can leave
@@ -380,11 +453,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         ok = wait_or_abort(&empty_bar[d % kStages], (uint32_t)(d / kStages) & 1u);
       if (!ok) abort_flag = 1;
     }
-  } else if (warp == 1) {
-    // The tensor cores queue few products, so whatever this warp does between two of them
-    // shows: one wait per 128 of K, the wait for the accumulator in the middle of the one
-    // before, and a warp-uniform loop with one elected lane (136 instead of 242 clocks lost
-    // per 768).
+  } else if (warp == 1 || warp == 10) {
+    // The tensor cores queue few products, so whatever a warp does between two of them shows
+    // (a satisfied wait costs 185 clocks, a unit of 128 of K is 1536 clocks of products): two
+    // warps take the units in turn, one waiting while the other's products run, in
+    // warp-uniform loops with one elected lane.
     if (rank == 0) {
       const uint32_t idesc = (1u << 4) | ((uint32_t)(kB >> 3) << 17) | ((uint32_t)(2 * kB >> 4) << 24);  // fp16 -> fp32
       const uint32_t base = tc::smem_u32(smem);
@@ -396,41 +469,39 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         const int4 item = c.items[g - it * c.n_items];
         const int mb = c.mats[item.x].mb, K = item.y == kGram ? c.mats[item.x].nb : mb;
         for (int k = 0; ok && k < K; ++k, ++j) {
-          // the majors of operand_a and operand_b
-          const bool a_mn = item.y != kGram && item.z > (k >> 1);
-          const bool b_mn = item.y == kApply || (item.y == kPoly && (item.w >> 1) > (k >> 1));
+          if ((j & 1) != (warp == 10)) continue;
+          // the majors of operand()
+          const bool a_mn = item.y != kGram && k < 2 * item.z;
+          const bool b_mn = item.y == kApply || (item.y == kPoly && k < (item.w & ~1));
           const uint32_t id = idesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
           const uint32_t da = a_mn ? 16u : 256u, db = b_mn ? 16u : 128u;  // 16 of K, in 16-byte units
-          const int acc = j % kAcc, s = 2 * (j & 1);
-          const uint32_t D = tmem + (uint32_t)(acc * kB);
+          const int s = 2 * (j & 1);                // stages and accumulators s and s + 1
+          const uint32_t par = (uint32_t)(j >> 1) & 1u;
           auto a_desc = [&](uint32_t x) { return a_mn ? tc::smem_desc(x, 128u, 1024u) : tc::smem_desc(x, 2048u, 128u); };
           auto b_desc = [&](uint32_t x) { return b_mn ? tc::smem_desc(x, 128u, 1024u) : tc::smem_desc(x, 1024u, 128u); };
           const uint64_t a0 = a_desc(base + (uint32_t)s * kStage), b0 = b_desc(base + (uint32_t)s * kStage + 2 * kHalf);
           constexpr uint64_t kLoA = kHalf / 16, kLoB = kHalf / 32, kNext = kStage / 16;
-          auto mma = [&](uint64_t a, uint64_t b, bool first) {
+          if (!(ok = wait_warp(&full_bar[j & 1], par))) break;
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              mma_pair(D, a + (uint64_t)(da * kk), b + (uint64_t)(db * kk), id, !(first && kk == 0));
-          };
-          if (!(ok = wait_warp(&full_bar[j & 1], (uint32_t)(j >> 1) & 1u))) break;
-          if (one) {
-            mma(a0, b0 + kLoB, true);
-            mma(a0 + kLoA, b0, false);
-            mma(a0, b0, false);
-            commit_pair(&empty_bar[s]);
-            mma(a0 + kNext, b0 + kNext + kLoB, false);
-            mma(a0 + kNext + kLoA, b0 + kNext, false);
+          for (int h = 0; ok && h < 2; ++h) {
+            if (j >= 2 && !(ok = wait_warp(&acce_bar[s + h], par ^ 1u))) break;
+            tc::fence_after_sync();
+            if (one) {
+              const uint32_t D = tmem + (uint32_t)((s + h) * kB);
+              const uint64_t a = a0 + h * kNext, b = b0 + h * kNext;
+              auto mma = [&](uint64_t x, uint64_t y, bool first) {
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                  mma_pair(D, x + (uint64_t)(da * kk), y + (uint64_t)(db * kk), id, !(first && kk == 0));
+              };
+              mma(a, b + kLoB, true);
+              mma(a + kLoA, b, false);
+              mma(a, b, false);
+              commit_pair(&empty_bar[s + h]);
+              commit_pair(&accf_bar[s + h]);
+            }
+            __syncwarp();
           }
-          // the accumulator of the next 128 of K
-          const int n = j + 1;
-          if (n >= kAcc && !(ok = wait_warp(&acce_bar[n % kAcc], (uint32_t)(n / kAcc - 1) & 1u))) break;
-          tc::fence_after_sync();
-          if (one) {
-            mma(a0 + kNext, b0 + kNext, false);
-            commit_pair(&empty_bar[s + 1]);
-            commit_pair(&accf_bar[acc]);
-          }
-          __syncwarp();
         }
       }
       if (!ok) abort_flag = 1;
@@ -452,12 +523,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       uint8_t* out = c.ws + (phase == kGram ? m.a : phase == kPoly ? m.b : it & 1 ? m.x[0] : m.x[1]) + blk * kBlk +
                      chunk_at(r, c_beg >> 3);
       const int64_t lo_off = phase == kApply ? m.x_lo : m.s_lo;
-      const float scale = phase == kGram ? kSA / (kSX * kSX) : phase == kPoly ? kC * kSB / (kSA * kSA) : 1.0f / kSB;
+      const float scale = kUp * (phase == kGram ? kSA / (kSX * kSX) : phase == kPoly ? kC * kSB / (kSA * kSA) : 1.0f / kSB);
       const float diag = phase == kApply || I != J ? 0.0f : phase == kGram ? kShift * kSA : kDiag * kSB;
       float f[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) f[e] = 0.0f;
-      for (int k = 0; k < K; ++k, ++j) {
+      for (int k = 0; ok && k < 2 * K; ++k, ++j) {
         const int acc = j % kAcc;
         // warp-uniform: tensor-memory loads are collective
         if (!(ok = wait_warp(&accf_bar[acc], (uint32_t)(j / kAcc) & 1u))) break;
@@ -490,7 +561,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           for (int e = 0; e < 64; e += 4) {
             float o[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) o[x] = f[e + x] * (1.0f / (kSB * kSX));
+            for (int x = 0; x < 4; ++x) o[x] = f[e + x] * (kUp / (kSB * kSX));
             if (four) {
               float4* w = reinterpret_cast<float4*>(static_cast<float*>(out) + at0 + e);
               if (c.update) {
@@ -548,10 +619,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   tc::fence_before_sync();
   __syncthreads();
   if (tid == 0 && abort_flag) atomicOr(c.status, kStatusTimeout);
-  if (warp == 1 && lane == 0 && rank == 0) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                     tc::smem_u32(&drain_bar))
-                 : "memory");
+  if ((warp == 1 || warp == 10) && rank == 0) {
+    if (tc::elect_one())  // the lane that issued this warp's products
+      asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                       tc::smem_u32(&drain_bar))
+                   : "memory");
+    __syncwarp();
     tc::mbar_wait(&drain_bar, 0);
   }
   if (warp == 0 && lane == 0 && rank == 0 && abort_flag) {
@@ -692,7 +765,7 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     m.b = region((int64_t)m.mb * m.mb);
     m.x_lo = (int64_t)m.mb * m.nb * kBlk;
     m.s_lo = (int64_t)m.mb * m.mb * kBlk;
-    m.norm_blocks = (int)std::min<int64_t>(((int64_t)m.rows * m.cols + 2047) / 2048, kNormBlocks);
+    m.norm_blocks = (int)std::min<int64_t>(((int64_t)m.rows * m.cols + 4095) / 4096, kNormBlocks);
     most = std::max(most, (int64_t)m.mb * m.nb);
     for (int I = 0; I < m.mb; ++I) m.sym_tiles += m.mb - (I & ~1);
     s->norm_blocks = std::max(s->norm_blocks, m.norm_blocks);
