@@ -302,7 +302,7 @@ __device__ __forceinline__ uint32_t pair_rank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ void pair_sync() {
+__device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
 // The address of a shared object of this CTA in CTA 0 of the pair.
@@ -338,6 +338,64 @@ __device__ __forceinline__ void commit_pair(uint64_t* mbar) {
           tc::smem_u32(mbar)),
       "h"((uint16_t)3)
       : "memory");
+}
+
+// 64 columns j0.. of row i of the orthogonal factor (the accumulated product f, unscaled) into
+// the caller's matrix: the weight update, or the factor itself.
+__device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int k, const Mat& m, int i, int j0,
+                                             const float (&f)[64]) {
+  if (i >= m.m) return;
+  const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
+  const int64_t ld = p.ld_out[k], step = m.tall ? ld : 1;
+  const int64_t at0 = m.tall ? (int64_t)j0 * ld + i : (int64_t)i * ld + j0;
+  void* out = p.out[k];
+  // rows of whole, aligned groups of four
+  const bool four = !m.tall && j0 + 64 <= m.n && !c.bf16_out && ((uintptr_t)out & 15) == 0 && (ld & 3) == 0;
+  // sixteen columns at a time: their loads are in flight together
+#pragma unroll
+  for (int b = 0; b < 64; b += 16) {
+    float o[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = f[b + e] * (kUp / (kSB * kSX));
+    if (four) {
+      float4* w = reinterpret_cast<float4*>(static_cast<float*>(out) + at0 + b);
+      float4 old[4];
+      if (c.update) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) old[q] = w[q];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          o[4 * q] = fmaf(-lr, o[4 * q], c.decay * old[q].x);
+          o[4 * q + 1] = fmaf(-lr, o[4 * q + 1], c.decay * old[q].y);
+          o[4 * q + 2] = fmaf(-lr, o[4 * q + 2], c.decay * old[q].z);
+          o[4 * q + 3] = fmaf(-lr, o[4 * q + 3], c.decay * old[q].w);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+      continue;
+    }
+    const int left = m.n - j0 - b;             // columns that exist
+    if (c.update) {
+      float* w = static_cast<float*>(out) + at0 + b * step;
+      float old[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) old[e] = e < left ? w[e * step] : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e < left) w[e * step] = fmaf(-lr, o[e], c.decay * old[e]);
+    } else if (c.bf16_out) {
+      __nv_bfloat16* w = static_cast<__nv_bfloat16*>(out) + at0 + b * step;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e < left) w[e * step] = __float2bfloat16_rn(o[e]);
+    } else {
+      float* w = static_cast<float*>(out) + at0 + b * step;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e < left) w[e * step] = o[e];
+    }
+  }
 }
 
 // One persistent cooperative kernel of CTA pairs runs every product of the call: the items
@@ -385,7 +443,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   }
   tc::fence_before_sync();
   __syncthreads();
-  pair_sync();
+  cluster_sync();
   tc::fence_after_sync();
   const uint32_t tmem = tmem_slot;
   int issued = 0;  // (producer) stages filled
@@ -549,45 +607,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       const bool last = phase == kApply && it + 1 == c.steps;
       if (ok && mine && last) {
-        const int i = I * kB + r, j0 = J * kB + c_beg;
-        if (i < m.m) {
-          const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
-          const int64_t ld = p.ld_out[item.x], step = m.tall ? ld : 1;
-          const int64_t at0 = m.tall ? (int64_t)j0 * ld + i : (int64_t)i * ld + j0;
-          void* out = p.out[item.x];
-          // rows of whole, aligned groups of four
-          const bool four = !m.tall && j0 + 64 <= m.n && !c.bf16_out && ((uintptr_t)out & 15) == 0 && (ld & 3) == 0;
-#pragma unroll
-          for (int e = 0; e < 64; e += 4) {
-            float o[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) o[x] = f[e + x] * (kUp / (kSB * kSX));
-            if (four) {
-              float4* w = reinterpret_cast<float4*>(static_cast<float*>(out) + at0 + e);
-              if (c.update) {
-                const float4 old = *w;
-                *w = make_float4(fmaf(-lr, o[0], c.decay * old.x), fmaf(-lr, o[1], c.decay * old.y),
-                                 fmaf(-lr, o[2], c.decay * old.z), fmaf(-lr, o[3], c.decay * old.w));
-              } else {
-                *w = make_float4(o[0], o[1], o[2], o[3]);
-              }
-              continue;
-            }
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              if (j0 + e + x >= m.n) continue;
-              const int64_t at = at0 + (e + x) * step;
-              if (c.update) {
-                float* w = static_cast<float*>(out) + at;
-                *w = fmaf(-lr, o[x], c.decay * *w);
-              } else if (c.bf16_out) {
-                static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(o[x]);
-              } else {
-                static_cast<float*>(out)[at] = o[x];
-              }
-            }
-          }
-        }
+        store_result(c, p, item.x, m, I * kB + r, J * kB + c_beg, f);
       } else if (ok && mine) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
@@ -633,10 +653,226 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   }
   tc::fence_before_sync();
   __syncthreads();
-  pair_sync();
+  cluster_sync();
   if (warp == 0) {
     tc::fence_after_sync();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  }
+}
+
+// ---- matrices of at most 128 rows (short side), whole on chip -----------------------------
+// Between the phases of such a matrix products() spends 5 us on counters, fences and copies
+// through L2 for 0.8 us of products.  Here a cluster of up to 8 CTAs takes a matrix from the
+// gradient to the updated weights in one launch: a CTA holds 128 columns of X and all of S (or
+// B) in shared memory; the partial Gram matrices of the CTAs are summed in distributed shared
+// memory, each CTA its share of the rows, in the order of the CTAs.  The other two products need
+// no exchange.
+constexpr int kSmallCluster = 8;
+constexpr int kSmallThreads = 256;
+constexpr uint32_t kSmallSmem = 6 * kBlk;      // X hi, lo; S hi, lo (or the partial sums); the sum
+
+__device__ __forceinline__ uint32_t peer_addr(const void* p, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(tc::smem_u32(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float4 peer_load(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void peer_store(uint32_t a, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ double peer_load_f64(uint32_t a) {
+  double v;
+  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(a) : "memory");
+  return v;
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 1)
+    small_updates(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, int cluster) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ __align__(8) uint64_t done_bar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ double norm_s[kSmallThreads], norm_all;
+  uint8_t *xs = smem, *ss = smem + 2 * kBlk, *sum = smem + 4 * kBlk;  // partial sums share ss
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int k = (int)blockIdx.x / cluster, rank = (int)blockIdx.x % cluster;
+  const Mat& m = c.mats[k];
+  const int nb = m.nb, rows = m.m, cols = m.n, tall = m.tall;
+  const bool on = rank < nb;                   // (the cluster is as wide as the widest matrix needs)
+  const int r = 32 * (warp & 3) + lane, c_beg = 64 * (warp >> 2);  // this thread's row and 64 columns
+  const int j0 = rank * kB + c_beg;
+  if (tid == 0) {
+    tc::mbar_init(&done_bar, 1);
+    tc::mbar_init_fence();
+  }
+  if (warp == 0) tc::tmem_alloc(&tmem_slot, 256);
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = tmem_slot, lane_base = (uint32_t)(32 * (warp & 3)) << 16;
+  const bool one = warp == 0 && tc::elect_one();
+  uint32_t parity = 0;
+  bool ok = true;
+
+  float f[64];
+  auto split_to = [&](uint8_t* hi_block) {     // f -> the hi and lo blocks
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      uint4 hi, lo;
+      split8(f + 8 * t, hi, lo);
+      uint8_t* at = hi_block + chunk_at(r, (c_beg >> 3) + t);
+      *reinterpret_cast<uint4*>(at) = hi;
+      *reinterpret_cast<uint4*>(at + kBlk) = lo;
+    }
+    tc::fence_proxy_async();                   // the products read through the async proxy
+  };
+  // f = a 128 x 128 x 128 product of hi + lo blocks, 64 of K in each of two accumulators (see
+  // products()); b_mn: B's block has K along its rows
+  auto product = [&](const uint8_t* a, const uint8_t* b, bool b_mn) {
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    if (ok && one) {
+      const uint32_t id = (1u << 4) | ((uint32_t)(kB >> 3) << 17) | ((uint32_t)(kB >> 4) << 24) | (b_mn ? 1u << 16 : 0u);
+      const uint64_t ad = tc::smem_desc(tc::smem_u32(a), 2048u, 128u);
+      const uint64_t bd = b_mn ? tc::smem_desc(tc::smem_u32(b), 128u, 2048u) : tc::smem_desc(tc::smem_u32(b), 2048u, 128u);
+      const uint32_t db = b_mn ? 16u : 256u;
+      constexpr uint64_t kLo = kBlk / 16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int part = 0; part < 3; ++part)   // hi lo, lo hi, hi hi
+#pragma unroll
+          for (int kk = 4 * h; kk < 4 * h + 4; ++kk)
+            tc::mma_ss(tmem + (uint32_t)(h * kB), ad + 256u * kk + (part == 1 ? kLo : 0),
+                       bd + (uint64_t)(db * kk) + (part == 0 ? kLo : 0), id, part > 0 || kk > 4 * h);
+      tc::commit(&done_bar);
+    }
+    bool got = true;
+    if (ok) {
+      got = false;
+      for (int tries = 0; tries < 1000 && !got; ++tries) got = tc::mbar_wait(&done_bar, parity, 2000000ull);
+    }
+    parity ^= 1u;
+    ok = !__syncthreads_or(!got) && ok;        // all threads of the CTA go on alike
+    tc::fence_after_sync();
+#pragma unroll
+    for (int e = 0; e < 64; ++e) f[e] = 0.0f;
+    if (!ok) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c0 = 0; c0 < 64; c0 += 32) {
+        uint32_t v[32];
+        tc::ld_x32(tmem + (uint32_t)(h * kB + c_beg + c0) + lane_base, v);
+        tc::wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) f[c0 + e] += __uint_as_float(v[e]);
+      }
+  };
+  auto scale = [&](float s, float diag) {      // the diagonal: column c_beg + e of S is row r
+#pragma unroll
+    for (int e = 0; e < 64; ++e) f[e] = fmaf(f[e], s, r == c_beg + e ? diag : 0.0f);
+  };
+
+  // momentum, U and its norm; X = U / (||U||_F + eps)
+  double sq = 0.0;
+#pragma unroll
+  for (int b = 0; b < 64; b += 16) {           // sixteen columns' loads in flight together
+    const int left = on && r < rows ? min(16, max(0, cols - j0 - b)) : 0;
+    const int64_t step_m = tall ? p.ld_mom[k] : 1;
+    float* mp = c.update ? p.mom[k] + (tall ? (int64_t)(j0 + b) * p.ld_mom[k] + r : (int64_t)r * p.ld_mom[k] + j0 + b) : nullptr;
+    float mom[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      f[b + e] = e < left ? load_in(c, p, k, tall ? j0 + b + e : r, tall ? r : j0 + b + e) : 0.0f;
+      mom[e] = mp && e < left ? mp[e * step_m] : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      mom[e] = fmaf(c.mu, mom[e], f[b + e]);
+      if (mp && e < left) mp[e * step_m] = mom[e];
+      f[b + e] = u_of(c, f[b + e], mom[e]);
+      sq += (double)(f[b + e] * f[b + e]);
+    }
+  }
+  norm_s[tid] = sq;
+  for (int s = kSmallThreads / 2; s > 0; s >>= 1) {
+    __syncthreads();
+    if (tid < s) norm_s[tid] += norm_s[tid + s];
+  }
+  __syncthreads();
+  cluster_sync();
+  if (tid == 0) {
+    double t = 0.0;
+    for (int q = 0; q < nb; ++q) t += peer_load_f64(peer_addr(&norm_s[0], q));
+    norm_all = t;
+  }
+  __syncthreads();
+  const float inv = (float)(1.0 / (sqrt(norm_all) + (double)c.eps));
+#pragma unroll
+  for (int e = 0; e < 64; ++e) f[e] = (f[e] * inv) * kSX;
+  if (on) split_to(xs);
+
+  // rows of the Gram matrix this CTA sums for all
+  const int r_beg = on ? kB * rank / nb : 0, r_cnt = on ? kB * (rank + 1) / nb - r_beg : 0;
+  auto at4 = [&](uint8_t* base, int row, int c4) { return base + (c4 * kB + row) * 16; };  // 4 columns of a row
+  for (int it = 0; it < c.steps; ++it) {
+    if (on) product(xs, xs, false);
+    if (nb > 1) {
+      if (on) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          *reinterpret_cast<float4*>(at4(ss, r, (c_beg >> 2) + q)) =
+              make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]);
+      }
+      cluster_sync();
+      for (int e = tid; e < 32 * r_cnt; e += kSmallThreads) {
+        const int c4 = e / r_cnt, row = r_beg + e - c4 * r_cnt;
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int q = 0; q < nb; ++q) {
+          const float4 v = peer_load(peer_addr(at4(ss, row, c4), q));
+          t = make_float4(t.x + v.x, t.y + v.y, t.z + v.z, t.w + v.w);
+        }
+        for (int q = 0; q < nb; ++q) peer_store(peer_addr(at4(sum, row, c4), q), t);
+      }
+      cluster_sync();
+      if (on) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const float4 v = *reinterpret_cast<const float4*>(at4(sum, r, (c_beg >> 2) + q));
+          f[4 * q] = v.x;
+          f[4 * q + 1] = v.y;
+          f[4 * q + 2] = v.z;
+          f[4 * q + 3] = v.w;
+        }
+      }
+    }
+    if (!on) continue;
+    scale(kUp * kSA / (kSX * kSX), kShift * kSA);
+    split_to(ss);
+    product(ss, ss, false);
+    scale(kUp * kC * kSB / (kSA * kSA), kDiag * kSB);
+    split_to(ss);
+    product(ss, xs, true);
+    if (it + 1 == c.steps) {
+      if (ok) store_result(c, p, k, m, r, j0, f);
+    } else {
+      scale(kUp / kSB, 0.0f);
+      split_to(xs);
+    }
+  }
+
+  if (tid == 0 && !ok) atomicOr(c.status, kStatusTimeout);
+  tc::fence_before_sync();
+  __syncthreads();
+  cluster_sync();                            // no CTA leaves while another may read its sums
+  if (warp == 0) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmem, 256);
   }
 }
 
@@ -663,6 +899,7 @@ struct aht_muon {
   Mat* d_mats = nullptr;
   int4* items = nullptr;
   uint32_t* done = nullptr;
+  int cluster = 0;               // CTAs per matrix of small_updates; 0: the set needs products
   Maps maps{};
   int pairs = 0;                 // CTA pairs resident at once
   uint8_t* ws = nullptr;
@@ -706,12 +943,24 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   c.mu = s->cfg.momentum;
   c.nesterov = s->cfg.nesterov;
   const unsigned n = (unsigned)s->mats.size();
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[2];
+  if (s->cluster) {
+    cfg.gridDim = dim3(n * (unsigned)s->cluster);
+    cfg.blockDim = dim3(kSmallThreads);
+    cfg.dynamicSmemBytes = kSmallSmem;
+    cfg.stream = s->stream;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)s->cluster, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    MUON_CUDA(cudaLaunchKernelEx(&cfg, small_updates, c, p, s->cluster));
+    return AHT_OK;
+  }
   momentum_norm<<<dim3((unsigned)s->norm_blocks, n), 256, 0, s->stream>>>(c, p);
   MUON_CUDA(cudaGetLastError());
   normalise<<<dim3((unsigned)s->norm_chunks, n), 256, 0, s->stream>>>(c, p);
   MUON_CUDA(cudaGetLastError());
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[2];
   products_config(cfg, attr, std::min(s->n_items, s->pairs), s->stream);
   MUON_CUDA(cudaLaunchKernelEx(&cfg, products, c, p, s->maps));
   return AHT_OK;
@@ -807,6 +1056,15 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
       !alloc((void**)&s->done, (size_t)n * 3 * kMaxSteps * 4) || !alloc((void**)&s->status, 4) ||
       cudaMemset(s->status, 0, 4) != cudaSuccess)
     return set_last_error(AHT_ENOMEM, "workspace allocation failed");
+  // A set of matrices that each fit a cluster of small_updates runs there; beside a larger one
+  // they cost nothing in products(), whose other tiles fill their waits.
+  int wide = 0;
+  for (const Mat& m : s->mats) wide = std::max(wide, m.mb == 1 ? m.nb : kSmallCluster + 1);
+  if (wide <= kSmallCluster) {
+    for (s->cluster = 1; s->cluster < wide;) s->cluster *= 2;
+    MUON_CUDA(cudaFuncSetAttribute(small_updates, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem));
+    return AHT_OK;
+  }
   MUON_CUDA(cudaFuncSetAttribute(products, cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * (int)kStage));
   cudaLaunchConfig_t cfg2{};
   cudaLaunchAttribute attr[2];
