@@ -148,6 +148,7 @@ __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Com
           }
         }
       }
+      float part = 0.0f;                       // 16 squares in fp32, the rest in fp64
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         if (mp[x]) {
@@ -157,8 +158,9 @@ __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Com
         }
         const float ux = u_of(c, g[x].x, o[x].x), uy = u_of(c, g[x].y, o[x].y), uz = u_of(c, g[x].z, o[x].z),
                     uw = u_of(c, g[x].w, o[x].w);
-        sum += (double)(ux * ux + uy * uy) + (double)(uz * uz + uw * uw);
+        part += (ux * ux + uy * uy) + (uz * uz + uw * uw);
       }
+      sum += part;
     }
   } else {
     const uint32_t total = rows * cols;
@@ -664,12 +666,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 // Between the phases of such a matrix products() spends 5 us on counters, fences and copies
 // through L2 for 0.8 us of products.  Here a cluster of up to 8 CTAs takes a matrix from the
 // gradient to the updated weights in one launch: a CTA holds 128 columns of X and all of S (or
-// B) in shared memory; the partial Gram matrices of the CTAs are summed in distributed shared
-// memory, each CTA its share of the rows, in the order of the CTAs.  The other two products need
-// no exchange.
+// B) in shared memory.  The CTAs' partial Gram matrices meet in distributed shared memory: each
+// CTA receives everyone's part of its share of the rows, sums them in the order of the CTAs and
+// sends the sum to all (stores only: a remote load waits 0.3 us).  The other two products need no
+// exchange.
 constexpr int kSmallCluster = 8;
 constexpr int kSmallThreads = 256;
-constexpr uint32_t kSmallSmem = 6 * kBlk;      // X hi, lo; S hi, lo (or the partial sums); the sum
+constexpr uint32_t kStaged = 32 * (kB + 1) * 16;  // 128 x 128 fp32, four columns of a row together, padded
+constexpr uint32_t kParts = 7 * 32 * 19 * 16;  // the CTAs' partial sums of one CTA's rows (most: 7 of 19 rows)
+constexpr uint32_t kSmallSmem = 2 * kBlk + kStaged + kParts;  // X hi, lo; S hi, lo or staged; partial sums
+static_assert(2 * kBlk <= kStaged && kStaged <= kParts, "S hi, lo and a staged matrix fit");
 
 __device__ __forceinline__ uint32_t peer_addr(const void* p, int rank) {
   uint32_t r;
@@ -695,8 +701,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ __align__(8) uint64_t done_bar;
   __shared__ uint32_t tmem_slot;
-  __shared__ double norm_s[kSmallThreads], norm_all;
-  uint8_t *xs = smem, *ss = smem + 2 * kBlk, *sum = smem + 4 * kBlk;  // partial sums share ss
+  __shared__ double norm_s[kSmallThreads / 32], norm_all;
+  uint8_t *xs = smem, *ss = smem + 2 * kBlk, *parts = ss + kStaged;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int k = (int)blockIdx.x / cluster, rank = (int)blockIdx.x % cluster;
   const Mat& m = c.mats[k];
@@ -773,45 +779,126 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         for (int e = 0; e < 32; ++e) f[c0 + e] += __uint_as_float(v[e]);
       }
   };
-  auto scale = [&](float s, float diag) {      // the diagonal: column c_beg + e of S is row r
+  auto scale = [&](float s) {
 #pragma unroll
-    for (int e = 0; e < 64; ++e) f[e] = fmaf(f[e], s, r == c_beg + e ? diag : 0.0f);
+    for (int e = 0; e < 64; ++e) f[e] *= s;
+  };
+  auto add_diag = [&](float d) {               // column c_beg + e of S is row r
+    if ((r >> 6) != (c_beg >> 6)) return;      // (warp-uniform)
+#pragma unroll
+    for (int e = 0; e < 64; ++e) f[e] += r == c_beg + e ? d : 0.0f;
+  };
+  // four columns 4 c4.. of a row of a staged matrix
+  auto at4 = [&](uint8_t* base, int row, int c4) { return base + (c4 * (kB + 1) + row) * 16; };
+  auto stage = [&](uint8_t* base) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+      *reinterpret_cast<float4*>(at4(base, r, (c_beg >> 2) + q)) =
+          make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]);
+  };
+  auto unstage = [&](uint8_t* base) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const float4 v = *reinterpret_cast<const float4*>(at4(base, r, (c_beg >> 2) + q));
+      f[4 * q] = v.x;
+      f[4 * q + 1] = v.y;
+      f[4 * q + 2] = v.z;
+      f[4 * q + 3] = v.w;
+    }
   };
 
-  // momentum, U and its norm; X = U / (||U||_F + eps)
-  double sq = 0.0;
+  // Momentum, U and its norm; X = U / (||U||_F + eps).  A wide matrix is read along its rows (a
+  // warp 16 rows, a lane 4 columns of each) through a staged copy; a tall one's rows are columns
+  // of X, and neighbouring threads, rows of X, read neighbouring elements.
+  float sq = 0.0f;                             // 64 squares a thread, the rest in fp64
+  if (!tall) {
+    const bool four = fours(c, p, k, cols);
+    const int c0 = rank * kB + 4 * lane;       // first column of this lane
+    const int left = on ? min(4, max(0, cols - c0)) : 0;
 #pragma unroll
-  for (int b = 0; b < 64; b += 16) {           // sixteen columns' loads in flight together
-    const int left = on && r < rows ? min(16, max(0, cols - j0 - b)) : 0;
-    const int64_t step_m = tall ? p.ld_mom[k] : 1;
-    float* mp = c.update ? p.mom[k] + (tall ? (int64_t)(j0 + b) * p.ld_mom[k] + r : (int64_t)r * p.ld_mom[k] + j0 + b) : nullptr;
-    float mom[16];
+    for (int b = 0; b < 16; b += 8) {          // eight rows' loads in flight together
+      float4 g[8], o[8];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      f[b + e] = e < left ? load_in(c, p, k, tall ? j0 + b + e : r, tall ? r : j0 + b + e) : 0.0f;
-      mom[e] = mp && e < left ? mp[e * step_m] : 0.0f;
+      for (int x = 0; x < 8; ++x) {
+        const int row = 16 * warp + b + x;
+        g[x] = o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row >= rows || left == 0) continue;
+        const float* mp = c.update ? p.mom[k] + (int64_t)row * p.ld_mom[k] + c0 : nullptr;
+        if (four) {                            // (cols is a multiple of four: left is 4)
+          g[x] = load_in4(c, p, k, row, c0);
+          if (mp) o[x] = *reinterpret_cast<const float4*>(mp);
+        } else {
+          float* gs = &g[x].x;
+          float* os = &o[x].x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < left) {
+              gs[e] = load_in(c, p, k, row, c0 + e);
+              if (mp) os[e] = mp[e];
+            }
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int row = 16 * warp + b + x;
+        o[x] = make_float4(fmaf(c.mu, o[x].x, g[x].x), fmaf(c.mu, o[x].y, g[x].y), fmaf(c.mu, o[x].z, g[x].z),
+                           fmaf(c.mu, o[x].w, g[x].w));
+        if (c.update && row < rows && left) {
+          float* mp = p.mom[k] + (int64_t)row * p.ld_mom[k] + c0;
+          if (four) *reinterpret_cast<float4*>(mp) = o[x];
+          else {
+            const float os[4] = {o[x].x, o[x].y, o[x].z, o[x].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e < left) mp[e] = os[e];
+          }
+        }
+        const float4 u = make_float4(u_of(c, g[x].x, o[x].x), u_of(c, g[x].y, o[x].y), u_of(c, g[x].z, o[x].z),
+                                     u_of(c, g[x].w, o[x].w));
+        sq += (u.x * u.x + u.y * u.y) + (u.z * u.z + u.w * u.w);
+        *reinterpret_cast<float4*>(at4(ss, row, lane)) = u;
+      }
     }
+  } else {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      mom[e] = fmaf(c.mu, mom[e], f[b + e]);
-      if (mp && e < left) mp[e * step_m] = mom[e];
-      f[b + e] = u_of(c, f[b + e], mom[e]);
-      sq += (double)(f[b + e] * f[b + e]);
+    for (int b = 0; b < 64; b += 16) {         // sixteen columns' loads in flight together
+      const int left = on && r < rows ? min(16, max(0, cols - j0 - b)) : 0;
+      const int64_t step_m = p.ld_mom[k];
+      float* mp = c.update ? p.mom[k] + (int64_t)(j0 + b) * step_m + r : nullptr;
+      float mom[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        f[b + e] = e < left ? load_in(c, p, k, j0 + b + e, r) : 0.0f;
+        mom[e] = mp && e < left ? mp[e * step_m] : 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        mom[e] = fmaf(c.mu, mom[e], f[b + e]);
+        if (mp && e < left) mp[e * step_m] = mom[e];
+        f[b + e] = u_of(c, f[b + e], mom[e]);
+        sq += f[b + e] * f[b + e];
+      }
     }
   }
-  norm_s[tid] = sq;
-  for (int s = kSmallThreads / 2; s > 0; s >>= 1) {
-    __syncthreads();
-    if (tid < s) norm_s[tid] += norm_s[tid + s];
-  }
+  double warp_sq = sq;
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) warp_sq += __shfl_xor_sync(0xFFFFFFFFu, warp_sq, x);
+  if (lane == 0) norm_s[warp] = warp_sq;
   __syncthreads();
-  cluster_sync();
   if (tid == 0) {
     double t = 0.0;
-    for (int q = 0; q < nb; ++q) t += peer_load_f64(peer_addr(&norm_s[0], q));
-    norm_all = t;
+    for (int w = 0; w < kSmallThreads / 32; ++w) t += norm_s[w];
+    norm_s[0] = t;
+  }
+  cluster_sync();
+  if (warp == 0) {
+    const double mine = lane < nb ? peer_load_f64(peer_addr(&norm_s[0], lane)) : 0.0;
+    double t = 0.0;
+    for (int q = 0; q < nb; ++q) t += __shfl_sync(0xFFFFFFFFu, mine, q);
+    if (lane == 0) norm_all = t;
   }
   __syncthreads();
+  if (!tall) unstage(ss);
   const float inv = (float)(1.0 / (sqrt(norm_all) + (double)c.eps));
 #pragma unroll
   for (int e = 0; e < 64; ++e) f[e] = (f[e] * inv) * kSX;
@@ -819,50 +906,95 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
 
   // rows of the Gram matrix this CTA sums for all
   const int r_beg = on ? kB * rank / nb : 0, r_cnt = on ? kB * (rank + 1) / nb - r_beg : 0;
-  auto at4 = [&](uint8_t* base, int row, int c4) { return base + (c4 * kB + row) * 16; };  // 4 columns of a row
   for (int it = 0; it < c.steps; ++it) {
     if (on) product(xs, xs, false);
     if (nb > 1) {
-      if (on) {
+      if (on) {                                // this CTA's part of row r, to the CTA that sums it
+        const int owner = min(nb - 1, (r * nb + nb - 1) / kB), first = kB * owner / nb;
+        const int to = r < first ? owner - 1 : owner, beg = kB * to / nb, cnt = kB * (to + 1) / nb - beg;
+        const uint32_t at = peer_addr(parts, to) + (uint32_t)((rank * 32 + (c_beg >> 2)) * cnt + r - beg) * 16u;
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-          *reinterpret_cast<float4*>(at4(ss, r, (c_beg >> 2) + q)) =
-              make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]);
+          peer_store(at + (uint32_t)(q * cnt) * 16u, make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]));
       }
       cluster_sync();
       for (int e = tid; e < 32 * r_cnt; e += kSmallThreads) {
-        const int c4 = e / r_cnt, row = r_beg + e - c4 * r_cnt;
+        const int c4 = e / r_cnt, row = e - c4 * r_cnt;
         float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int q = 0; q < nb; ++q) {
-          const float4 v = peer_load(peer_addr(at4(ss, row, c4), q));
+          const float4 v = *reinterpret_cast<const float4*>(parts + ((q * 32 + c4) * r_cnt + row) * 16);
           t = make_float4(t.x + v.x, t.y + v.y, t.z + v.z, t.w + v.w);
         }
-        for (int q = 0; q < nb; ++q) peer_store(peer_addr(at4(sum, row, c4), q), t);
+        const uint32_t off = (uint32_t)(c4 * (kB + 1) + r_beg + row) * 16u;
+        for (int q = 0; q < nb; ++q) peer_store(peer_addr(ss, q) + off, t);
       }
       cluster_sync();
-      if (on) {
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          const float4 v = *reinterpret_cast<const float4*>(at4(sum, r, (c_beg >> 2) + q));
-          f[4 * q] = v.x;
-          f[4 * q + 1] = v.y;
-          f[4 * q + 2] = v.z;
-          f[4 * q + 3] = v.w;
-        }
-      }
+      if (on) unstage(ss);
+      __syncthreads();                         // (ss is written next)
     }
     if (!on) continue;
-    scale(kUp * kSA / (kSX * kSX), kShift * kSA);
+    scale(kUp * kSA / (kSX * kSX));
+    add_diag(kShift * kSA);
     split_to(ss);
     product(ss, ss, false);
-    scale(kUp * kC * kSB / (kSA * kSA), kDiag * kSB);
+    scale(kUp * kC * kSB / (kSA * kSA));
+    add_diag(kDiag * kSB);
     split_to(ss);
     product(ss, xs, true);
-    if (it + 1 == c.steps) {
-      if (ok) store_result(c, p, k, m, r, j0, f);
-    } else {
-      scale(kUp / kSB, 0.0f);
+    if (it + 1 < c.steps) {
+      scale(kUp / kSB);
       split_to(xs);
+    }
+  }
+  // the weights, along their rows like the gradient
+  if (on && tall && ok) store_result(c, p, k, m, r, j0, f);
+  if (on && !tall) {
+    scale(kUp / (kSB * kSX));
+    stage(parts);
+    __syncthreads();
+    const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
+    const int c0 = rank * kB + 4 * lane, left = min(4, max(0, cols - c0));
+    const bool four = left == 4 && !c.bf16_out && ((uintptr_t)p.out[k] & 15) == 0 && (p.ld_out[k] & 3) == 0;
+#pragma unroll
+    for (int b = 0; b < 16; b += 8) {
+      float4 o[8], old[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int row = 16 * warp + b + x;
+        o[x] = *reinterpret_cast<const float4*>(at4(parts, row, lane));
+        old[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!c.update || !ok || row >= rows) continue;
+        const float* w = static_cast<const float*>(p.out[k]) + (int64_t)row * p.ld_out[k] + c0;
+        if (four) old[x] = *reinterpret_cast<const float4*>(w);
+        else {
+          float* os = &old[x].x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < left) os[e] = w[e];
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int row = 16 * warp + b + x;
+        if (!ok || row >= rows) continue;
+        const int64_t at = (int64_t)row * p.ld_out[k] + c0;
+        float v[4] = {o[x].x, o[x].y, o[x].z, o[x].w};
+        if (c.update) {
+          v[0] = fmaf(-lr, v[0], c.decay * old[x].x);
+          v[1] = fmaf(-lr, v[1], c.decay * old[x].y);
+          v[2] = fmaf(-lr, v[2], c.decay * old[x].z);
+          v[3] = fmaf(-lr, v[3], c.decay * old[x].w);
+        }
+        if (four) *reinterpret_cast<float4*>(static_cast<float*>(p.out[k]) + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (e >= left) continue;
+            if (c.bf16_out) static_cast<__nv_bfloat16*>(p.out[k])[at + e] = __float2bfloat16_rn(v[e]);
+            else static_cast<float*>(p.out[k])[at + e] = v[e];
+          }
+        }
+      }
     }
   }
 
