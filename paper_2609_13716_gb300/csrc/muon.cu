@@ -677,6 +677,8 @@ constexpr uint32_t kParts = 7 * 32 * 19 * 16;  // the CTAs' partial sums of one 
 constexpr uint32_t kSmallSmem = 2 * kBlk + kStaged + kParts;  // X hi, lo; S hi, lo or staged; partial sums
 static_assert(2 * kBlk <= kStaged && kStaged <= kParts, "S hi, lo and a staged matrix fit");
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer_addr(const void* p, int rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(tc::smem_u32(p)), "r"(rank));
@@ -908,7 +910,27 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   const int r_beg = on ? kB * rank / nb : 0, r_cnt = on ? kB * (rank + 1) / nb - r_beg : 0;
   for (int it = 0; it < c.steps; ++it) {
     if (on) product(xs, xs, false);
-    if (nb > 1) {
+    if (nb == 2) {                             // each takes the other's part whole: one wait
+      if (it > 0) cluster_wait();              // the other has read what it received last
+      if (on) {
+        const uint32_t at = peer_addr(parts, rank ^ 1) + (uint32_t)((c_beg >> 2) * (kB + 1) + r) * 16u;
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          peer_store(at + (uint32_t)(q * (kB + 1)) * 16u, make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]));
+      }
+      cluster_sync();
+      if (on) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {         // (a sum of two: the same bits in either order)
+          const float4 v = *reinterpret_cast<const float4*>(at4(parts, r, (c_beg >> 2) + q));
+          f[4 * q] += v.x;
+          f[4 * q + 1] += v.y;
+          f[4 * q + 2] += v.z;
+          f[4 * q + 3] += v.w;
+        }
+      }
+      cluster_arrive();
+    } else if (nb > 2) {
       if (on) {                                // this CTA's part of row r, to the CTA that sums it
         const int owner = min(nb - 1, (r * nb + nb - 1) / kB), first = kB * owner / nb;
         const int to = r < first ? owner - 1 : owner, beg = kB * to / nb, cnt = kB * (to + 1) / nb - beg;
@@ -946,6 +968,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       split_to(xs);
     }
   }
+  if (nb == 2) cluster_wait();
   // the weights, along their rows like the gradient
   if (on && tall && ok) store_result(c, p, k, m, r, j0, f);
   if (on && !tall) {
