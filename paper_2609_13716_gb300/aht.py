@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 import threading
 
 import torch
@@ -98,6 +99,8 @@ def library_path() -> str:
 def load() -> C.CDLL:
     """Loads libaht.so (built in-tree).  Raises if it is missing: no fallback exists."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             path = library_path()
@@ -124,10 +127,10 @@ def load() -> C.CDLL:
             L.aht_glr_ckpt_elems.restype = i64
             L.aht_glr_workspace.argtypes = [i64, i64, i32]
             L.aht_glr_workspace.restype = i64
-            L.aht_glr_forward.argtypes = [C.POINTER(GlrArgs), vp, C.POINTER(Seq), vp, vp, vp]
+            # (structs go as packed bytes or by reference: vp takes both)
+            L.aht_glr_forward.argtypes = [vp, vp, vp, vp, vp, vp]
             L.aht_glr_forward.restype = C.c_int
-            L.aht_glr_backward.argtypes = [C.POINTER(GlrArgs), vp, C.POINTER(Seq), vp, C.POINTER(Seq), C.POINTER(Seq),
-                                           C.POINTER(Seq), vp, vp, vp, i64, vp]
+            L.aht_glr_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
             L.aht_glr_backward.restype = C.c_int
             L.aht_muon_create.argtypes = [i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(MuonConfig), vp, C.POINTER(vp)]
             L.aht_muon_destroy.argtypes = [vp]
@@ -205,13 +208,19 @@ def _ptr(t, dtype=None, shape=None, name="tensor"):
         raise ValueError(f"{name} must be contiguous")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     return t.data_ptr()
 
 
+# the current stream's handle without a Stream object (about 2 us less a call), where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
@@ -696,42 +705,46 @@ class GlrArgs(C.Structure):
                 ("lengths", C.c_void_p)]
 
 
+_pack_seq = struct.Struct("@Pqq").pack              # Seq
+_pack_glr = struct.Struct("@iiqqPqqPqqPqqPPP").pack  # GlrArgs
+
+
 def _seq(t, shape, dtype, name, written=False):
-    """A [T][N][D] tensor with contiguous channels and any step and env strides."""
+    """Pointer and strides of a [T][N][D] tensor with contiguous channels and any step and env
+    strides."""
     if t is None:
-        return Seq(None, 0, 0)
+        return 0, 0, 0
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     T, N, D = shape
-    if t.numel() and D > 1 and t.stride(2) != 1:
+    st, sn, sd = t.stride()
+    if sd != 1 and D > 1 and t.numel():
         raise ValueError(f"{name} must have contiguous channels (stride 1 in its last dimension)")
-    st, sn = (t.stride(0) if T > 1 else 0), (t.stride(1) if N > 1 else 0)
-    if written and t.numel():
+    if written and not (st >= sn * N and sn >= D) and t.numel():
         # every element an address of its own: the strides nest around a row of D channels
-        dims = sorted((s, k) for s, k in ((st, T), (sn, N)) if k > 1)
         extent = D
-        for s, k in dims:
+        for s, k in sorted((s, k) for s, k in ((st, T), (sn, N)) if k > 1):
             if s < extent:
                 raise ValueError(f"{name} is written: its steps and envs must not overlap in memory")
             extent = s * (k - 1) + extent
-    return Seq(t.data_ptr(), st, sn)
+    return t.data_ptr(), st, sn
 
 
 def _glr_args(x, r, i, lam, reset, lengths):
     if not isinstance(x, torch.Tensor) or x.dim() != 3:
         raise ValueError("x must be a [T][N][D] tensor")
-    if x.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError(f"x must be float32 or bfloat16, got {x.dtype}")
-    T, N, D = x.shape
-    dt = x.dtype
-    return (T, N, D), dt, GlrArgs(
-        AHT_FP32 if dt == torch.float32 else AHT_BF16, D, T, N, _seq(x, x.shape, dt, "x"), _seq(r, x.shape, dt, "r"),
-        _seq(i, x.shape, dt, "i"), _ptr(lam, torch.float32, (D,), "lam"),
-        _ptr(reset, torch.uint8, (T, N), "reset"), _ptr(lengths, torch.int32, (N,), "lengths"))
+    dt, shape = x.dtype, x.shape
+    if dt is not torch.float32 and dt is not torch.bfloat16:
+        raise TypeError(f"x must be float32 or bfloat16, got {dt}")
+    T, N, D = shape
+    return shape, dt, _pack_glr(
+        AHT_FP32 if dt is torch.float32 else AHT_BF16, D, T, N, *_seq(x, shape, dt, "x"), *_seq(r, shape, dt, "r"),
+        *_seq(i, shape, dt, "i"), _ptr(lam, torch.float32, (D,), "lam") or 0,
+        _ptr(reset, torch.uint8, (T, N), "reset") or 0, _ptr(lengths, torch.int32, (N,), "lengths") or 0)
 
 
 def aht_glr_ckpt_shape(T, N, D):
@@ -750,8 +763,7 @@ def aht_glr_forward(x, r, i, lam, h=None, reset=None, lengths=None, h0=None, h_l
     shape, dt, a = _glr_args(x, r, i, lam, reset, lengths)
     T, N, D = shape
     f32 = torch.float32
-    hs = _seq(h, shape, dt, "h", written=True)
-    _check(load().aht_glr_forward(C.byref(a), _ptr(h0, f32, (N, D), "h0"), C.byref(hs),
+    _check(load().aht_glr_forward(a, _ptr(h0, f32, (N, D), "h0"), _pack_seq(*_seq(h, shape, dt, "h", True)),
                                   _ptr(h_last, f32, (N, D), "h_last"),
                                   _ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt"), _stream(stream)))
 
@@ -762,11 +774,12 @@ def aht_glr_backward(x, r, i, lam, ckpt, dh, dx, dr, di, dlam=None, workspace=No
     shape, dt, a = _glr_args(x, r, i, lam, reset, lengths)
     T, N, D = shape
     f32 = torch.float32
-    s = {k: _seq(t, shape, dt, k, written=k != "dh") for k, t in (("dh", dh), ("dx", dx), ("dr", dr), ("di", di))}
+    sdh, sdx, sdr, sdi = (_pack_seq(*_seq(t, shape, dt, k, k != "dh"))
+                          for k, t in (("dh", dh), ("dx", dx), ("dr", dr), ("di", di)))
     ws = _ptr(workspace, torch.uint8, None, "workspace")
-    _check(load().aht_glr_backward(C.byref(a), _ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt"),
-                                   C.byref(s["dh"]), _ptr(dh_last, f32, (N, D), "dh_last"), C.byref(s["dx"]),
-                                   C.byref(s["dr"]), C.byref(s["di"]), _ptr(dlam, f32, (D,), "dlam"),
+    _check(load().aht_glr_backward(a, _ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt"), sdh,
+                                   _ptr(dh_last, f32, (N, D), "dh_last"), sdx, sdr, sdi,
+                                   _ptr(dlam, f32, (D,), "dlam"),
                                    _ptr(dh0, f32, (N, D), "dh0"), ws, 0 if workspace is None else workspace.numel(),
                                    _stream(stream)))
 
