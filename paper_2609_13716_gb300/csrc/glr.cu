@@ -167,12 +167,11 @@ struct Walk {
   }
 };
 
-// Bit k: step t0 + k begins an episode (t0 + k < len), for k < S <= 32; one byte per lane.
+// Whether step t0 + lane begins an episode (t0 + lane < len); a ballot of it gives a segment's
+// resets.  Loaded with a segment's rows, a window before the ballot waits for it.
 template <int S>
-__device__ __forceinline__ uint32_t reset_bits(const GlrDev& a, const Place& at, int64_t t0, int lane) {
-  if (!a.reset) return 0;
-  const bool r = lane < S && t0 + lane < at.len && __ldg(a.reset + (t0 + lane) * a.N + at.n) != 0;
-  return __ballot_sync(0xFFFFFFFFu, r);
+__device__ __forceinline__ uint8_t reset_byte(const GlrDev& a, const Place& at, int64_t t0, int lane) {
+  return a.reset && lane < S && t0 + lane < at.len ? __ldg(a.reset + (t0 + lane) * a.N + at.n) : (uint8_t)0;
 }
 
 // The map that reaches segment (rank, wt) of a window, from the maps (A, H) that every
@@ -297,7 +296,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   }
   small = __all_sync(0xFFFFFFFFu, small);
   Vec<E, V> nx[S], nr[S], ni[S];
-  uint32_t nrs = 0;
+  uint8_t nrs = 0;
   const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
   const E* pr = static_cast<const E*>(a.r.p) + at.n * a.r.sn + at.d;
   const E* pi = static_cast<const E*>(a.i.p) + at.n * a.i.sn + at.d;
@@ -316,13 +315,13 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         nx[k].load(qx);
       }
     }
-    nrs = reset_bits<S>(a, at, t0, lane);
+    nrs = reset_byte<S>(a, at, t0, lane);
   };
   fetch((int64_t)seg * S);
   int buf = 0;
   for (int64_t w0 = 0; w0 < a.T; w0 += window, buf ^= 1) {
     const int64_t t0 = w0 + (int64_t)seg * S;
-    const uint32_t rs = nrs;
+    const uint32_t rs = __ballot_sync(0xFFFFFFFFu, nrs != 0);
     // a full segment without a reset needs no masks
     const bool plain = rs == 0 && t0 + S <= at.len;
     float da[kE], b[kE];  // decay and input of element k V + v
@@ -462,7 +461,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   small = __all_sync(0xFFFFFFFFu, small);
   Vec<E, V> nx[S], nr[S], ni[S], ng[S];
   float nc[V];
-  uint32_t nrs = 0;
+  uint8_t nrs = 0;
   const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
   const E* pr = static_cast<const E*>(a.r.p) + at.n * a.r.sn + at.d;
   const E* pi = static_cast<const E*>(a.i.p) + at.n * a.i.sn + at.d;
@@ -488,7 +487,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         if (b.dh.p) ng[k].load(qg);
       }
     }
-    nrs = reset_bits<S>(a, at, t0, lane);
+    nrs = reset_byte<S>(a, at, t0, lane);
   };
   if (kAhead && a.T > 0) fetch(last);
   int buf = 0;
@@ -496,7 +495,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     if (!kAhead) fetch(t0);
     float em[kE], rho[kE], iota[kE], prev[kE], p[V];
     Vec<E, V> x[S], g[S];
-    const uint32_t rs = nrs;
+    const uint32_t rs = __ballot_sync(0xFFFFFFFFu, nrs != 0);
     const bool plain = rs == 0 && t0 + S <= at.len;  // no masks needed
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = nc[v];
