@@ -167,6 +167,36 @@ struct Walk {
   }
 };
 
+// A warp's ring of segments in shared memory, filled by asynchronous copies: a row is 128 bytes
+// (32 lanes of 4), copied by 8 lanes, 16 bytes each; what lies past the env's steps or its
+// channels is zero.  Rows start on 16-byte boundaries (checked by the host).
+template <int kTensors, int S, int kExtra>
+struct Ring {
+  static constexpr int kStage = kTensors * S * 128 + kExtra;  // bytes of a segment
+  __device__ __forceinline__ static void copy16(void* dst, const void* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(dst)), "l"(src), "r"(on ? 16 : 0)
+                 : "memory");
+  }
+  __device__ __forceinline__ static void rows(uint8_t* slot, int tensor, const Seq& s, const void* lane0, int esz,
+                                              int64_t t0, int64_t left, int lane, bool chunk) {
+    const int64_t step = s.st * esz;
+    const char* src = static_cast<const char*>(lane0) + (t0 + (lane >> 3)) * step + (lane & 7) * 16;
+    uint8_t* dst = slot + tensor * S * 128 + (lane >> 3) * 128 + (lane & 7) * 16;
+#pragma unroll
+    for (int k = 0; k < S; k += 4) {
+      const bool on = chunk && k + (lane >> 3) < left;
+      copy16(dst + k * 128, on ? src : static_cast<const char*>(s.p), on);
+      src += 4 * step;
+    }
+  }
+  __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  template <int kLeft>
+  __device__ __forceinline__ static void wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+    __syncwarp();
+  }
+};
+
 // Whether step t0 + lane begins an episode (t0 + lane < len); a ballot of it gives a segment's
 // resets.  Loaded with a segment's rows, a window before the ballot waits for it.
 template <int S>
@@ -267,8 +297,10 @@ struct Exchange {
   }
 };
 
-// CTAs of kWarps warps: WT of them share lanes, kWarps / WT lane groups.
-template <typename E, int V, int S, int WT, int kWarps, bool kCluster>
+// CTAs of kWarps warps: WT of them share lanes, kWarps / WT lane groups.  kRing > 0: the rows
+// come through a ring of that many segments (rows of 4-byte lanes, aligned); 0: the next
+// segment waits in registers.
+template <typename E, int V, int S, int WT, int kWarps, bool kCluster, int kRing>
 __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     glr_fwd(const __grid_constant__ GlrDev a, const float* h0, const __grid_constant__ Seq h, float* h_last,
             float* ckpt, int n_rank) {
@@ -297,10 +329,24 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   small = __all_sync(0xFFFFFFFFu, small);
   Vec<E, V> nx[S], nr[S], ni[S];
   uint8_t nrs = 0;
+  using R = Ring<3, S, 0>;
+  static_assert(kRing == 0 || V * sizeof(E) == 4, "the ring's rows have 4 bytes a lane");
+  extern __shared__ __align__(128) uint8_t ring_smem[];
+  uint8_t* ring = ring_smem + (kRing ? warp * kRing * R::kStage : 0);
+  const bool any = unit < a.N * tiles, chunk = any && at.d - lane * V + (lane & 7) * 4 * V < a.D;
+  int slot = 0;
   const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
   const E* pr = static_cast<const E*>(a.r.p) + at.n * a.r.sn + at.d;
   const E* pi = static_cast<const E*>(a.i.p) + at.n * a.i.sn + at.d;
   const E* ph = static_cast<const E*>(h.p) + at.n * h.sn + at.d;
+  auto fetch_ring = [&](int64_t t0, int to) {
+    uint8_t* dst = ring + to * R::kStage;
+    const int64_t left = at.len - t0;
+    R::rows(dst, 0, a.r, pr - lane * V, sizeof(E), t0, left, lane, chunk);
+    R::rows(dst, 1, a.i, pi - lane * V, sizeof(E), t0, left, lane, chunk);
+    R::rows(dst, 2, a.x, px - lane * V, sizeof(E), t0, left, lane, chunk);
+    R::commit();
+  };
   auto fetch = [&](int64_t t0) {
     Walk wr(a.r, pr, sizeof(E), t0), wi(a.i, pi, sizeof(E), t0), wx(a.x, px, sizeof(E), t0);
 #pragma unroll
@@ -317,7 +363,13 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     }
     nrs = reset_byte<S>(a, at, t0, lane);
   };
-  fetch((int64_t)seg * S);
+  if (kRing) {
+#pragma unroll
+    for (int w = 0; w < kRing; ++w) fetch_ring((int64_t)seg * S + w * window, w);
+    nrs = reset_byte<S>(a, at, (int64_t)seg * S, lane);
+  } else {
+    fetch((int64_t)seg * S);
+  }
   int buf = 0;
   for (int64_t w0 = 0; w0 < a.T; w0 += window, buf ^= 1) {
     const int64_t t0 = w0 + (int64_t)seg * S;
@@ -326,6 +378,16 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     const bool plain = rs == 0 && t0 + S <= at.len;
     float da[kE], b[kE];  // decay and input of element k V + v
     float y[V];
+    if (kRing) {
+      R::template wait<(kRing > 0 ? kRing - 1 : 0)>();
+      const uint8_t* src = ring + slot * R::kStage + lane * 4;
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        nr[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + k * 128);
+        ni[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (S + k) * 128);
+        nx[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (2 * S + k) * 128);
+      }
+    }
     auto gate = [&](auto small_c) {
 #pragma unroll
       for (int e = 0; e < kE; e += 2) {
@@ -342,7 +404,14 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     };
     if (small) gate(std::true_type());
     else gate(std::false_type());
-    if (w0 + window < a.T) fetch(t0 + window);
+    if (kRing) {
+      __syncwarp();                       // every lane has read the slot
+      fetch_ring(t0 + kRing * window, slot);
+      slot = slot + 1 == kRing ? 0 : slot + 1;
+      nrs = reset_byte<S>(a, at, t0 + window, lane);
+    } else if (w0 + window < a.T) {
+      fetch(t0 + window);
+    }
     if (!plain) {
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
@@ -417,6 +486,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
       for (int v = 0; v < V; ++v) carry[v] = y[v];
     }
   }
+  if (kRing) R::template wait<0>();
   if (h_last && at.on && seg == 0) {
 #pragma unroll
     for (int v = 0; v < V; ++v) h_last[me + v] = carry[v];
@@ -432,8 +502,8 @@ struct GlrGrad {
   float* part;  // [segments of a window][N][D] sums of w over a thread's steps
 };
 
-// kAhead: the next segment is loaded while the present one is computed (registers allowing).
-template <typename E, int V, int WT, int kWarps, bool kCluster, bool kAhead>
+// kRing as in glr_fwd; 0: loaded when needed, which other warps cover.
+template <typename E, int V, int WT, int kWarps, bool kCluster, int kRing>
 __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     glr_bwd(const __grid_constant__ GlrDev a, const __grid_constant__ GlrGrad b, int n_rank) {
   using X = Exchange<V, WT, kCluster>;
@@ -462,6 +532,12 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   Vec<E, V> nx[S], nr[S], ni[S], ng[S];
   float nc[V];
   uint8_t nrs = 0;
+  using R = Ring<4, S, 128 * V>;  // and the checkpoint
+  static_assert(kRing == 0 || V * sizeof(E) == 4, "the ring's rows have 4 bytes a lane");
+  extern __shared__ __align__(128) uint8_t ring_smem[];
+  uint8_t* ring = ring_smem + (kRing ? warp * kRing * R::kStage : 0);
+  const bool any = unit < a.N * tiles, chunk = any && at.d - lane * V + (lane & 7) * 4 * V < a.D;
+  int slot = 0;
   const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
   const E* pr = static_cast<const E*>(a.r.p) + at.n * a.r.sn + at.d;
   const E* pi = static_cast<const E*>(a.i.p) + at.n * a.i.sn + at.d;
@@ -469,6 +545,20 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   const E* pdx = static_cast<const E*>(b.dx.p) + at.n * b.dx.sn + at.d;
   const E* pdr = static_cast<const E*>(b.dr.p) + at.n * b.dr.sn + at.d;
   const E* pdi = static_cast<const E*>(b.di.p) + at.n * b.di.sn + at.d;
+  auto fetch_ring = [&](int64_t t0, int to) {  // (t0 < 0: before the first step, nothing is copied)
+    uint8_t* dst = ring + to * R::kStage;
+    const int64_t left = t0 < 0 ? 0 : at.len - t0;
+    R::rows(dst, 0, a.r, pr - lane * V, sizeof(E), t0, left, lane, chunk);
+    R::rows(dst, 1, a.i, pi - lane * V, sizeof(E), t0, left, lane, chunk);
+    R::rows(dst, 2, a.x, px - lane * V, sizeof(E), t0, left, lane, chunk);
+    if (b.dh.p) R::rows(dst, 3, b.dh, pg - lane * V, sizeof(E), t0, left, lane, chunk);
+    // 32 V floats, 4 a lane (V = 1: lanes 0..7)
+    const int64_t d4 = at.d - lane * V + 4 * lane;
+    const bool on = any && lane < 8 * V && d4 < a.D && left > 0;
+    if (lane < 8 * V)
+      R::copy16(dst + 4 * S * 128 + lane * 16, on ? b.ckpt + (t0 / kSeg) * lanes + at.n * a.D + d4 : b.ckpt, on);
+    R::commit();
+  };
   auto fetch = [&](int64_t t0) {
     Walk wr(a.r, pr, sizeof(E), t0), wi(a.i, pi, sizeof(E), t0), wx(a.x, px, sizeof(E), t0), wg(b.dh, pg, sizeof(E), t0);
 #pragma unroll
@@ -489,10 +579,29 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     }
     nrs = reset_byte<S>(a, at, t0, lane);
   };
-  if (kAhead && a.T > 0) fetch(last);
+  if (kRing && a.T > 0) {
+#pragma unroll
+    for (int w = 0; w < kRing; ++w) fetch_ring(last - w * window, w);
+    nrs = reset_byte<S>(a, at, last, lane);
+  }
   int buf = 0;
   for (int64_t t0 = last, w = (a.T + window - 1) / window; w > 0; --w, t0 -= window, buf ^= 1) {
-    if (!kAhead) fetch(t0);
+    if (kRing) {
+      R::template wait<(kRing > 0 ? kRing - 1 : 0)>();
+      const uint8_t* src = ring + slot * R::kStage + lane * 4;
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        nr[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + k * 128);
+        ni[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (S + k) * 128);
+        nx[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (2 * S + k) * 128);
+        ng[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (3 * S + k) * 128);
+        if (!b.dh.p) ng[k].zero();
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) nc[v] = reinterpret_cast<const float*>(ring + slot * R::kStage + 4 * S * 128)[lane * V + v];
+    } else {
+      fetch(t0);
+    }
     float em[kE], rho[kE], iota[kE], prev[kE], p[V];
     Vec<E, V> x[S], g[S];
     const uint32_t rs = __ballot_sync(0xFFFFFFFFu, nrs != 0);
@@ -523,7 +632,12 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     };
     if (small) gate(std::true_type());
     else gate(std::false_type());
-    if (kAhead && w > 1) fetch(t0 - window);
+    if (kRing) {
+      __syncwarp();                       // every lane has read the slot
+      fetch_ring(t0 - kRing * window, slot);
+      slot = slot + 1 == kRing ? 0 : slot + 1;
+      nrs = w > 1 ? reset_byte<S>(a, at, t0 - window, lane) : (uint8_t)0;
+    }
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
       const int k = e / V, v = e % V;
@@ -604,6 +718,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
       if (WT == 1 && !kCluster) carry[v] = p[v];
     }
   }
+  if (kRing) R::template wait<0>();
   if (!at.on) return;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
@@ -690,10 +805,13 @@ Split split_of(int64_t T, int64_t N, int32_t D, int V) {
 }
 
 template <typename K, typename... Args>
-aht_status launch(K kernel, int64_t blocks, int threads, int cl, cudaStream_t s, Args... args) {
+aht_status launch(K kernel, int64_t blocks, int threads, int cl, int smem, cudaStream_t s, Args... args) {
+  if (smem > 48 * 1024)
+    if (aht_status e = launched(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem))) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(blocks * cl));
   cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -708,26 +826,29 @@ template <typename E, int V, int S>
 aht_status forward_wide(const aht_glr_args* a, const float* h0, const Seq& h, float* h_last, float* ckpt, cudaStream_t s) {
   const int64_t four = (split_of(a->T, a->N, a->D, V).units + 3) / 4;
   constexpr int kShort = V > 1 ? 1 : 2;  // steps of a segment when T = 1 (elements go in pairs)
-  if (a->T <= 1) return launch(glr_fwd<E, V, kShort, 1, 4, false>, four, 128, 1, s, dev(a), h0, h, h_last, ckpt, 1);
-  return launch(glr_fwd<E, V, S, 1, 4, false>, four, 128, 1, s, dev(a), h0, h, h_last, ckpt, 1);
+  if (a->T <= 1) return launch(glr_fwd<E, V, kShort, 1, 4, false, 0>, four, 128, 1, 0, s, dev(a), h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, S, 1, 4, false, 0>, four, 128, 1, 0, s, dev(a), h0, h, h_last, ckpt, 1);
 }
 // Few lanes: 8 warps and p.cl CTAs along time.
-template <typename E, int V, int S>
+template <typename E, int V, int S, int kRing>
 aht_status forward_long(const aht_glr_args* a, const Split& p, const float* h0, const Seq& h, float* h_last, float* ckpt,
                         cudaStream_t s) {
-  if (p.cl == 1) return launch(glr_fwd<E, V, S, 8, 8, false>, p.units, 256, 1, s, dev(a), h0, h, h_last, ckpt, 1);
-  return launch(glr_fwd<E, V, S, 8, 8, true>, p.units, 256, p.cl, s, dev(a), h0, h, h_last, ckpt, p.cl);
+  constexpr int kSmem = 8 * kRing * Ring<3, S, 0>::kStage;
+  if (p.cl == 1)
+    return launch(glr_fwd<E, V, S, 8, 8, false, kRing>, p.units, 256, 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, S, 8, 8, true, kRing>, p.units, 256, p.cl, kSmem, s, dev(a), h0, h, h_last, ckpt, p.cl);
 }
 
-template <typename E, int V>
+template <typename E, int V, bool kRows>  // kRows: rows aligned for the ring
 aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStream_t s) {
   const Split p = split_of(a->T, a->N, a->D, V);
   const GlrDev d = dev(a);
   *rows = p.segs();
-  constexpr bool kAhead = V == 1;
-  if (p.wt == 1) return launch(glr_bwd<E, V, 1, 4, false, kAhead>, (p.units + 3) / 4, 128, 1, s, d, g, 1);
-  if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kAhead>, p.units, 256, 1, s, d, g, 1);
-  return launch(glr_bwd<E, V, 8, 8, true, kAhead>, p.units, 256, p.cl, s, d, g, p.cl);
+  constexpr int kStage = Ring<4, kSeg, 128 * V>::kStage, kWide = kRows && V == 1 ? 2 : 0, kLong = kRows ? (V == 1 ? 3 : 2) : 0;
+  if (p.wt == 1)
+    return launch(glr_bwd<E, V, 1, 4, false, kWide>, (p.units + 3) / 4, 128, 1, 4 * kWide * kStage, s, d, g, 1);
+  if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kLong>, p.units, 256, 1, 8 * kLong * kStage, s, d, g, 1);
+  return launch(glr_bwd<E, V, 8, 8, true, kLong>, p.units, 256, p.cl, 8 * kLong * kStage, s, d, g, p.cl);
 }
 
 constexpr int kSumRows = 64;  // row groups of the first pass of dlam's sum
@@ -762,20 +883,25 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
   };
   // groups of 32 V channels that leave at most one thread in `of` without channels
   auto fills = [&](int V, int of) { return (a->D + 32 * V - 1) / (32 * V) * 32 * V <= a->D + a->D / of; };
+  const bool rows = fits(16 / esz);      // every row a whole number of aligned 16-byte chunks
   auto wide = [&](int V) { return a->T <= 1 || split_of(a->T, a->N, a->D, V).wt == 1; };
   if (a->dtype == AHT_FP32) {
     if (fits(4) && fills(4, 8) && wide(4)) return forward_wide<float, 4, 4>(a, h0, out, h_last, ckpt, s);
     if (fits(2) && fills(2, 3) && wide(2)) return forward_wide<float, 2, kSeg>(a, h0, out, h_last, ckpt, s);
     if (wide(1)) return forward_wide<float, 1, kSeg>(a, h0, out, h_last, ckpt, s);
-    return forward_long<float, 1, 2 * kSeg>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
+    const Split p = split_of(a->T, a->N, a->D, 1);
+    return rows ? forward_long<float, 1, 2 * kSeg, 2>(a, p, h0, out, h_last, ckpt, s)
+                : forward_long<float, 1, 2 * kSeg, 0>(a, p, h0, out, h_last, ckpt, s);
   }
   if (fits(4) && fills(4, 8) && wide(4)) return forward_wide<__nv_bfloat16, 4, 4>(a, h0, out, h_last, ckpt, s);
   if (fits(2)) {
     if (wide(2)) return forward_wide<__nv_bfloat16, 2, kSeg>(a, h0, out, h_last, ckpt, s);
-    return forward_long<__nv_bfloat16, 2, kSeg>(a, split_of(a->T, a->N, a->D, 2), h0, out, h_last, ckpt, s);
+    const Split p = split_of(a->T, a->N, a->D, 2);
+    return rows ? forward_long<__nv_bfloat16, 2, kSeg, 3>(a, p, h0, out, h_last, ckpt, s)
+                : forward_long<__nv_bfloat16, 2, kSeg, 0>(a, p, h0, out, h_last, ckpt, s);
   }
   if (wide(1)) return forward_wide<__nv_bfloat16, 1, kSeg>(a, h0, out, h_last, ckpt, s);
-  return forward_long<__nv_bfloat16, 1, 2 * kSeg>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
+  return forward_long<__nv_bfloat16, 1, 2 * kSeg, 0>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
 }
 
 aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_seq* dh, const float* dh_last,
@@ -793,15 +919,21 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
                   di ? seq(*di) : none, dh0, part};
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const int esz = a->dtype == AHT_FP32 ? 4 : 2;
-  bool two = a->D % 2 == 0;
-  for (const Seq& q : {seq(a->x), seq(a->r), seq(a->i), g.dh, g.dx, g.dr, g.di})
-    two = two && aligned(q, esz, 2, a->T, a->N);
+  auto fits = [&](int V) {
+    bool ok = a->D % V == 0;
+    for (const Seq& q : {seq(a->x), seq(a->r), seq(a->i), g.dh, g.dx, g.dr, g.di}) ok = ok && aligned(q, esz, V, a->T, a->N);
+    return ok;
+  };
+  // every row a whole number of aligned 16-byte chunks (and the checkpoints' rows)
+  const bool rows_16 = fits(16 / esz) && (uintptr_t)ckpt % 16 == 0;
   int segs = 1;
   aht_status e;
   if (a->dtype == AHT_FP32)
-    e = backward<float, 1>(a, g, &segs, s);
+    e = rows_16 ? backward<float, 1, true>(a, g, &segs, s) : backward<float, 1, false>(a, g, &segs, s);
+  else if (fits(2))
+    e = rows_16 ? backward<__nv_bfloat16, 2, true>(a, g, &segs, s) : backward<__nv_bfloat16, 2, false>(a, g, &segs, s);
   else
-    e = two ? backward<__nv_bfloat16, 2>(a, g, &segs, s) : backward<__nv_bfloat16, 1>(a, g, &segs, s);
+    e = backward<__nv_bfloat16, 1, false>(a, g, &segs, s);
   if (e != AHT_OK || !dlam) return e;
   const int64_t rows = (int64_t)segs * a->N;
   const dim3 grid((a->D + 31) / 32), block(32, 32);
