@@ -207,25 +207,53 @@ __device__ __forceinline__ uint8_t reset_byte(const GlrDev& a, const Place& at, 
 // The map that reaches segment (rank, wt) of a window, from the maps (A, H) that every
 // segment publishes, and the composition of the whole window.  Segments run in the order of
 // the scan (for the backward pass the caller numbers them from the end).
+//
+// Between CTAs the maps travel as asynchronous remote stores that count on the receiver's
+// mbarrier: a cluster barrier would have to release, that is wait for, every global store the
+// threads have in flight (a sixth of the stalls).  Two buffers suffice: a CTA sends for window
+// w + 2 after it has everyone's maps of w + 1, which each CTA sends after all its warps have
+// read w.
 template <int V, int WT, bool kCluster>
 struct Exchange {
   struct Shared {
-    float a[2][WT][32][V], h[2][WT][32][V];                       // maps of the CTA's warps
-    float ca[2][kMaxCluster][32][V], ch[2][kMaxCluster][32][V];   // maps of the cluster's CTAs
+    float a[2][WT][32][V], h[2][WT][32][V];   // maps of the CTA's warps
+    alignas(16) float c[2][kMaxCluster][32][2 * V];  // maps of the cluster's CTAs: A, then H
+    alignas(8) uint64_t bar[2];
   };
+  __device__ __forceinline__ static void init(Shared& sh) {
+    if (!kCluster) return;
+    if (threadIdx.x == 0) {
+      tc::mbar_init(&sh.bar[0], 1);
+      tc::mbar_init(&sh.bar[1], 1);
+      tc::mbar_init_fence();
+    }
+    cg::this_cluster().sync();
+  }
+  // No CTA leaves while another may send to it.
+  __device__ __forceinline__ static void finish() {
+    if (kCluster) cg::this_cluster().sync();
+  }
+  __device__ __forceinline__ static void send(const float* to, const float* v, const uint64_t* bar, int dst) {
+    uint32_t at, mb;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(to)), "r"(dst));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(mb) : "r"(tc::smem_u32(bar)), "r"(dst));
+    if (V == 1)
+      asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(at),
+                   "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(mb)
+                   : "memory");
+    else
+      asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                       at),
+                   "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[V])),
+                   "r"(__float_as_uint(v[2 * V - 1])), "r"(mb)
+                   : "memory");
+  }
   // carry: the state before the window, in; after the window, out.  in: the state before
-  // this segment.
-  __device__ __forceinline__ static void run(Shared& sh, int buf, int rank, int n_rank, int wt, int lane,
+  // this segment.  n: windows before this one.
+  __device__ __forceinline__ static void run(Shared& sh, uint32_t n, int rank, int n_rank, int wt, int lane,
                                              const float (&A)[V], const float (&H)[V], float (&carry)[V],
                                              float (&in)[V]) {
-    if (WT == 1 && !kCluster) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        in[v] = carry[v];
-        carry[v] = apply(A[v], carry[v], H[v]);
-      }
-      return;
-    }
+    const int buf = (int)(n & 1u);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       sh.a[buf][wt][lane][v] = A[v];
@@ -245,7 +273,7 @@ struct Exchange {
       pa[v] = 1.0f;
       ph[v] = 0.0f;
     }
-    auto then = [&](float (&ca)[V], float (&ch)[V], int w) {
+    auto then = [&](float* ca, float* ch, int w) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         ch[v] = apply(wa[w][v], ch[v], wh[w][v]);
@@ -256,34 +284,31 @@ struct Exchange {
     for (int w = 0; w < WT; ++w)
       if (w < wt) then(pa, ph, w);
     if (kCluster) {
-      cg::cluster_group cl = cg::this_cluster();
       if (wt == WT - 1) {  // the last warp has the CTA's map: to every CTA of the cluster
-        float ta[V], th[V];
+        float t[2 * V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          ta[v] = pa[v];
-          th[v] = ph[v];
+          t[v] = pa[v];
+          t[V + v] = ph[v];
         }
-        then(ta, th, WT - 1);
-        for (int dst = 0; dst < n_rank; ++dst) {
-          float* ra = cl.map_shared_rank(&sh.ca[buf][rank][lane][0], dst);
-          float* rh = cl.map_shared_rank(&sh.ch[buf][rank][lane][0], dst);
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            ra[v] = ta[v];
-            rh[v] = th[v];
-          }
-        }
+        then(t, t + V, WT - 1);
+        if (lane == 0) tc::mbar_expect_tx(&sh.bar[buf], (uint32_t)n_rank * 32u * 2u * V * 4u);
+        for (int dst = 0; dst < n_rank; ++dst) send(&sh.c[buf][rank][lane][0], t, &sh.bar[buf], dst);
       }
-      cl.sync();
+      // bounded; a window whose maps did not arrive makes everything after it NaN
+      const bool got = tc::mbar_wait(&sh.bar[buf], (n >> 1) & 1u);
 #pragma unroll
       for (int v = 0; v < V; ++v) in[v] = carry[v];
       for (int c = 0; c < n_rank; ++c)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           if (c == rank) in[v] = carry[v];
-          carry[v] = apply(sh.ca[buf][c][lane][v], carry[v], sh.ch[buf][c][lane][v]);
+          carry[v] = apply(sh.c[buf][c][lane][v], carry[v], sh.c[buf][c][lane][V + v]);
         }
+      if (!got) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) in[v] = carry[v] = __int_as_float(0x7FC00000);
+      }
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) in[v] = carry[v];
@@ -317,6 +342,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   const int64_t lanes = a.N * a.D, me = at.n * a.D + at.d;
   const int seg = rank * WT + wt;
   const int64_t window = (int64_t)(kCluster ? n_rank : 1) * WT * S;
+  X::init(sh);
 
   float m[V], carry[V];  // m = -s
   bool small = true;
@@ -370,8 +396,8 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   } else {
     fetch((int64_t)seg * S);
   }
-  int buf = 0;
-  for (int64_t w0 = 0; w0 < a.T; w0 += window, buf ^= 1) {
+  uint32_t n = 0;  // windows so far
+  for (int64_t w0 = 0; w0 < a.T; w0 += window, ++n) {
     const int64_t t0 = w0 + (int64_t)seg * S;
     const uint32_t rs = __ballot_sync(0xFFFFFFFFu, nrs != 0);
     // a full segment without a reset needs no masks
@@ -441,7 +467,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
           A[e % V] = da[e] == 0.0f ? 0.0f : A[e % V] * da[e];
         }
       }
-      X::run(sh, buf, rank, n_rank, wt, lane, A, H, carry, y);
+      X::run(sh, n, rank, n_rank, wt, lane, A, H, carry, y);
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) y[v] = carry[v];
@@ -487,6 +513,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     }
   }
   if (kRing) R::template wait<0>();
+  X::finish();
   if (h_last && at.on && seg == 0) {
 #pragma unroll
     for (int v = 0; v < V; ++v) h_last[me + v] = carry[v];
@@ -517,6 +544,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   const int64_t lanes = a.N * a.D, me = at.n * a.D + at.d;
   const int n_seg = (kCluster ? n_rank : 1) * WT, seg = rank * WT + wt;  // seg 0: the latest steps
   const int64_t window = (int64_t)n_seg * S;
+  X::init(sh);
   const int64_t last = (a.T + window - 1) / window * window - (int64_t)(seg + 1) * S;  // its first t0
 
   float m[V], carry[V], sum[V], comp[V];
@@ -584,8 +612,8 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     for (int w = 0; w < kRing; ++w) fetch_ring(last - w * window, w);
     nrs = reset_byte<S>(a, at, last, lane);
   }
-  int buf = 0;
-  for (int64_t t0 = last, w = (a.T + window - 1) / window; w > 0; --w, t0 -= window, buf ^= 1) {
+  uint32_t n = 0;  // windows so far
+  for (int64_t t0 = last, w = (a.T + window - 1) / window; w > 0; --w, t0 -= window, ++n) {
     if (kRing) {
       R::template wait<(kRing > 0 ? kRing - 1 : 0)>();
       const uint8_t* src = ring + slot * R::kStage + lane * 4;
@@ -666,7 +694,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
           A[v] = cut ? 0.0f : A[v] * d;
         }
       }
-      X::run(sh, buf, rank, n_rank, wt, lane, A, P, carry, p);
+      X::run(sh, n, rank, n_rank, wt, lane, A, P, carry, p);
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) p[v] = carry[v];
@@ -719,6 +747,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     }
   }
   if (kRing) R::template wait<0>();
+  X::finish();
   if (!at.on) return;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
