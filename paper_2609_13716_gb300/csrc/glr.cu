@@ -2,9 +2,9 @@
 // the model): forward over T steps, one serving step (T = 1), and the backward pass.
 //
 // A lane is one channel d of one env n; its T steps are a chain, lanes are independent.  A
-// thread owns V neighbouring channels of one env (one 4- or 8-byte load per row) and a
-// segment of S consecutive steps; a warp's row is contiguous.  The loads of the next segment
-// are issued before the present one is computed, so the copies run during the arithmetic.
+// thread owns V neighbouring channels of one env and a segment of S consecutive steps; a
+// warp's row is contiguous.  The next segments are copied while the present one is computed:
+// through a ring in shared memory where rows are aligned, else one ahead in registers.
 //   - Many lanes: a warp walks its lanes' whole chain, segment after segment.
 //   - Few lanes: WT warps of a CTA, and CL CTAs of a cluster, take consecutive segments of
 //     the same lanes.  A segment is an affine map of the state it receives, h -> A h + H;
@@ -15,8 +15,8 @@
 // receives, p -> A p + P with the same A.
 //
 // State, gates and sums are fp32 whatever the tensors' type; each output is rounded once.
-// Where a map has A = 0 (a reset, or a decay that underflowed) it drops what it receives,
-// NaN and infinity included.
+// Where a segment's map has A = 0 (a reset in it, or a decay that underflowed) it drops what it
+// receives, NaN and infinity included.
 //
 // The backward pass needs the state before every step.  The forward pass leaves it as fp32
 // checkpoints every kSeg = 8 steps (0.5 B per element; the rounded h would cost 2-4 B and
@@ -81,6 +81,16 @@ struct Vec {
   }
   __device__ __forceinline__ float get(int v) const { return (float)e[v]; }
   __device__ __forceinline__ void set(int v, float f) { e[v] = (E)f; }
+  __device__ __forceinline__ void set2(int v, float f0, float f1) {  // v even
+    if constexpr (sizeof(E) == 2) {
+      const uint32_t both = tc::pack_bf16(f0, f1);
+      if constexpr (V == 2) w = both;
+      else if constexpr (V == 4) (v ? w.y : w.x) = both;
+    } else {
+      e[v] = f0;
+      e[v + 1] = f1;
+    }
+  }
 };
 
 __device__ __forceinline__ float softplus_f(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))); }
@@ -167,12 +177,14 @@ struct Walk {
   }
 };
 
-// A warp's ring of segments in shared memory, filled by asynchronous copies: a row is 128 bytes
-// (32 lanes of 4), copied by 8 lanes, 16 bytes each; what lies past the env's steps or its
-// channels is zero.  Rows start on 16-byte boundaries (checked by the host).
-template <int kTensors, int S, int kExtra>
+// A warp's ring of segments in shared memory, filled by asynchronous copies: a row is 32 lanes of
+// kLane bytes (2 or 4), copied 16 bytes a lane; what lies past the env's steps or its channels is
+// zero.  Rows start on 16-byte boundaries (checked by the host).
+template <int kTensors, int S, int kLane, int kExtra>
 struct Ring {
-  static constexpr int kStage = kTensors * S * 128 + kExtra;  // bytes of a segment
+  static constexpr int kRow = 32 * kLane, kChunks = kRow / 16, kPer = 32 / kChunks;  // rows an instruction copies
+  static constexpr int kStage = kTensors * S * kRow + kExtra;  // bytes of a segment
+  static_assert(S % kPer == 0, "whole instructions a segment");
   __device__ __forceinline__ static void copy16(void* dst, const void* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(dst)), "l"(src), "r"(on ? 16 : 0)
                  : "memory");
@@ -180,13 +192,13 @@ struct Ring {
   __device__ __forceinline__ static void rows(uint8_t* slot, int tensor, const Seq& s, const void* lane0, int esz,
                                               int64_t t0, int64_t left, int lane, bool chunk) {
     const int64_t step = s.st * esz;
-    const char* src = static_cast<const char*>(lane0) + (t0 + (lane >> 3)) * step + (lane & 7) * 16;
-    uint8_t* dst = slot + tensor * S * 128 + (lane >> 3) * 128 + (lane & 7) * 16;
+    const char* src = static_cast<const char*>(lane0) + (t0 + lane / kChunks) * step + (lane % kChunks) * 16;
+    uint8_t* dst = slot + tensor * S * kRow + lane * 16;
 #pragma unroll
-    for (int k = 0; k < S; k += 4) {
-      const bool on = chunk && k + (lane >> 3) < left;
-      copy16(dst + k * 128, on ? src : static_cast<const char*>(s.p), on);
-      src += 4 * step;
+    for (int k = 0; k < S; k += kPer) {
+      const bool on = chunk && k + lane / kChunks < left;
+      copy16(dst + k * kRow, on ? src : static_cast<const char*>(s.p), on);
+      src += kPer * step;
     }
   }
   __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -326,7 +338,7 @@ struct Exchange {
 // come through a ring of that many segments (rows of 4-byte lanes, aligned); 0: the next
 // segment waits in registers.
 template <typename E, int V, int S, int WT, int kWarps, bool kCluster, int kRing>
-__global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
+__global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 2 ? 5 : 16 / kWarps)
     glr_fwd(const __grid_constant__ GlrDev a, const float* h0, const __grid_constant__ Seq h, float* h_last,
             float* ckpt, int n_rank) {
   using X = Exchange<V, WT, kCluster>;
@@ -355,11 +367,10 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   small = __all_sync(0xFFFFFFFFu, small);
   Vec<E, V> nx[S], nr[S], ni[S];
   uint8_t nrs = 0;
-  using R = Ring<3, S, 0>;
-  static_assert(kRing == 0 || V * sizeof(E) == 4, "the ring's rows have 4 bytes a lane");
+  using R = Ring<3, kRing ? S : 8, kRing ? V * (int)sizeof(E) : 4, 0>;
   extern __shared__ __align__(128) uint8_t ring_smem[];
   uint8_t* ring = ring_smem + (kRing ? warp * kRing * R::kStage : 0);
-  const bool any = unit < a.N * tiles, chunk = any && at.d - lane * V + (lane & 7) * 4 * V < a.D;
+  const bool any = unit < a.N * tiles, chunk = any && at.d - lane * V + lane % R::kChunks * (16 / (int)sizeof(E)) < a.D;
   int slot = 0;
   const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
   const E* pr = static_cast<const E*>(a.r.p) + at.n * a.r.sn + at.d;
@@ -406,12 +417,12 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     float y[V];
     if (kRing) {
       R::template wait<(kRing > 0 ? kRing - 1 : 0)>();
-      const uint8_t* src = ring + slot * R::kStage + lane * 4;
+      const uint8_t* src = ring + slot * R::kStage + lane * V * (int)sizeof(E);
 #pragma unroll
       for (int k = 0; k < S; ++k) {
-        nr[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + k * 128);
-        ni[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (S + k) * 128);
-        nx[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (2 * S + k) * 128);
+        nr[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + k * R::kRow);
+        ni[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (S + k) * R::kRow);
+        nx[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (2 * S + k) * R::kRow);
       }
     }
     auto gate = [&](auto small_c) {
@@ -486,9 +497,12 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         if (k % kSeg == 0) save(k);
         Vec<E, V> o;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          y[v] = fmaf(da[k * V + v], y[v], b[k * V + v]);
-          o.set(v, y[v]);
+        for (int v = 0; v < V; ++v) y[v] = fmaf(da[k * V + v], y[v], b[k * V + v]);
+        if constexpr (V == 1) {
+          o.set(0, y[0]);
+        } else {
+#pragma unroll
+          for (int v = 0; v < V; v += 2) o.set2(v, y[v], y[v + 1]);
         }
         char* q = wh.next();
         if (h.p && at.on) o.store(q);
@@ -560,11 +574,10 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   Vec<E, V> nx[S], nr[S], ni[S], ng[S];
   float nc[V];
   uint8_t nrs = 0;
-  using R = Ring<4, S, 128 * V>;  // and the checkpoint
-  static_assert(kRing == 0 || V * sizeof(E) == 4, "the ring's rows have 4 bytes a lane");
+  using R = Ring<4, S, V * (int)sizeof(E), 128 * V>;  // and the checkpoint
   extern __shared__ __align__(128) uint8_t ring_smem[];
   uint8_t* ring = ring_smem + (kRing ? warp * kRing * R::kStage : 0);
-  const bool any = unit < a.N * tiles, chunk = any && at.d - lane * V + (lane & 7) * 4 * V < a.D;
+  const bool any = unit < a.N * tiles, chunk = any && at.d - lane * V + lane % R::kChunks * (16 / (int)sizeof(E)) < a.D;
   int slot = 0;
   const E* px = static_cast<const E*>(a.x.p) + at.n * a.x.sn + at.d;
   const E* pr = static_cast<const E*>(a.r.p) + at.n * a.r.sn + at.d;
@@ -584,7 +597,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     const int64_t d4 = at.d - lane * V + 4 * lane;
     const bool on = any && lane < 8 * V && d4 < a.D && left > 0;
     if (lane < 8 * V)
-      R::copy16(dst + 4 * S * 128 + lane * 16, on ? b.ckpt + (t0 / kSeg) * lanes + at.n * a.D + d4 : b.ckpt, on);
+      R::copy16(dst + 4 * S * R::kRow + lane * 16, on ? b.ckpt + (t0 / kSeg) * lanes + at.n * a.D + d4 : b.ckpt, on);
     R::commit();
   };
   auto fetch = [&](int64_t t0) {
@@ -614,33 +627,45 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
   }
   uint32_t n = 0;  // windows so far
   for (int64_t t0 = last, w = (a.T + window - 1) / window; w > 0; --w, t0 -= window, ++n) {
+    // Ring: one channel a thread has room for the whole segment, and the slot is refilled as soon
+    // as it is read; two read x and dh from the slot where they are used, and refill it last.
+    const uint8_t* src = ring + slot * R::kStage + lane * V * (int)sizeof(E);
+    using W = typename Vec<E, V>::W;
     if (kRing) {
       R::template wait<(kRing > 0 ? kRing - 1 : 0)>();
-      const uint8_t* src = ring + slot * R::kStage + lane * 4;
 #pragma unroll
       for (int k = 0; k < S; ++k) {
-        nr[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + k * 128);
-        ni[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (S + k) * 128);
-        nx[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (2 * S + k) * 128);
-        ng[k].w = *reinterpret_cast<const typename Vec<E, V>::W*>(src + (3 * S + k) * 128);
-        if (!b.dh.p) ng[k].zero();
+        nr[k].w = *reinterpret_cast<const W*>(src + k * R::kRow);
+        ni[k].w = *reinterpret_cast<const W*>(src + (S + k) * R::kRow);
+        if (V == 1) {
+          nx[k].w = *reinterpret_cast<const W*>(src + (2 * S + k) * R::kRow);
+          ng[k].w = *reinterpret_cast<const W*>(src + (3 * S + k) * R::kRow);
+          if (!b.dh.p) ng[k].zero();
+        }
       }
 #pragma unroll
-      for (int v = 0; v < V; ++v) nc[v] = reinterpret_cast<const float*>(ring + slot * R::kStage + 4 * S * 128)[lane * V + v];
+      for (int v = 0; v < V; ++v) nc[v] = reinterpret_cast<const float*>(ring + slot * R::kStage + 4 * S * R::kRow)[lane * V + v];
     } else {
       fetch(t0);
     }
+    auto x_of = [&](int k) {
+      if (!kRing || V == 1) return nx[k];
+      Vec<E, V> q;
+      q.w = *reinterpret_cast<const W*>(src + (2 * S + k) * R::kRow);
+      return q;
+    };
+    auto g_of = [&](int k) {
+      if (!kRing || V == 1) return ng[k];
+      Vec<E, V> q;
+      q.w = *reinterpret_cast<const W*>(src + (3 * S + k) * R::kRow);
+      if (!b.dh.p) q.zero();
+      return q;
+    };
     float em[kE], rho[kE], iota[kE], prev[kE], p[V];
-    Vec<E, V> x[S], g[S];
     const uint32_t rs = __ballot_sync(0xFFFFFFFFu, nrs != 0);
     const bool plain = rs == 0 && t0 + S <= at.len;  // no masks needed
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = nc[v];
-#pragma unroll
-    for (int k = 0; k < S; ++k) {
-      x[k] = nx[k];
-      g[k] = ng[k];
-    }
     // gates; prev holds beta iota x until the states are rebuilt
     auto gate = [&](auto small_c) {
 #pragma unroll
@@ -651,7 +676,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         const uint64_t io = sigmoid2(tc::f2_pack(ni[k0].get(v0), ni[k1].get(v1)));
         float b0, b1;
         tc::f2_unpack(beta_sq(z), b0, b1);
-        const uint64_t ix = tc::f2_mul(io, tc::f2_pack(x[k0].get(v0), x[k1].get(v1)));
+        const uint64_t ix = tc::f2_mul(io, tc::f2_pack(x_of(k0).get(v0), x_of(k1).get(v1)));
         tc::f2_unpack(tc::f2_mul(tc::f2_pack(sqrt_q(b0), sqrt_q(b1)), ix), prev[e], prev[e + 1]);
         tc::f2_unpack(rh, rho[e], rho[e + 1]);
         tc::f2_unpack(io, iota[e], iota[e + 1]);
@@ -660,11 +685,14 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     };
     if (small) gate(std::true_type());
     else gate(std::false_type());
-    if (kRing) {
+    auto refill = [&]() {
       __syncwarp();                       // every lane has read the slot
       fetch_ring(t0 - kRing * window, slot);
       slot = slot + 1 == kRing ? 0 : slot + 1;
+    };
+    if (kRing) {
       nrs = w > 1 ? reset_byte<S>(a, at, t0 - window, lane) : (uint8_t)0;
+      if (V == 1) refill();
     }
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
@@ -686,11 +714,11 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         const int k = e / V, v = e % V;
         const float d = 1.0f + em[e];
         if (plain) {
-          P[v] = d * (g[k].get(v) + P[v]);
+          P[v] = d * (g_of(k).get(v) + P[v]);
           A[v] *= d;
         } else if (t0 + k < at.len) {
           const bool cut = (rs >> k) & 1u;
-          P[v] = cut ? 0.0f : d * (g[k].get(v) + P[v]);
+          P[v] = cut ? 0.0f : d * (g_of(k).get(v) + P[v]);
           A[v] = cut ? 0.0f : A[v] * d;
         }
       }
@@ -706,30 +734,65 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     auto grads = [&](auto plain_c) {
       constexpr bool kPlain = decltype(plain_c)::value;
 #pragma unroll
-      for (int k = S - 1; k >= 0; --k) {
-        const bool live = kPlain || t0 + k < at.len, cut = !kPlain && ((rs >> k) & 1u);
+      for (int e = kE - 2; e >= 0; e -= 2) {
+        const int k0 = e / V, v0 = e % V, k1 = (e + 1) / V, v1 = (e + 1) % V;
+        // With G = dL/dh: dx = c1 G, di = c2 dx, w = -q a dL/da = c3 G, dr = c4 w, all but G
+        // known before the scan.  1 / beta stays finite where beta = 0 (dx is 0 there, and
+        // q / beta -> 0 with q).
+        const uint64_t z = tc::f2_pack(em[e], em[e + 1]), rh = tc::f2_pack(rho[e], rho[e + 1]);
+        const uint64_t io = tc::f2_pack(iota[e], iota[e + 1]), xx = tc::f2_pack(x_of(k0).get(v0), x_of(k1).get(v1));
+        const uint64_t d = tc::f2_add(z, both(1.0f)), b2 = beta_sq(z);
+        float s0, s1, d0, d1;
+        tc::f2_unpack(b2, s0, s1);
+        const uint64_t inv = tc::f2_pack(rsqrt_q(fmaxf(s0, 1e-37f)), rsqrt_q(fmaxf(s1, 1e-37f)));
+        const uint64_t c1 = tc::f2_mul(io, tc::f2_mul(b2, inv)), c2 = tc::f2_mul(xx, tc::f2_fma(io, both(-1.0f), both(1.0f)));
+        const uint64_t nq = tc::f2_mul(tc::f2_pack(m[v0], m[v1]), rh);  // -q
+        const uint64_t c3 = tc::f2_mul(tc::f2_mul(d, nq),
+                                       tc::f2_sub(tc::f2_pack(prev[e], prev[e + 1]), tc::f2_mul(tc::f2_mul(inv, d), tc::f2_mul(io, xx))));
+        const uint64_t c4 = tc::f2_fma(rh, both(-1.0f), both(1.0f));
+        tc::f2_unpack(d, d0, d1);
+        const bool live0 = kPlain || t0 + k0 < at.len, live1 = kPlain || t0 + k1 < at.len;
+        const bool cut0 = !kPlain && ((rs >> k0) & 1u), cut1 = !kPlain && ((rs >> k1) & 1u);
+        // the scan: element e + 1 is a later step (V = 1) or another channel
+        const float G1 = g_of(k1).get(v1) + p[v1];
+        p[v1] = live1 ? (cut1 ? 0.0f : d1 * G1) : p[v1];
+        const float G0 = g_of(k0).get(v0) + p[v0];
+        p[v0] = live0 ? (cut0 ? 0.0f : d0 * G0) : p[v0];
+        const uint64_t G = tc::f2_pack(G0, G1), dx = tc::f2_mul(G, c1), w = tc::f2_mul(G, c3);
+        float a0, a1, b0, b1, e0, e1, w0, w1;
+        tc::f2_unpack(dx, a0, a1);
+        tc::f2_unpack(tc::f2_mul(w, c4), b0, b1);
+        tc::f2_unpack(tc::f2_mul(dx, c2), e0, e1);
+        tc::f2_unpack(w, w0, w1);
+        if (!kPlain) {
+          if (!live0) a0 = b0 = e0 = w0 = 0.0f;
+          if (!live1) a1 = b1 = e1 = w1 = 0.0f;
+        }
+        part[v1] += w1;
+        part[v0] += w0;
         Vec<E, V> ox, orr, oi;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const int e = k * V + v;
-          const float xx = x[k].get(v), io = iota[e], z = em[e], d = 1.0f + z;
-          const float G = g[k].get(v) + p[v];
-          const float b2 = z * (-2.0f - z), nq = m[v] * rho[e];     // nq = -q
-          // 1 / beta, finite where beta = 0: dx is 0 there, and q / beta -> 0 with q
-          const float inv = rsqrt_q(fmaxf(b2, 1e-37f));
-          const float u = G * io;                                   // dL/d(beta x)
-          const float dx = u * (b2 * inv);
-          // w = -q a dL/da = a (-q G prev + (q / beta) a u x)
-          const float wv = d * (nq * (G * prev[e] - (inv * d) * (u * xx)));
-          const float dr = wv - rho[e] * wv, di = (dx * xx) * (1.0f - io);
-          ox.set(v, live ? dx : 0.0f);
-          oi.set(v, live ? di : 0.0f);
-          orr.set(v, live ? dr : 0.0f);
-          part[v] += live ? wv : 0.0f;
-          p[v] = live ? (cut ? 0.0f : d * G) : p[v];
+        if constexpr (V == 1) {
+          Vec<E, V> px1, pr1, pi1;
+          px1.set(0, a1);
+          pr1.set(0, b1);
+          pi1.set(0, e1);
+          char *qx = wdx.next_back(), *qr = wdr.next_back(), *qi = wdi.next_back();
+          if (at.on && (kPlain || t0 + k1 < a.T)) {
+            px1.store(qx);
+            pr1.store(qr);
+            pi1.store(qi);
+          }
+          ox.set(0, a0);
+          orr.set(0, b0);
+          oi.set(0, e0);
+        } else {
+          static_assert(V <= 2, "a pair is a row");
+          ox.set2(v0, a0, a1);
+          orr.set2(v0, b0, b1);
+          oi.set2(v0, e0, e1);
         }
         char *qx = wdx.next_back(), *qr = wdr.next_back(), *qi = wdi.next_back();
-        if (at.on && (kPlain || t0 + k < a.T)) {
+        if (at.on && (kPlain || t0 + k0 < a.T)) {
           ox.store(qx);
           orr.store(qr);
           oi.store(qi);
@@ -738,6 +801,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     };
     if (plain) grads(std::true_type());
     else grads(std::false_type());
+    if (kRing && V > 1) refill();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const float yk = part[v] - comp[v], sk = sum[v] + yk;  // compensated over the segments
@@ -823,7 +887,9 @@ struct Split {
   int segs() const { return wt * cl; }
 };
 
-constexpr int kFill = 152 * 12;  // warps that keep every SM's loads in flight
+// Warps that keep every SM's loads in flight: with fewer groups than this the steps are split
+// (1000 x 300 x 256 bf16, 1200 groups: split 146 us forward and 228 backward, whole 180 and 317).
+constexpr int kFill = 152 * 12;
 
 Split split_of(int64_t T, int64_t N, int32_t D, int V) {
   Split p{1, 1, N * ((D + 32 * V - 1) / (32 * V))};
@@ -851,18 +917,18 @@ aht_status launch(K kernel, int64_t blocks, int threads, int cl, int smem, cudaS
 }
 
 // Many lanes (or T = 1): a warp per group of 32 V lanes.
-template <typename E, int V, int S>
+template <typename E, int V, int S, int kRing>
 aht_status forward_wide(const aht_glr_args* a, const float* h0, const Seq& h, float* h_last, float* ckpt, cudaStream_t s) {
   const int64_t four = (split_of(a->T, a->N, a->D, V).units + 3) / 4;
-  constexpr int kShort = V > 1 ? 1 : 2;  // steps of a segment when T = 1 (elements go in pairs)
-  if (a->T <= 1) return launch(glr_fwd<E, V, kShort, 1, 4, false, 0>, four, 128, 1, 0, s, dev(a), h0, h, h_last, ckpt, 1);
-  return launch(glr_fwd<E, V, S, 1, 4, false, 0>, four, 128, 1, 0, s, dev(a), h0, h, h_last, ckpt, 1);
+  constexpr int kSmem = 4 * kRing * Ring<3, 8, V * (int)sizeof(E), 0>::kStage;
+  static_assert(kRing == 0 || S == 8, "");
+  return launch(glr_fwd<E, V, S, 1, 4, false, kRing>, four, 128, 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
 }
 // Few lanes: 8 warps and p.cl CTAs along time.
 template <typename E, int V, int S, int kRing>
 aht_status forward_long(const aht_glr_args* a, const Split& p, const float* h0, const Seq& h, float* h_last, float* ckpt,
                         cudaStream_t s) {
-  constexpr int kSmem = 8 * kRing * Ring<3, S, 0>::kStage;
+  constexpr int kSmem = 8 * kRing * Ring<3, S, V * (int)sizeof(E), 0>::kStage;
   if (p.cl == 1)
     return launch(glr_fwd<E, V, S, 8, 8, false, kRing>, p.units, 256, 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
   return launch(glr_fwd<E, V, S, 8, 8, true, kRing>, p.units, 256, p.cl, kSmem, s, dev(a), h0, h, h_last, ckpt, p.cl);
@@ -873,11 +939,14 @@ aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStre
   const Split p = split_of(a->T, a->N, a->D, V);
   const GlrDev d = dev(a);
   *rows = p.segs();
-  constexpr int kStage = Ring<4, kSeg, 128 * V>::kStage, kWide = kRows && V == 1 ? 2 : 0, kLong = kRows ? (V == 1 ? 3 : 2) : 0;
-  if (p.wt == 1)
+  constexpr int kStage = Ring<4, kSeg, V * (int)sizeof(E), 128 * V>::kStage, kWide = kRows ? 2 : 0, kLong = kRows ? 3 : 0;
+  if (V > 1 || p.wt == 1)
     return launch(glr_bwd<E, V, 1, 4, false, kWide>, (p.units + 3) / 4, 128, 1, 4 * kWide * kStage, s, d, g, 1);
-  if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kLong>, p.units, 256, 1, 8 * kLong * kStage, s, d, g, 1);
-  return launch(glr_bwd<E, V, 8, 8, true, kLong>, p.units, 256, p.cl, 8 * kLong * kStage, s, d, g, p.cl);
+  if constexpr (V == 1) {
+    if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kLong>, p.units, 256, 1, 8 * kLong * kStage, s, d, g, 1);
+    return launch(glr_bwd<E, V, 8, 8, true, kLong>, p.units, 256, p.cl, 8 * kLong * kStage, s, d, g, p.cl);
+  }
+  return AHT_EINVAL;  // (V > 1 is wide)
 }
 
 constexpr int kSumRows = 64;  // row groups of the first pass of dlam's sum
@@ -913,23 +982,35 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
   // groups of 32 V channels that leave at most one thread in `of` without channels
   auto fills = [&](int V, int of) { return (a->D + 32 * V - 1) / (32 * V) * 32 * V <= a->D + a->D / of; };
   const bool rows = fits(16 / esz);      // every row a whole number of aligned 16-byte chunks
-  auto wide = [&](int V) { return a->T <= 1 || split_of(a->T, a->N, a->D, V).wt == 1; };
+  auto wide = [&](int V) { return split_of(a->T, a->N, a->D, V).wt == 1; };
+  // Wide passes, us for 128 steps (fp32 8192 x 128, bf16 16384 x 128; copies alone take 317): two
+  // channels a thread through the ring 307 / 362, two in registers 332 / 399, four in
+  // registers 333 / 394.  The ring wants aligned rows, two channels a well-filled warp.
   if (a->dtype == AHT_FP32) {
-    if (fits(4) && fills(4, 8) && wide(4)) return forward_wide<float, 4, 4>(a, h0, out, h_last, ckpt, s);
-    if (fits(2) && fills(2, 3) && wide(2)) return forward_wide<float, 2, kSeg>(a, h0, out, h_last, ckpt, s);
-    if (wide(1)) return forward_wide<float, 1, kSeg>(a, h0, out, h_last, ckpt, s);
+    if (a->T <= 1)
+      return fits(4) ? forward_wide<float, 4, 1, 0>(a, h0, out, h_last, ckpt, s)
+                     : forward_wide<float, 1, 2, 0>(a, h0, out, h_last, ckpt, s);
+    if (fits(2) && fills(2, 3) && wide(2))
+      return rows ? forward_wide<float, 2, kSeg, 2>(a, h0, out, h_last, ckpt, s)
+                  : forward_wide<float, 2, kSeg, 0>(a, h0, out, h_last, ckpt, s);
+    if (wide(1)) return forward_wide<float, 1, kSeg, 0>(a, h0, out, h_last, ckpt, s);
     const Split p = split_of(a->T, a->N, a->D, 1);
     return rows ? forward_long<float, 1, 2 * kSeg, 2>(a, p, h0, out, h_last, ckpt, s)
                 : forward_long<float, 1, 2 * kSeg, 0>(a, p, h0, out, h_last, ckpt, s);
   }
-  if (fits(4) && fills(4, 8) && wide(4)) return forward_wide<__nv_bfloat16, 4, 4>(a, h0, out, h_last, ckpt, s);
+  if (a->T <= 1)
+    return fits(4)   ? forward_wide<__nv_bfloat16, 4, 1, 0>(a, h0, out, h_last, ckpt, s)
+           : fits(2) ? forward_wide<__nv_bfloat16, 2, 1, 0>(a, h0, out, h_last, ckpt, s)
+                     : forward_wide<__nv_bfloat16, 1, 2, 0>(a, h0, out, h_last, ckpt, s);
   if (fits(2)) {
-    if (wide(2)) return forward_wide<__nv_bfloat16, 2, kSeg>(a, h0, out, h_last, ckpt, s);
+    if (wide(2))
+      return rows ? forward_wide<__nv_bfloat16, 2, kSeg, 2>(a, h0, out, h_last, ckpt, s)
+                  : forward_wide<__nv_bfloat16, 2, kSeg, 0>(a, h0, out, h_last, ckpt, s);
     const Split p = split_of(a->T, a->N, a->D, 2);
     return rows ? forward_long<__nv_bfloat16, 2, kSeg, 3>(a, p, h0, out, h_last, ckpt, s)
                 : forward_long<__nv_bfloat16, 2, kSeg, 0>(a, p, h0, out, h_last, ckpt, s);
   }
-  if (wide(1)) return forward_wide<__nv_bfloat16, 1, kSeg>(a, h0, out, h_last, ckpt, s);
+  if (wide(1)) return forward_wide<__nv_bfloat16, 1, kSeg, 0>(a, h0, out, h_last, ckpt, s);
   return forward_long<__nv_bfloat16, 1, 2 * kSeg, 0>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
 }
 
@@ -959,10 +1040,12 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
   aht_status e;
   if (a->dtype == AHT_FP32)
     e = rows_16 ? backward<float, 1, true>(a, g, &segs, s) : backward<float, 1, false>(a, g, &segs, s);
-  else if (fits(2))
+  // Wide bf16 passes of 128 x 16384 x 128: two channels a thread 689 us, one 892; split ones of
+  // 1000 x 300 x 256: two channels (their state spilled) 571 us, one 228.
+  else if (fits(2) && split_of(a->T, a->N, a->D, 2).wt == 1)
     e = rows_16 ? backward<__nv_bfloat16, 2, true>(a, g, &segs, s) : backward<__nv_bfloat16, 2, false>(a, g, &segs, s);
   else
-    e = backward<__nv_bfloat16, 1, false>(a, g, &segs, s);
+    e = rows_16 ? backward<__nv_bfloat16, 1, true>(a, g, &segs, s) : backward<__nv_bfloat16, 1, false>(a, g, &segs, s);
   if (e != AHT_OK || !dlam) return e;
   const int64_t rows = (int64_t)segs * a->N;
   const dim3 grid((a->D + 31) / 32), block(32, 32);
