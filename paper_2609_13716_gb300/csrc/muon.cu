@@ -342,60 +342,89 @@ __device__ __forceinline__ void commit_pair(uint64_t* mbar) {
       : "memory");
 }
 
-// 64 columns j0.. of row i of the orthogonal factor (the accumulated product f, unscaled) into
-// the caller's matrix: the weight update, or the factor itself.
-__device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int k, const Mat& m, int i, int j0,
-                                             const float (&f)[64]) {
-  if (i >= m.m) return;
+// A 32 x 32 block held as a row a lane (v[e]: column e) becomes a column a lane (v[e]: row e).
+__device__ __forceinline__ void transpose32(float* v, int lane) {
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1)
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      if (e & s) continue;
+      const bool up = lane & s;
+      const float got = __shfl_xor_sync(0xFFFFFFFFu, up ? v[e] : v[e + s], s);
+      if (up) v[e] = got;
+      else v[e + s] = got;
+    }
+}
+
+// 64 columns j0.. of 32 rows i0.. of the orthogonal factor, a row a lane (the accumulated
+// product f, unscaled), into the caller's matrix: the weight update, or the factor itself.  A wide
+// fp32 matrix whose rows allow it takes groups of four columns; a tall one is stored transposed,
+// so its lanes write neighbours; any other wide one is turned first (a block of 130 x 777 bf16
+// 3 us, a lane writing its row 9; turned fp32 rows 1 us a tile more than groups of four).
+// Sixteen elements at a time: their loads are in flight together.
+__device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int k, const Mat& m, int i0, int lane, int j0,
+                                             float (&f)[64]) {
   const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
-  const int64_t ld = p.ld_out[k], step = m.tall ? ld : 1;
-  const int64_t at0 = m.tall ? (int64_t)j0 * ld + i : (int64_t)i * ld + j0;
+  const int64_t ld = p.ld_out[k];
   void* out = p.out[k];
-  // rows of whole, aligned groups of four
-  const bool four = !m.tall && j0 + 64 <= m.n && !c.bf16_out && ((uintptr_t)out & 15) == 0 && (ld & 3) == 0;
-  // sixteen columns at a time: their loads are in flight together
+  if (!m.tall && j0 + 64 <= m.n && !c.bf16_out && ((uintptr_t)out & 15) == 0 && (ld & 3) == 0) {
+    if (i0 + lane >= m.m) return;
+    float4* w = reinterpret_cast<float4*>(static_cast<float*>(out) + (int64_t)(i0 + lane) * ld + j0);
 #pragma unroll
-  for (int b = 0; b < 64; b += 16) {
-    float o[16];
+    for (int b = 0; b < 16; b += 4) {
+      float4 o[4], old[4];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[e] = f[b + e] * (kUp / (kSB * kSX));
-    if (four) {
-      float4* w = reinterpret_cast<float4*>(static_cast<float*>(out) + at0 + b);
-      float4 old[4];
-      if (c.update) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) old[q] = w[q];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          o[4 * q] = fmaf(-lr, o[4 * q], c.decay * old[q].x);
-          o[4 * q + 1] = fmaf(-lr, o[4 * q + 1], c.decay * old[q].y);
-          o[4 * q + 2] = fmaf(-lr, o[4 * q + 2], c.decay * old[q].z);
-          o[4 * q + 3] = fmaf(-lr, o[4 * q + 3], c.decay * old[q].w);
-        }
+      for (int e = 0; e < 4; ++e) {
+        const float* v = f + 4 * (b + e);
+        constexpr float s = kUp / (kSB * kSX);
+        o[e] = make_float4(v[0] * s, v[1] * s, v[2] * s, v[3] * s);
+        if (c.update) old[e] = w[b + e];
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) w[q] = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-      continue;
+      for (int e = 0; e < 4; ++e) {
+        if (c.update)
+          o[e] = make_float4(fmaf(-lr, o[e].x, c.decay * old[e].x), fmaf(-lr, o[e].y, c.decay * old[e].y),
+                             fmaf(-lr, o[e].z, c.decay * old[e].z), fmaf(-lr, o[e].w, c.decay * old[e].w));
+        w[b + e] = o[e];
+      }
     }
-    const int left = m.n - j0 - b;             // columns that exist
-    if (c.update) {
-      float* w = static_cast<float*>(out) + at0 + b * step;
-      float old[16];
+    return;
+  }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) old[e] = e < left ? w[e * step] : 0.0f;
+  for (int b = 0; b < 64; b += 32) {
+    if (!m.tall) transpose32(f + b, lane);
+    // element e of this lane: row i0 + e, column j0 + b + lane; tall: row i0 + lane, column j0 + b + e
+    const int lane_at = m.tall ? i0 + lane : j0 + b + lane, lane_end = m.tall ? m.m : m.n;
+    const int e_at = m.tall ? j0 + b : i0, e_end = m.tall ? m.n : m.m;
+    if (lane_at >= lane_end) continue;
+    // X (i, j) is element (j, i) of a tall matrix, (i, j) of a wide one: e runs over rows of the matrix
+    const int64_t at0 = (int64_t)e_at * ld + lane_at;
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (e < left) w[e * step] = fmaf(-lr, o[e], c.decay * old[e]);
-    } else if (c.bf16_out) {
-      __nv_bfloat16* w = static_cast<__nv_bfloat16*>(out) + at0 + b * step;
+    for (int h = 0; h < 32; h += 16) {
+      const int left = e_end - e_at - h;
+      const int64_t at = at0 + h * ld;
+      float o[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (e < left) w[e * step] = __float2bfloat16_rn(o[e]);
-    } else {
-      float* w = static_cast<float*>(out) + at0 + b * step;
+      for (int e = 0; e < 16; ++e) o[e] = f[b + h + e] * (kUp / (kSB * kSX));
+      if (c.update) {
+        float* w = static_cast<float*>(out) + at;
+        float old[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (e < left) w[e * step] = o[e];
+        for (int e = 0; e < 16; ++e) old[e] = e < left ? w[e * ld] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (e < left) w[e * ld] = fmaf(-lr, o[e], c.decay * old[e]);
+      } else if (c.bf16_out) {
+        __nv_bfloat16* w = static_cast<__nv_bfloat16*>(out) + at;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (e < left) w[e * ld] = __float2bfloat16_rn(o[e]);
+      } else {
+        float* w = static_cast<float*>(out) + at;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (e < left) w[e * ld] = o[e];
+      }
     }
   }
 }
@@ -480,6 +509,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       // lane 0: hi of A, 1: lo of A, 2: this CTA's half of B's hi, 3: of its lo
       const bool of_a = lane < 2, lo = lane & 1;
       uint8_t* dst0 = smem + (of_a ? lane * kHalf : 2 * kHalf + (lane - 2) * (kHalf / 2));
+      if (lane < 3)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &maps.cols : lane == 1 ? &maps.rows : &maps.quarter)
+                     : "memory");
       const uint32_t full0 = in_leader(&full_bar[0]);
       const int half0 = of_a ? 0 : 8 * rank;      // this CTA's half of B's rows
       bool ok = true;
@@ -489,11 +521,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         const int it = g / c.n_items;
         const int4 item = c.items[g - it * c.n_items];
         const Mat m = c.mats[item.x];
-        if (!(ok = ready(m, item.x, item.y, it))) break;
-        fence_proxy_global();
         const int I = min(2 * item.z + rank, m.mb - 1);  // (an odd last row is computed twice, stored once)
         const int K = item.y == kGram ? m.nb : m.mb;
         const Operand o = operand(item.y, m, it & 1, of_a, lo, I, item.w);
+        if (!(ok = ready(m, item.x, item.y, it))) break;
+        fence_proxy_global();
         for (int k = 0; ok && k < K; ++k) {
           const bool mn = o.mn(k);
           const int col0 = o.block(k) * 16 + (mn ? half0 : 0);
@@ -609,7 +641,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       const bool last = phase == kApply && it + 1 == c.steps;
       if (ok && mine && last) {
-        store_result(c, p, item.x, m, I * kB + r, J * kB + c_beg, f);
+        store_result(c, p, item.x, m, I * kB + 32 * q, lane, J * kB + c_beg, f);
       } else if (ok && mine) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
@@ -970,7 +1002,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   }
   if (nb == 2) cluster_wait();
   // the weights, along their rows like the gradient
-  if (on && tall && ok) store_result(c, p, k, m, r, j0, f);
+  if (on && tall && ok) store_result(c, p, k, m, 32 * (warp & 3), lane, j0, f);
   if (on && !tall) {
     scale(kUp / (kSB * kSX));
     stage(parts);
