@@ -6,7 +6,7 @@
 // warp's row is contiguous.  The next segments are copied while the present one is computed:
 // through a ring in shared memory where rows are aligned, else one ahead in registers.
 //   - Many lanes: a warp walks its lanes' whole chain, segment after segment.
-//   - Few lanes: WT warps of a CTA, and CL CTAs of a cluster, take consecutive segments of
+//   - Few lanes: WT warps of a CTA, and up to 16 CTAs of a cluster, take consecutive segments of
 //     the same lanes.  A segment is an affine map of the state it receives, h -> A h + H;
 //     the maps are composed over the warps in shared memory and over the CTAs in distributed
 //     shared memory, then every thread applies its own from the state that reaches it.  All
@@ -42,7 +42,7 @@ namespace {
 
 constexpr int kSeg = AHT_GLR_SEGMENT;  // steps between two checkpoints
 constexpr float kGateScale = 8.0f;     // s = 8 softplus(lam)
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;
 
 struct Seq {
   void* p;
@@ -890,12 +890,18 @@ struct Split {
 // Warps that keep every SM's loads in flight: with fewer groups than this the steps are split
 // (1000 x 300 x 256 bf16, 1200 groups: split 146 us forward and 228 backward, whole 180 and 317).
 constexpr int kFill = 152 * 12;
+// Clusters of n CTAs of a split pass that a GB300 holds at once, two CTAs an SM (as the occupancy
+// query answers).  The largest cluster at which every group's is resident is the quickest
+// (65537 x 1 x 896 fp32, 28 groups, forward: 8 CTAs 206 us, 9 183, 10 172; 20000 x 2 x 256, 16
+// groups: 8 66 us, 12 53, 16 in two waves 65).
+constexpr int kResident[kMaxCluster + 1] = {0, 304, 152, 97, 74, 58, 46, 38, 36, 30, 28, 23, 23, 19, 14, 14, 14};
 
 Split split_of(int64_t T, int64_t N, int32_t D, int V) {
   Split p{1, 1, N * ((D + 32 * V - 1) / (32 * V))};
   if (p.units >= kFill || T <= 2 * kSeg) return p;
   p.wt = 8;
-  while (p.cl < kMaxCluster && p.units * p.wt * p.cl < kFill && (int64_t)p.wt * p.cl * 2 * kSeg <= T) p.cl *= 2;
+  for (int cl = 2; cl <= kMaxCluster; ++cl)
+    if (p.units <= kResident[cl] && (int64_t)p.wt * cl * kSeg <= T) p.cl = cl;
   return p;
 }
 
@@ -903,6 +909,8 @@ template <typename K, typename... Args>
 aht_status launch(K kernel, int64_t blocks, int threads, int cl, int smem, cudaStream_t s, Args... args) {
   if (smem > 48 * 1024)
     if (aht_status e = launched(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem))) return e;
+  if (cl > 8)  // beyond what every device runs
+    if (aht_status e = launched(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1))) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(blocks * cl));
   cfg.blockDim = dim3((unsigned)threads);
