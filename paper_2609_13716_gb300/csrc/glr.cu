@@ -887,8 +887,8 @@ struct Split {
   int segs() const { return wt * cl; }
 };
 
-// Warps that keep every SM's loads in flight: with fewer groups than this the steps are split
-// (1000 x 300 x 256 bf16, 1200 groups: split 146 us forward and 228 backward, whole 180 and 317).
+// Warps that keep every SM's loads in flight.  A pass with fewer groups than a share of them has its
+// steps split, unless it is so short that the windows' hand-overs cost more than the loads gain.
 constexpr int kFill = 152 * 12;
 // Clusters of n CTAs of a split pass that a GB300 holds at once, two CTAs an SM (as the occupancy
 // query answers).  The largest cluster at which every group's is resident is the quickest
@@ -896,13 +896,26 @@ constexpr int kFill = 152 * 12;
 // groups: 8 66 us, 12 53, 16 in two waves 65).
 constexpr int kResident[kMaxCluster + 1] = {0, 304, 152, 97, 74, 58, 46, 38, 36, 30, 28, 23, 23, 19, 14, 14, 14};
 
-Split split_of(int64_t T, int64_t N, int32_t D, int V) {
+Split split_of(int64_t T, int64_t N, int32_t D, int V, int fill) {
   Split p{1, 1, N * ((D + 32 * V - 1) / (32 * V))};
-  if (p.units >= kFill || T <= 2 * kSeg) return p;
+  if (p.units >= fill || T <= 2 * kSeg) return p;
   p.wt = 8;
   for (int cl = 2; cl <= kMaxCluster; ++cl)
     if (p.units <= kResident[cl] && (int64_t)p.wt * cl * kSeg <= T) p.cl = cl;
   return p;
+}
+
+// Split / whole, us: fp32 100 x 57 x 256 (456 groups) 12 / 15, 100 x 114 x 256 17 / 15, 400 x 150 x 256
+// (1200) 61 / 64, 400 x 200 x 256 77 / 72, 1000 x 200 x 256 146 / 174; bf16, two channels, 300 x 300 x
+// 256 (1200) 56 / 52, 1000 x 300 x 256 144 / 152.
+Split split_fwd(int64_t T, int64_t N, int32_t D, int V) {
+  return split_of(T, N, D, V, (int)std::min<int64_t>(std::max<int64_t>(3 * T, kFill / 3), kFill));
+}
+// One channel a thread, split / whole, us: 100 x 57 x 256 (456 groups) fp32 21 / 20, bf16 22 / 20;
+// 400 x 76 x 256 59 / 54, 52 / 58; 1000 x 76 x 256 109 / 117, 97 / 140; 1000 x 150 x 256 199 / 169,
+// 174 / 163.  Two channels are for whole passes that one would not fill (see the dispatch).
+Split split_bwd(int64_t T, int64_t N, int32_t D, int V) {
+  return split_of(T, N, D, V, V > 1 ? kFill : (int)std::min<int64_t>(std::max<int64_t>(T, kFill / 4), kFill / 2));
 }
 
 template <typename K, typename... Args>
@@ -927,7 +940,7 @@ aht_status launch(K kernel, int64_t blocks, int threads, int cl, int smem, cudaS
 // Many lanes (or T = 1): a warp per group of 32 V lanes.
 template <typename E, int V, int S, int kRing>
 aht_status forward_wide(const aht_glr_args* a, const float* h0, const Seq& h, float* h_last, float* ckpt, cudaStream_t s) {
-  const int64_t four = (split_of(a->T, a->N, a->D, V).units + 3) / 4;
+  const int64_t four = (split_fwd(a->T, a->N, a->D, V).units + 3) / 4;
   constexpr int kSmem = 4 * kRing * Ring<3, 8, V * (int)sizeof(E), 0>::kStage;
   static_assert(kRing == 0 || S == 8, "");
   return launch(glr_fwd<E, V, S, 1, 4, false, kRing>, four, 128, 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
@@ -944,7 +957,7 @@ aht_status forward_long(const aht_glr_args* a, const Split& p, const float* h0, 
 
 template <typename E, int V, bool kRows>  // kRows: rows aligned for the ring
 aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStream_t s) {
-  const Split p = split_of(a->T, a->N, a->D, V);
+  const Split p = split_bwd(a->T, a->N, a->D, V);
   const GlrDev d = dev(a);
   *rows = p.segs();
   constexpr int kStage = Ring<4, kSeg, V * (int)sizeof(E), 128 * V>::kStage, kWide = kRows ? 2 : 0, kLong = kRows ? 3 : 0;
@@ -960,8 +973,7 @@ aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStre
 constexpr int kSumRows = 64;  // row groups of the first pass of dlam's sum
 
 int64_t part_floats(int64_t T, int64_t N, int32_t D) {
-  const int64_t s = std::max(split_of(T, N, D, 1).segs(), std::max(split_of(T, N, D, 2).segs(), split_of(T, N, D, 4).segs()));
-  return s * N * D;
+  return (int64_t)std::max(split_bwd(T, N, D, 1).segs(), split_bwd(T, N, D, 2).segs()) * N * D;
 }
 
 }  // namespace
@@ -990,7 +1002,7 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
   // groups of 32 V channels that leave at most one thread in `of` without channels
   auto fills = [&](int V, int of) { return (a->D + 32 * V - 1) / (32 * V) * 32 * V <= a->D + a->D / of; };
   const bool rows = fits(16 / esz);      // every row a whole number of aligned 16-byte chunks
-  auto wide = [&](int V) { return split_of(a->T, a->N, a->D, V).wt == 1; };
+  auto wide = [&](int V) { return split_fwd(a->T, a->N, a->D, V).wt == 1; };
   // Wide passes, us for 128 steps (fp32 8192 x 128, bf16 16384 x 128; copies alone take 317): two
   // channels a thread through the ring 307 / 362, two in registers 332 / 399, four in
   // registers 333 / 394.  The ring wants aligned rows, two channels a well-filled warp.
@@ -1002,7 +1014,7 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
       return rows ? forward_wide<float, 2, kSeg, 2>(a, h0, out, h_last, ckpt, s)
                   : forward_wide<float, 2, kSeg, 0>(a, h0, out, h_last, ckpt, s);
     if (wide(1)) return forward_wide<float, 1, kSeg, 0>(a, h0, out, h_last, ckpt, s);
-    const Split p = split_of(a->T, a->N, a->D, 1);
+    const Split p = split_fwd(a->T, a->N, a->D, 1);
     return rows ? forward_long<float, 1, 2 * kSeg, 2>(a, p, h0, out, h_last, ckpt, s)
                 : forward_long<float, 1, 2 * kSeg, 0>(a, p, h0, out, h_last, ckpt, s);
   }
@@ -1016,15 +1028,15 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
                   : forward_wide<__nv_bfloat16, 2, kSeg, 0>(a, h0, out, h_last, ckpt, s);
     // One channel a thread while that leaves every CTA resident (65537 x 1 x 896: 173 us against 220
     // with two), two beyond (1000 x 150 x 256: 78 against 88).
-    const Split one = split_of(a->T, a->N, a->D, 1);
+    const Split one = split_fwd(a->T, a->N, a->D, 1);
     if (rows && one.units <= kResident[1])
       return forward_long<__nv_bfloat16, 1, 2 * kSeg, 2>(a, one, h0, out, h_last, ckpt, s);
-    const Split p = split_of(a->T, a->N, a->D, 2);
+    const Split p = split_fwd(a->T, a->N, a->D, 2);
     return rows ? forward_long<__nv_bfloat16, 2, kSeg, 3>(a, p, h0, out, h_last, ckpt, s)
                 : forward_long<__nv_bfloat16, 2, kSeg, 0>(a, p, h0, out, h_last, ckpt, s);
   }
   if (wide(1)) return forward_wide<__nv_bfloat16, 1, kSeg, 0>(a, h0, out, h_last, ckpt, s);
-  return forward_long<__nv_bfloat16, 1, 2 * kSeg, 0>(a, split_of(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
+  return forward_long<__nv_bfloat16, 1, 2 * kSeg, 0>(a, split_fwd(a->T, a->N, a->D, 1), h0, out, h_last, ckpt, s);
 }
 
 aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_seq* dh, const float* dh_last,
@@ -1053,9 +1065,9 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
   aht_status e;
   if (a->dtype == AHT_FP32)
     e = rows_16 ? backward<float, 1, true>(a, g, &segs, s) : backward<float, 1, false>(a, g, &segs, s);
-  // Wide bf16 passes of 128 x 16384 x 128: two channels a thread 689 us, one 892; split ones of
-  // 1000 x 300 x 256: two channels (their state spilled) 571 us, one 228.
-  else if (fits(2) && split_of(a->T, a->N, a->D, 2).wt == 1)
+  // Two channels a thread while whole groups of them fill the SMs (128 x 16384 x 128: 689 us, one
+  // channel 892), one below (1000 x 300 x 256, 1200 groups of two: 228 against 258).
+  else if (fits(2) && split_bwd(a->T, a->N, a->D, 2).wt == 1)
     e = rows_16 ? backward<__nv_bfloat16, 2, true>(a, g, &segs, s) : backward<__nv_bfloat16, 2, false>(a, g, &segs, s);
   else
     e = rows_16 ? backward<__nv_bfloat16, 1, true>(a, g, &segs, s) : backward<__nv_bfloat16, 1, false>(a, g, &segs, s);
