@@ -26,6 +26,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -60,11 +61,13 @@ constexpr float kUp = 1.0f + 2.0f / 8388608.0f;
 constexpr float kShift = kBq / (2.0f * kC), kDiag = kA - kBq * kBq / (4.0f * kC);
 constexpr int kNormBlocks = 1024;              // most partial sums of squares per matrix
 constexpr int kMaxSteps = 32;
+constexpr int kShareK = 4;                     // least blocks of K of an item that two pairs share
+constexpr uint32_t kParcel = 32 * kEpiThreads * 4;  // bytes of half a tile in fp32
 
 struct Mat {
   int32_t rows, cols, m, n, mb, nb, tall;
   int32_t norm_blocks;                         // partial sums of squares
-  int32_t sym_tiles;                           // stored blocks of a symmetric matrix
+  int32_t stores[3];                           // a phase's stores of tiles or, where shared, halves of them
   int64_t x[2], a, b;                          // byte offsets of the hi blocks
   int64_t x_lo, s_lo;                          // from a hi block to its lo block
 };
@@ -85,8 +88,9 @@ struct Common {
   double* norm;                                // [n_mats][kNormBlocks]
   uint32_t* done;                              // [n_mats][3 phases][kMaxSteps] finished tiles
   uint32_t* status;
-  const int4* items;                           // (matrix, phase, row pair, J) of one step
+  const int4* items;                           // of one step, see Item
   int32_t n_items, steps;
+  int32_t paired;                              // clusters are of two pairs, else of one
   int32_t bf16_in, bf16_out, update, nesterov;
   float mu, eps, decay, lr;                    // decay = 1 - lr * weight_decay
 };
@@ -298,8 +302,21 @@ __device__ __forceinline__ void add_release(uint32_t* p) {
 // Orders this thread's ordinary accesses to global memory with bulk copies, both ways.
 __device__ __forceinline__ void fence_proxy_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 
-// ---- a pair of CTAs (a cluster of two) ----
-__device__ __forceinline__ uint32_t pair_rank() {
+// An entry of the list of a step's work: (matrix or -1, phase | 4 * part, row pair, J).  Part 0 is all
+// of K, 1 and 2 its halves, the parts of the two pairs of a cluster.
+struct Item {
+  int mat, phase, part, I2, J, it;
+};
+__device__ __forceinline__ Item item_at(const Common& c, int g) {
+  const int it = g / c.n_items;
+  const int4 v = c.items[g - it * c.n_items];
+  return Item{v.x, v.y & 3, v.y >> 2, v.z, v.w, it};
+}
+__device__ __forceinline__ int first_k(int part, int K) { return part == 2 ? (K + 1) / 2 : 0; }
+__device__ __forceinline__ int end_k(int part, int K) { return part == 1 ? (K + 1) / 2 : K; }
+
+// ---- pairs of CTAs, two in a cluster ----
+__device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
@@ -307,16 +324,27 @@ __device__ __forceinline__ uint32_t pair_rank() {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
-// The address of a shared object of this CTA in CTA 0 of the pair.
-__device__ __forceinline__ uint32_t in_leader(const void* p) {
+// The address of a shared object of this CTA in another of the cluster.
+__device__ __forceinline__ uint32_t peer_addr(const void* p, int rank) {
   uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(tc::smem_u32(p)));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(tc::smem_u32(p)), "r"(rank));
   return r;
 }
 // (cta-scope release: what is handed over is tensor memory, ordered by the tcgen05 fence before
 // it; a cluster-scope release waits for the thread's stores, 600 clocks an arrival.)
 __device__ __forceinline__ void arrive_at(uint32_t mbar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(mbar) : "memory");
+}
+// The same where reads of shared memory have to be complete before the other side writes there.
+__device__ __forceinline__ void arrive_cluster(uint32_t mbar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mbar) : "memory");
+}
+// Sixteen bytes into another CTA of the cluster, counted on a barrier there.
+__device__ __forceinline__ void send16(uint32_t to, float4 v, uint32_t mbar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
+               "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y)), "r"(__float_as_uint(v.z)), "r"(__float_as_uint(v.w)),
+               "r"(mbar)
+               : "memory");
 }
 // A box of the workspace into this CTA's shared memory, counted on a barrier of either CTA.
 __device__ __forceinline__ void box_g2s(void* dst, const CUtensorMap* map, int row_group, int col_group, uint32_t mbar) {
@@ -333,12 +361,12 @@ __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uin
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
 }
-// The products issued so far arrive on a barrier of both CTAs when they are complete.
-__device__ __forceinline__ void commit_pair(uint64_t* mbar) {
+// The products issued so far arrive on a barrier of the CTAs of a mask (a pair) when they are complete.
+__device__ __forceinline__ void commit_pair(uint64_t* mbar, uint16_t ctas) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
           tc::smem_u32(mbar)),
-      "h"((uint16_t)3)
+      "h"(ctas)
       : "memory");
 }
 
@@ -356,22 +384,23 @@ __device__ __forceinline__ void transpose32(float* v, int lane) {
     }
 }
 
-// 64 columns j0.. of 32 rows i0.. of the orthogonal factor, a row a lane (the accumulated
+// W columns j0.. of 32 rows i0.. of the orthogonal factor, a row a lane (the accumulated
 // product f, unscaled), into the caller's matrix: the weight update, or the factor itself.  A wide
 // fp32 matrix whose rows allow it takes groups of four columns; a tall one is stored transposed,
 // so its lanes write neighbours; any other wide one is turned first (a block of 130 x 777 bf16
 // 3 us, a lane writing its row 9; turned fp32 rows 1 us a tile more than groups of four).
 // Sixteen elements at a time: their loads are in flight together.
+template <int W>
 __device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int k, const Mat& m, int i0, int lane, int j0,
-                                             float (&f)[64]) {
+                                             float (&f)[W]) {
   const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
   const int64_t ld = p.ld_out[k];
   void* out = p.out[k];
-  if (!m.tall && j0 + 64 <= m.n && !c.bf16_out && ((uintptr_t)out & 15) == 0 && (ld & 3) == 0) {
+  if (!m.tall && j0 + W <= m.n && !c.bf16_out && ((uintptr_t)out & 15) == 0 && (ld & 3) == 0) {
     if (i0 + lane >= m.m) return;
     float4* w = reinterpret_cast<float4*>(static_cast<float*>(out) + (int64_t)(i0 + lane) * ld + j0);
 #pragma unroll
-    for (int b = 0; b < 16; b += 4) {
+    for (int b = 0; b < W / 4; b += 4) {
       float4 o[4], old[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -391,7 +420,7 @@ __device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int
     return;
   }
 #pragma unroll
-  for (int b = 0; b < 64; b += 32) {
+  for (int b = 0; b < W; b += 32) {
     if (!m.tall) transpose32(f + b, lane);
     // element e of this lane: row i0 + e, column j0 + b + lane; tall: row i0 + lane, column j0 + b + e
     const int lane_at = m.tall ? i0 + lane : j0 + b + lane, lane_end = m.tall ? m.m : m.n;
@@ -448,15 +477,22 @@ __device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int
 // to fp32 registers (the tensor core rounds its running sum towards zero: summed over all of K
 // the bias of a 1024-wide product showed as 2e-5 of the result, 128 at a time as 6e-6, 64 at a
 // time as 3e-6, fp32 products have 2.6e-6) and run the tile's epilogue.
+//
+// A phase of few items leaves pairs idle while each item's sum over K runs (1 us per 128).  Where
+// no phase has more items than pairs, clusters are of two pairs and share the items with long
+// sums: each sums half of K, then sends half of its columns to the other, adds what it receives
+// and finishes its half (the exchange costs 1.1 us: 1024 x 1024, 8 blocks of K, 152 us instead of 183;
+// three of 130 x 777, where one product of three is shared, 117 instead of 125).
 __global__ void __launch_bounds__(kGemmThreads, 1)
     products(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ __align__(8) uint64_t full_bar[kStages / 2], empty_bar[kStages];
-  __shared__ __align__(8) uint64_t accf_bar[kAcc], acce_bar[kAcc], drain_bar;
+  __shared__ __align__(8) uint64_t accf_bar[kAcc], acce_bar[kAcc], drain_bar, parcel_bar, read_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = (int)pair_rank(), pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+  const int in_cluster = (int)cluster_rank(), rank = in_cluster & 1, leader = in_cluster & ~1;
+  const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) tc::mbar_init(&empty_bar[s], 1);
     for (int s = 0; s < kStages / 2; ++s) tc::mbar_init(&full_bar[s], 1);
@@ -465,6 +501,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       tc::mbar_init(&acce_bar[i], 2 * kEpiThreads / 32);  // a lane of every epilogue warp of the pair
     }
     tc::mbar_init(&drain_bar, 2);
+    tc::mbar_init(&parcel_bar, 1);
+    tc::mbar_init(&read_bar, 1);
     tc::mbar_init_fence();
     abort_flag = 0;
   }
@@ -478,6 +516,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   tc::fence_after_sync();
   const uint32_t tmem = tmem_slot;
   int issued = 0;  // (producer) stages filled
+  uint32_t sent = 0;  // (epilogue) halves of tiles exchanged
   const int n_all = c.n_items * c.steps;
 
   auto wait_or_abort = [&](uint64_t* bar, uint32_t parity) {
@@ -493,7 +532,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   auto ready = [&](const Mat& m, int k, int phase, int it) {
     if (phase == kGram && it == 0) return true;
     const int from = phase == kGram ? kApply : phase - 1;
-    const uint32_t want = (uint32_t)(from == kApply ? m.mb * m.nb : m.sym_tiles);
+    const uint32_t want = (uint32_t)(from == kGram ? m.stores[kGram] : from == kPoly ? m.stores[kPoly] : m.stores[kApply]);
     const uint32_t* at = c.done + (k * 3 + from) * kMaxSteps + (phase == kGram ? it - 1 : it);
     if (ld_acquire(at) >= want) return true;
     const uint64_t t0 = tc::globaltimer_ns();
@@ -512,21 +551,21 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       if (lane < 3)
         asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &maps.cols : lane == 1 ? &maps.rows : &maps.quarter)
                      : "memory");
-      const uint32_t full0 = in_leader(&full_bar[0]);
+      const uint32_t full0 = peer_addr(&full_bar[0], leader);
       const int half0 = of_a ? 0 : 8 * rank;      // this CTA's half of B's rows
       bool ok = true;
       int s = 0;
       uint32_t par = 1;                           // of the release awaited (the first pass waits for none)
       for (int g = pair; ok && g < n_all; g += pairs) {
-        const int it = g / c.n_items;
-        const int4 item = c.items[g - it * c.n_items];
-        const Mat m = c.mats[item.x];
-        const int I = min(2 * item.z + rank, m.mb - 1);  // (an odd last row is computed twice, stored once)
-        const int K = item.y == kGram ? m.nb : m.mb;
-        const Operand o = operand(item.y, m, it & 1, of_a, lo, I, item.w);
-        if (!(ok = ready(m, item.x, item.y, it))) break;
+        const Item t = item_at(c, g);
+        if (t.mat < 0) continue;
+        const Mat m = c.mats[t.mat];
+        const int I = min(2 * t.I2 + rank, m.mb - 1);  // (an odd last row is computed twice, stored once)
+        const int K = t.phase == kGram ? m.nb : m.mb;
+        const Operand o = operand(t.phase, m, t.it & 1, of_a, lo, I, t.J);
+        if (!(ok = ready(m, t.mat, t.phase, t.it))) break;
         fence_proxy_global();
-        for (int k = 0; ok && k < K; ++k) {
+        for (int k = first_k(t.part, K), k_end = end_k(t.part, K); ok && k < k_end; ++k) {
           const bool mn = o.mn(k);
           const int col0 = o.block(k) * 16 + (mn ? half0 : 0);
           const CUtensorMap* map = !of_a ? &maps.quarter : mn ? &maps.rows : &maps.cols;
@@ -554,17 +593,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       const uint32_t idesc = (1u << 4) | ((uint32_t)(kB >> 3) << 17) | ((uint32_t)(2 * kB >> 4) << 24);  // fp16 -> fp32
       const uint32_t base = tc::smem_u32(smem);
       const bool one = tc::elect_one();
+      const uint16_t both = (uint16_t)(3u << leader);
       int j = 0;
       bool ok = true;
       for (int g = pair; ok && g < n_all; g += pairs) {
-        const int it = g / c.n_items;
-        const int4 item = c.items[g - it * c.n_items];
-        const int mb = c.mats[item.x].mb, K = item.y == kGram ? c.mats[item.x].nb : mb;
-        for (int k = 0; ok && k < K; ++k, ++j) {
+        const Item t = item_at(c, g);
+        if (t.mat < 0) continue;
+        const int K = t.phase == kGram ? c.mats[t.mat].nb : c.mats[t.mat].mb;
+        for (int k = first_k(t.part, K), k_end = end_k(t.part, K); ok && k < k_end; ++k, ++j) {
           if ((j & 1) != (warp == 10)) continue;
           // the majors of operand()
-          const bool a_mn = item.y != kGram && k < 2 * item.z;
-          const bool b_mn = item.y == kApply || (item.y == kPoly && k < (item.w & ~1));
+          const bool a_mn = t.phase != kGram && k < 2 * t.I2;
+          const bool b_mn = t.phase == kApply || (t.phase == kPoly && k < (t.J & ~1));
           const uint32_t id = idesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
           const uint32_t da = a_mn ? 16u : 256u, db = b_mn ? 16u : 128u;  // 16 of K, in 16-byte units
           const int s = 2 * (j & 1);                // stages and accumulators s and s + 1
@@ -589,8 +629,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
               mma(a, b + kLoB, true);
               mma(a + kLoA, b, false);
               mma(a, b, false);
-              commit_pair(&empty_bar[s + h]);
-              commit_pair(&accf_bar[s + h]);
+              commit_pair(&empty_bar[s + h], both);
+              commit_pair(&accf_bar[s + h], both);
             }
             __syncwarp();
           }
@@ -602,25 +642,52 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const int q = warp & 3, r = 32 * q + lane;      // row of the tile
     const uint32_t lane_base = (uint32_t)(32 * q) << 16;
     const int c_beg = ((warp - 2) >> 2) * 64;       // this warp's half of the columns
-    const uint32_t acce0 = in_leader(&acce_bar[0]);
+    const uint32_t acce0 = peer_addr(&acce_bar[0], leader);
+    // shared items: the halves of a tile that the CTAs of the same rank of the two pairs exchange
+    const int other = c.paired ? in_cluster ^ 2 : in_cluster, side = in_cluster >> 1;
+    const uint8_t* parcel = smem + kStages * kStage + (tid - 64) * 16;
+    const uint32_t to = peer_addr(parcel, other), to_bar = peer_addr(&parcel_bar, other), read = peer_addr(&read_bar, other);
     int j = 0;
     bool ok = true;
     for (int g = pair; g < n_all; g += pairs) {
-      const int it = g / c.n_items;
-      const int4 item = c.items[g - it * c.n_items];
-      const Mat& m = c.mats[item.x];
-      const int phase = item.y, I = 2 * item.z + rank, J = item.w, K = phase == kGram ? m.nb : m.mb;
+      const Item t = item_at(c, g);
+      if (t.mat < 0) continue;
+      const Mat& m = c.mats[t.mat];
+      const int phase = t.phase, I = 2 * t.I2 + rank, J = t.J, K = phase == kGram ? m.nb : m.mb;
       const bool mine = I < m.mb;                   // (of an odd last row: nothing to store)
       const int64_t blk = (phase == kApply ? (int64_t)I * m.nb : (int64_t)I * m.mb) + J;
-      uint8_t* out = c.ws + (phase == kGram ? m.a : phase == kPoly ? m.b : it & 1 ? m.x[0] : m.x[1]) + blk * kBlk +
-                     chunk_at(r, c_beg >> 3);
+      uint8_t* out = c.ws + (phase == kGram ? m.a : phase == kPoly ? m.b : t.it & 1 ? m.x[0] : m.x[1]) + blk * kBlk;
       const int64_t lo_off = phase == kApply ? m.x_lo : m.s_lo;
       const float scale = kUp * (phase == kGram ? kSA / (kSX * kSX) : phase == kPoly ? kC * kSB / (kSA * kSA) : 1.0f / kSB);
       const float diag = phase == kApply || I != J ? 0.0f : phase == kGram ? kShift * kSA : kDiag * kSB;
+      const bool last = phase == kApply && t.it + 1 == c.steps;
+      // the columns c_at.. of row r, complete: to the workspace or, after the last step, the caller
+      auto finish = [&](auto& v, int c_at) {
+        constexpr int W = sizeof(v) / sizeof(float);
+        if (last) {
+          store_result<W>(c, p, t.mat, m, I * kB + 32 * q, lane, J * kB + c_at, v);
+          return;
+        }
+        uint8_t* hi_at = out + chunk_at(r, c_at >> 3);
+#pragma unroll
+        for (int x = 0; x < W / 8; ++x) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[8 * x + e] *= scale;
+          if (diag != 0.0f) {  // (the tile's row r is its column r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[8 * x + e] += r == c_at + 8 * x + e ? diag : 0.0f;
+          }
+          uint4 hi, lo;
+          split8(v + 8 * x, hi, lo);
+          uint8_t* at = hi_at + x * 2048;  // the next group of 8 columns
+          *reinterpret_cast<uint4*>(at) = hi;
+          *reinterpret_cast<uint4*>(at + lo_off) = lo;
+        }
+      };
       float f[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) f[e] = 0.0f;
-      for (int k = 0; ok && k < 2 * K; ++k, ++j) {
+      for (int k = 2 * first_k(t.part, K), k_end = 2 * end_k(t.part, K); ok && k < k_end; ++k, ++j) {
         const int acc = j % kAcc;
         // warp-uniform: tensor-memory loads are collective
         if (!(ok = wait_warp(&accf_bar[acc], (uint32_t)(j / kAcc) & 1u))) break;
@@ -639,23 +706,38 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         __syncwarp();
         if (lane == 0) arrive_at(acce0 + (uint32_t)acc * 8u);
       }
-      const bool last = phase == kApply && it + 1 == c.steps;
-      if (ok && mine && last) {
-        store_result(c, p, item.x, m, I * kB + 32 * q, lane, J * kB + c_beg, f);
-      } else if (ok && mine) {
+      if (mine && t.part == 0) {
+        if (ok) finish(f, c_beg);
+      } else if (mine) {
+        // Each CTA keeps 32 of the thread's columns and sends the others.
+        if (tid == 64) tc::mbar_expect_tx(&parcel_bar, kParcel);
+        if (ok && sent > 0) ok = wait_warp(&read_bar, (sent - 1) & 1u);
+        float own[32];
+        if (ok) {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[8 * t + e] *= scale;
-          if (diag != 0.0f) {  // (the tile's row r is its column r)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[8 * t + e] += r == c_beg + 8 * t + e ? diag : 0.0f;
+          for (int x = 0; x < 8; ++x) {
+            float4 o;
+            o.x = side ? f[4 * x] : f[32 + 4 * x];
+            o.y = side ? f[4 * x + 1] : f[33 + 4 * x];
+            o.z = side ? f[4 * x + 2] : f[34 + 4 * x];
+            o.w = side ? f[4 * x + 3] : f[35 + 4 * x];
+            send16(to + (uint32_t)x * kEpiThreads * 16u, o, to_bar);
           }
-          uint4 hi, lo;
-          split8(f + 8 * t, hi, lo);
-          uint8_t* at = out + t * 2048;  // the next group of 8 columns
-          *reinterpret_cast<uint4*>(at) = hi;
-          *reinterpret_cast<uint4*>(at + lo_off) = lo;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) own[e] = side ? f[32 + e] : f[e];
+          ok = wait_warp(&parcel_bar, sent & 1u);
+        }
+        ++sent;
+        if (ok) {
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const float4 o = *reinterpret_cast<const float4*>(parcel + x * kEpiThreads * 16);
+            own[4 * x] += o.x;
+            own[4 * x + 1] += o.y;
+            own[4 * x + 2] += o.z;
+            own[4 * x + 3] += o.w;
+          }
+          finish(own, c_beg + 32 * side);
         }
       }
       // all eight warps leave together: none is left at the barrier
@@ -663,8 +745,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       if (!ok) break;
       if (!last && mine && tid == 64) {  // the barrier ordered the tile's stores before these
         fence_proxy_global();
-        add_release(c.done + (item.x * 3 + phase) * kMaxSteps + it);
+        add_release(c.done + (t.mat * 3 + phase) * kMaxSteps + t.it);
       }
+      if (t.part != 0 && mine && tid == 96) arrive_cluster(read);  // (all eight warps have read theirs)
     }
     if (!ok) abort_flag = 1;
   }
@@ -688,6 +771,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   tc::fence_before_sync();
   __syncthreads();
   cluster_sync();
+  if (warp == 2 && abort_flag) {  // what the other pair sent lands before this CTA leaves (bounded)
+    tc::mbar_wait(&parcel_bar, (sent - 1) & 1u, 1000000ull);
+    tc::mbar_wait(&parcel_bar, sent & 1u, 1000000ull);
+  }
   if (warp == 0) {
     tc::fence_after_sync();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
@@ -711,11 +798,6 @@ static_assert(2 * kBlk <= kStaged && kStaged <= kParts, "S hi, lo and a staged m
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-__device__ __forceinline__ uint32_t peer_addr(const void* p, int rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(tc::smem_u32(p)), "r"(rank));
-  return r;
-}
 __device__ __forceinline__ float4 peer_load(uint32_t a) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
@@ -1089,6 +1171,7 @@ struct aht_muon {
   int cluster = 0;               // CTAs per matrix of small_updates; 0: the set needs products
   Maps maps{};
   int pairs = 0;                 // CTA pairs resident at once
+  int paired = 0;                // two of them in a cluster, to share items
   uint8_t* ws = nullptr;
   double* norm = nullptr;
   uint32_t* status = nullptr;
@@ -1103,13 +1186,14 @@ namespace {
     if (e_ != cudaSuccess) return set_last_error(AHT_ECUDA, cudaGetErrorString(e_));  \
   } while (0)
 
-void products_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int pairs, cudaStream_t stream) {
+void products_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int pairs, int paired,
+                     cudaStream_t stream) {
   cfg.gridDim = dim3(2u * (unsigned)pairs);
   cfg.blockDim = dim3(kGemmThreads);
-  cfg.dynamicSmemBytes = kStages * kStage;
+  cfg.dynamicSmemBytes = kStages * kStage + (paired ? kParcel : 0);
   cfg.stream = stream;
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim = {2, 1, 1};
+  attr[0].val.clusterDim = {paired ? 4u : 2u, 1, 1};
   attr[1].id = cudaLaunchAttributeCooperative;  // every CTA resident: they wait for one another's tiles
   attr[1].val.cooperative = 1;
   cfg.attrs = attr;
@@ -1125,6 +1209,7 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   c.status = s->status;
   c.items = s->items;
   c.n_items = s->n_items;
+  c.paired = s->paired;
   c.steps = s->cfg.steps;
   c.eps = s->cfg.eps;
   c.mu = s->cfg.momentum;
@@ -1148,7 +1233,7 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   MUON_CUDA(cudaGetLastError());
   normalise<<<dim3((unsigned)s->norm_chunks, n), 256, 0, s->stream>>>(c, p);
   MUON_CUDA(cudaGetLastError());
-  products_config(cfg, attr, std::min(s->n_items, s->pairs), s->stream);
+  products_config(cfg, attr, std::min(s->n_items, s->pairs), s->paired, s->stream);
   MUON_CUDA(cudaLaunchKernelEx(&cfg, products, c, p, s->maps));
   return AHT_OK;
 }
@@ -1173,6 +1258,48 @@ aht_status make_maps(aht_muon* s, int64_t bytes) {
   return AHT_OK;
 }
 
+// The work of one step (see Item): the phases in order, in each the longest items first.  Where
+// clusters are of two pairs and a phase leaves half of the pairs idle, its items with a sum over K
+// long enough to pay for the exchange are shared.
+struct Work {
+  std::vector<int4> items;
+  std::vector<std::array<int32_t, 3>> stores;  // see Mat
+  size_t most = 0, shared = 0;                 // entries of a phase, items shared
+};
+Work work_list(const std::vector<Mat>& mats, int pairs, bool paired) {
+  Work w;
+  w.stores.resize(mats.size());
+  for (int ph = kGram; ph <= kApply; ++ph) {
+    auto blocks_of_k = [&](const int4& v) { return ph == kGram ? mats[v.x].nb : mats[v.x].mb; };
+    std::vector<int4> list;
+    for (int k = 0; k < (int)mats.size(); ++k) {
+      const Mat& m = mats[k];
+      for (int I = 0; 2 * I < m.mb; ++I)
+        for (int J = ph == kApply ? 0 : 2 * I; J < (ph == kApply ? m.nb : m.mb); ++J) list.push_back(make_int4(k, ph, I, J));
+    }
+    std::stable_sort(list.begin(), list.end(),
+                     [&](const int4& x, const int4& y) { return blocks_of_k(x) > blocks_of_k(y); });
+    size_t shared = 0;
+    if (paired)
+      while (shared < list.size() && blocks_of_k(list[shared]) >= kShareK) ++shared;
+    if (list.size() + shared > (size_t)pairs) shared = 0;
+    for (size_t x = 0; x < list.size(); ++x) {
+      const int4 v = list[x];
+      w.stores[v.x][ph] += (x < shared ? 2 : 1) * std::min(2, mats[v.x].mb - 2 * v.z);
+      if (x < shared) {
+        w.items.push_back(make_int4(v.x, ph | 4, v.z, v.w));
+        w.items.push_back(make_int4(v.x, ph | 8, v.z, v.w));
+      } else {
+        w.items.push_back(v);
+      }
+    }
+    w.most = std::max(w.most, list.size() + shared);
+    w.shared += shared;
+    if (paired && (w.items.size() & 1)) w.items.push_back(make_int4(-1, 0, 0, 0));  // (shared ones start at even places)
+  }
+  return w;
+}
+
 aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht_muon_config* cfg, cudaStream_t stream,
                   aht_muon* s) {
   s->stream = stream;
@@ -1185,7 +1312,6 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     at += 2 * blocks * kBlk;      // hi, then lo
     return o;
   };
-  std::vector<int4> items[3];
   for (int k = 0; k < n; ++k) {
     Mat m{};
     m.rows = rows[k];
@@ -1203,28 +1329,9 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     m.s_lo = (int64_t)m.mb * m.mb * kBlk;
     m.norm_blocks = (int)std::min<int64_t>(((int64_t)m.rows * m.cols + 4095) / 4096, kNormBlocks);
     most = std::max(most, (int64_t)m.mb * m.nb);
-    for (int I = 0; I < m.mb; ++I) m.sym_tiles += m.mb - (I & ~1);
     s->norm_blocks = std::max(s->norm_blocks, m.norm_blocks);
     s->mats.push_back(m);
-    for (int I = 0; 2 * I < m.mb; ++I) {
-      for (int J = 2 * I; J < m.mb; ++J) {
-        items[kGram].push_back(make_int4(k, kGram, I, J));
-        items[kPoly].push_back(make_int4(k, kPoly, I, J));
-      }
-      for (int J = 0; J < m.nb; ++J) items[kApply].push_back(make_int4(k, kApply, I, J));
-    }
   }
-  // the longest tiles of a phase first
-  std::vector<int4> all;
-  for (int ph = 0; ph < 3; ++ph) {
-    std::stable_sort(items[ph].begin(), items[ph].end(), [&](const int4& x, const int4& y) {
-      const Mat &a = s->mats[x.x], &b = s->mats[y.x];
-      return (ph == kGram ? a.nb : a.mb) > (ph == kGram ? b.nb : b.mb);
-    });
-    all.insert(all.end(), items[ph].begin(), items[ph].end());
-  }
-  if (all.size() > (1u << 31) / (size_t)cfg->steps / 2) return set_last_error(AHT_EINVAL, "too many tiles in one call");
-  s->n_items = (int)all.size();
   s->norm_chunks = (int)std::min<int64_t>(most * 8, 1024);
   auto alloc = [&](void** ptr, size_t bytes) {
     if (cudaMalloc(ptr, bytes) != cudaSuccess) {
@@ -1237,27 +1344,43 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
   auto up = [&](void** dst, const void* h, size_t bytes) {
     return alloc(dst, bytes) && cudaMemcpy(*dst, h, bytes, cudaMemcpyHostToDevice) == cudaSuccess;
   };
-  if (!up((void**)&s->d_mats, s->mats.data(), s->mats.size() * sizeof(Mat)) ||
-      !up((void**)&s->items, all.data(), all.size() * sizeof(int4)) || !alloc((void**)&s->ws, (size_t)at) ||
-      !alloc((void**)&s->norm, (size_t)n * kNormBlocks * sizeof(double)) ||
-      !alloc((void**)&s->done, (size_t)n * 3 * kMaxSteps * 4) || !alloc((void**)&s->status, 4) ||
-      cudaMemset(s->status, 0, 4) != cudaSuccess)
-    return set_last_error(AHT_ENOMEM, "workspace allocation failed");
   // A set of matrices that each fit a cluster of small_updates runs there; beside a larger one
   // they cost nothing in products(), whose other tiles fill their waits.
   int wide = 0;
   for (const Mat& m : s->mats) wide = std::max(wide, m.mb == 1 ? m.nb : kSmallCluster + 1);
+  std::vector<int4> items;
   if (wide <= kSmallCluster) {
     for (s->cluster = 1; s->cluster < wide;) s->cluster *= 2;
     MUON_CUDA(cudaFuncSetAttribute(small_updates, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallSmem));
-    return AHT_OK;
+  } else {
+    MUON_CUDA(cudaFuncSetAttribute(products, cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * (int)kStage + (int)kParcel));
+    // Clusters of two pairs where no phase has more items than pairs and some are shared: 1024 x 1024
+    // 152 us, else 183; with more items the matrices' phases overlap, and 72 pairs (clusters of
+    // four CTAs leave some SMs empty) are fewer than 76: the set of two S5 heads 288 us, else 275.
+    for (int paired = 1; paired >= 0 && items.empty(); --paired) {
+      cudaLaunchConfig_t query{};
+      cudaLaunchAttribute attr[2];
+      products_config(query, attr, s->n_sms / 4 * 2, paired, s->stream);
+      int clusters = 0;
+      MUON_CUDA(cudaOccupancyMaxActiveClusters(&clusters, products, &query));
+      s->pairs = clusters * (paired + 1);
+      s->paired = paired;
+      Work w = work_list(s->mats, s->pairs, paired);
+      if (clusters < 1 || (paired && (w.most > (size_t)s->pairs || w.shared == 0))) continue;
+      items.swap(w.items);
+      for (size_t k = 0; k < s->mats.size(); ++k) std::copy(w.stores[k].begin(), w.stores[k].end(), s->mats[k].stores);
+    }
+    if (!s->pairs) return set_last_error(AHT_ECUDA, "no room for a CTA pair of the products");
   }
-  MUON_CUDA(cudaFuncSetAttribute(products, cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * (int)kStage));
-  cudaLaunchConfig_t cfg2{};
-  cudaLaunchAttribute attr[2];
-  products_config(cfg2, attr, s->n_sms / 2, s->stream);
-  MUON_CUDA(cudaOccupancyMaxActiveClusters(&s->pairs, products, &cfg2));
-  if (s->pairs < 1) return set_last_error(AHT_ECUDA, "no room for a CTA pair of the products");
+  if (items.size() > (1u << 31) / (size_t)cfg->steps / 2) return set_last_error(AHT_EINVAL, "too many tiles in one call");
+  s->n_items = (int)items.size();
+  if (!up((void**)&s->d_mats, s->mats.data(), s->mats.size() * sizeof(Mat)) || !alloc((void**)&s->ws, (size_t)at) ||
+      (s->n_items && !up((void**)&s->items, items.data(), items.size() * sizeof(int4))) ||
+      !alloc((void**)&s->norm, (size_t)n * kNormBlocks * sizeof(double)) ||
+      !alloc((void**)&s->done, (size_t)n * 3 * kMaxSteps * 4) || !alloc((void**)&s->status, 4) ||
+      cudaMemset(s->status, 0, 4) != cudaSuccess)
+    return set_last_error(AHT_ENOMEM, "workspace allocation failed");
+  if (s->cluster) return AHT_OK;
   return make_maps(s, at);
 }
 
