@@ -59,7 +59,7 @@ constexpr float kSX = 16384.0f, kSA = 16384.0f, kSB = 8192.0f;
 // scaled back by 2 * 2^-23.
 constexpr float kUp = 1.0f + 2.0f / 8388608.0f;
 constexpr float kShift = kBq / (2.0f * kC), kDiag = kA - kBq * kBq / (4.0f * kC);
-constexpr int kNormBlocks = 1024;              // most partial sums of squares per matrix
+constexpr int kNormBlocks = 608;               // most partial sums of squares per matrix (one wave)
 constexpr int kMaxSteps = 32;
 constexpr int kShareK = 4;                     // least blocks of K of an item that two pairs share
 constexpr uint32_t kParcel = 32 * kEpiThreads * 4;  // bytes of half a tile in fp32
@@ -86,6 +86,8 @@ struct Common {
   const Mat* mats;
   uint8_t* ws;
   double* norm;                                // [n_mats][kNormBlocks]
+  float* inv;                                  // [n_mats] 1 / (||U||_F + eps)
+  uint32_t* summed;                            // [n_mats] blocks of momentum_norm that are through, 0 between calls
   uint32_t* done;                              // [n_mats][3 phases][kMaxSteps] finished tiles
   uint32_t* status;
   const int4* items;                           // of one step, see Item
@@ -168,6 +170,8 @@ __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Com
     }
   } else {
     const uint32_t total = rows * cols;
+    float part = 0.0f;
+    int held = 0;
     for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += blocks * 256) {
       const uint32_t r = e / cols, col = e - r * cols;
       const float g = load_in(c, p, k, r, col);
@@ -178,16 +182,43 @@ __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Com
         *mp = mom;
       }
       const float u = u_of(c, g, mom);
-      sum += (double)(u * u);
+      part += u * u;
+      if (++held == 16) {
+        sum += part;
+        part = 0.0f;
+        held = 0;
+      }
     }
+    sum += part;
   }
   __shared__ double sh[256];
-  sh[threadIdx.x] = sum;
-  for (int s = 128; s > 0; s >>= 1) {
-    __syncthreads();
-    if (threadIdx.x < s) sh[threadIdx.x] += sh[threadIdx.x + s];
+  __shared__ bool last;
+  auto block_sum = [&](double v) {             // at thread 0
+    sh[threadIdx.x] = v;
+    for (int s = 128; s > 0; s >>= 1) {
+      __syncthreads();
+      if (threadIdx.x < s) sh[threadIdx.x] += sh[threadIdx.x + s];
+    }
+    return sh[0];
+  };
+  sum = block_sum(sum);
+  if (threadIdx.x == 0) {
+    c.norm[k * kNormBlocks + blockIdx.x] = sum;
+    __threadfence();
+    last = atomicAdd(&c.summed[k], 1u) == (uint32_t)blocks - 1;
   }
-  if (threadIdx.x == 0) c.norm[k * kNormBlocks + blockIdx.x] = sh[0];
+  __syncthreads();
+  if (!last) return;
+  // the last block adds the sums, in their order, and divides once (64-bit additions and divisions
+  // are slow: with them in every block of normalise it took 30 us for 2048 x 4096, now 18)
+  __threadfence();
+  double all = 0.0;
+  for (int i = threadIdx.x; i < blocks; i += 256) all += __ldcg(&c.norm[k * kNormBlocks + i]);
+  all = block_sum(all);
+  if (threadIdx.x == 0) {
+    c.inv[k] = (float)(1.0 / (sqrt(all) + (double)c.eps));
+    c.summed[k] = 0;
+  }
 }
 
 // 8 values (already scaled) -> their hi and lo chunks
@@ -209,27 +240,22 @@ __device__ __forceinline__ void split8(const float* v, uint4& hi, uint4& lo) {
 __device__ __forceinline__ int64_t chunk_at(int r, int cb) { return ((cb * 16 + (r >> 3)) << 7) + ((r & 7) << 4); }
 
 // ---- X = U / (||U||_F + eps), split into blocks -------------------------------------------
-// One thread per 8-column chunk of a row of X; consecutive threads take consecutive rows.
+// One thread per 8-column chunk of a row of X.  A warp takes 8 rows x 4 chunks of a wide matrix, so
+// that it reads and writes runs of 128 bytes (an update of the two S5 heads 263 us; 32 rows of a
+// chunk each 275), and 32 rows of a tall one, whose rows are the caller's columns.
 __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common c, const __grid_constant__ Ptrs p) {
   const int k = blockIdx.y;
   const Mat m = c.mats[k];
   const int64_t chunks = (int64_t)m.mb * m.nb * 2048;
   if ((int64_t)blockIdx.x * 256 >= chunks) return;
-  __shared__ double sh[256];
-  double part = 0.0;
-  for (int i = threadIdx.x; i < m.norm_blocks; i += 256) part += c.norm[k * kNormBlocks + i];
-  sh[threadIdx.x] = part;
-  for (int s = 128; s > 0; s >>= 1) {
-    __syncthreads();
-    if (threadIdx.x < s) sh[threadIdx.x] += sh[threadIdx.x + s];
-  }
-  __syncthreads();
-  const float inv = (float)(1.0 / (sqrt(sh[0]) + (double)c.eps));
+  const float inv = c.inv[k];
   uint8_t* x = c.ws + m.x[0];
   const bool four = !m.tall && fours(c, p, k, m.cols);
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < chunks; q += (int64_t)gridDim.x * 256) {
     const int blk = (int)(q >> 11);
-    const int r = (int)(q & 127), cb = (int)(q >> 7) & 15;
+    const int z = (int)q & 2047;
+    const int r = m.tall ? z & 127 : (z & 7) | (z >> 2 & 0x78);
+    const int cb = m.tall ? z >> 7 : (z >> 3 & 3) | (z >> 7 & 12);
     const int bi = blk / m.nb, i = bi * kB + r, j0 = (blk - bi * m.nb) * kB + 8 * cb;
     float v[8];
     if (four && i < m.m && j0 + 8 <= m.n) {
@@ -486,7 +512,7 @@ __device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int
 __global__ void __launch_bounds__(kGemmThreads, 1)
     products(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t full_bar[kStages / 2], empty_bar[kStages];
+  __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages];
   __shared__ __align__(8) uint64_t accf_bar[kAcc], acce_bar[kAcc], drain_bar, parcel_bar, read_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
@@ -494,8 +520,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   const int in_cluster = (int)cluster_rank(), rank = in_cluster & 1, leader = in_cluster & ~1;
   const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) tc::mbar_init(&empty_bar[s], 1);
-    for (int s = 0; s < kStages / 2; ++s) tc::mbar_init(&full_bar[s], 1);
+    for (int s = 0; s < kStages; ++s) {
+      tc::mbar_init(&empty_bar[s], 1);
+      tc::mbar_init(&full_bar[s], 1);
+    }
     for (int i = 0; i < kAcc; ++i) {
       tc::mbar_init(&accf_bar[i], 1);
       tc::mbar_init(&acce_bar[i], 2 * kEpiThreads / 32);  // a lane of every epilogue warp of the pair
@@ -572,8 +600,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (issued >= kStages && !(ok = wait_or_abort(&empty_bar[s + h], par))) break;
-            if (lane == 0 && rank == 0 && h == 0) tc::mbar_expect_tx(&full_bar[s >> 1], 4 * kStage);
-            box_g2s(dst0 + (s + h) * kStage, map, mn ? 8 * h : half0, mn ? col0 : col0 + 8 * h, full0 + (s >> 1) * 8);
+            if (lane == 0 && rank == 0) tc::mbar_expect_tx(&full_bar[s + h], 2 * kStage);
+            box_g2s(dst0 + (s + h) * kStage, map, mn ? 8 * h : half0, mn ? col0 : col0 + 8 * h, full0 + (s + h) * 8);
             ++issued;
           }
           if ((s ^= 2) == 0) par ^= 1u;
@@ -613,9 +641,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           auto b_desc = [&](uint32_t x) { return b_mn ? tc::smem_desc(x, 128u, 1024u) : tc::smem_desc(x, 1024u, 128u); };
           const uint64_t a0 = a_desc(base + (uint32_t)s * kStage), b0 = b_desc(base + (uint32_t)s * kStage + 2 * kHalf);
           constexpr uint64_t kLoA = kHalf / 16, kLoB = kHalf / 32, kNext = kStage / 16;
-          if (!(ok = wait_warp(&full_bar[j & 1], par))) break;
+          // An item's first products start on half a unit; later units are waited for whole,
+          // under the other warp's products.
+          const bool first = k == first_k(t.part, K);
+          if (!(ok = wait_warp(&full_bar[s], par))) break;
+          if (!first && !(ok = wait_warp(&full_bar[s + 1], par))) break;
 #pragma unroll
           for (int h = 0; ok && h < 2; ++h) {
+            if (first && h == 1 && !(ok = wait_warp(&full_bar[s + 1], par))) break;
             if (j >= 2 && !(ok = wait_warp(&acce_bar[s + h], par ^ 1u))) break;
             tc::fence_after_sync();
             if (one) {
@@ -765,8 +798,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     tc::mbar_wait(&drain_bar, 0);
   }
   if (warp == 0 && lane == 0 && rank == 0 && abort_flag) {
-    for (int u = (issued + 1) / 2 - 1; u >= 0 && u >= (issued + 1) / 2 - 2; --u)
-      tc::mbar_wait(&full_bar[u & 1], (uint32_t)(u >> 1) & 1u);
+    for (int d = max(0, issued - kStages); d < issued; ++d)
+      tc::mbar_wait(&full_bar[d % kStages], (uint32_t)(d / kStages) & 1u);
   }
   tc::fence_before_sync();
   __syncthreads();
@@ -817,7 +850,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ __align__(8) uint64_t done_bar;
   __shared__ uint32_t tmem_slot;
-  __shared__ double norm_s[kSmallThreads / 32], norm_all;
+  __shared__ double norm_s[kSmallThreads / 32];
+  __shared__ float inv_s;
   uint8_t *xs = smem, *ss = smem + 2 * kBlk, *parts = ss + kStaged;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int k = (int)blockIdx.x / cluster, rank = (int)blockIdx.x % cluster;
@@ -1011,11 +1045,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     const double mine = lane < nb ? peer_load_f64(peer_addr(&norm_s[0], lane)) : 0.0;
     double t = 0.0;
     for (int q = 0; q < nb; ++q) t += __shfl_sync(0xFFFFFFFFu, mine, q);
-    if (lane == 0) norm_all = t;
+    if (lane == 0) inv_s = (float)(1.0 / (sqrt(t) + (double)c.eps));  // (once: 64-bit arithmetic is slow)
   }
   __syncthreads();
   if (!tall) unstage(ss);
-  const float inv = (float)(1.0 / (sqrt(norm_all) + (double)c.eps));
+  const float inv = inv_s;
 #pragma unroll
   for (int e = 0; e < 64; ++e) f[e] = (f[e] * inv) * kSX;
   if (on) split_to(xs);
@@ -1174,6 +1208,8 @@ struct aht_muon {
   int paired = 0;                // two of them in a cluster, to share items
   uint8_t* ws = nullptr;
   double* norm = nullptr;
+  float* inv = nullptr;
+  uint32_t* summed = nullptr;
   uint32_t* status = nullptr;
   std::vector<void*> owned;
 };
@@ -1205,6 +1241,8 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   c.mats = s->d_mats;
   c.ws = s->ws;
   c.norm = s->norm;
+  c.inv = s->inv;
+  c.summed = s->summed;
   c.done = s->done;
   c.status = s->status;
   c.items = s->items;
@@ -1332,7 +1370,7 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     s->norm_blocks = std::max(s->norm_blocks, m.norm_blocks);
     s->mats.push_back(m);
   }
-  s->norm_chunks = (int)std::min<int64_t>(most * 8, 1024);
+  s->norm_chunks = (int)std::min<int64_t>(most * 8, 4096);
   auto alloc = [&](void** ptr, size_t bytes) {
     if (cudaMalloc(ptr, bytes) != cudaSuccess) {
       cudaGetLastError();
@@ -1376,7 +1414,8 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
   s->n_items = (int)items.size();
   if (!up((void**)&s->d_mats, s->mats.data(), s->mats.size() * sizeof(Mat)) || !alloc((void**)&s->ws, (size_t)at) ||
       (s->n_items && !up((void**)&s->items, items.data(), items.size() * sizeof(int4))) ||
-      !alloc((void**)&s->norm, (size_t)n * kNormBlocks * sizeof(double)) ||
+      !alloc((void**)&s->norm, (size_t)n * kNormBlocks * sizeof(double)) || !alloc((void**)&s->inv, (size_t)n * 4) ||
+      !alloc((void**)&s->summed, (size_t)n * 4) || cudaMemset(s->summed, 0, (size_t)n * 4) != cudaSuccess ||
       !alloc((void**)&s->done, (size_t)n * 3 * kMaxSteps * 4) || !alloc((void**)&s->status, 4) ||
       cudaMemset(s->status, 0, 4) != cudaSuccess)
     return set_last_error(AHT_ENOMEM, "workspace allocation failed");
