@@ -421,7 +421,8 @@ aht_status aht_s5_sync(aht_s5* s);
  * data[t * st + n * sn + d]: time-major, env-major and slices of one fused projection are
  * all strides.  Gates, state and sums are fp32; each output is rounded once.  Outputs must
  * not overlap inputs or one another (h_last may be h0).  Lanes (n, d) are independent and
- * every sum has a fixed order: the same call gives the same bits.
+ * every sum has a fixed order: the same call gives the same bits.  N * ceil(D / 32) may be up
+ * to 2^32, N * D to 2^37 and T * N * D to 2^46.
  * T = 1 is the serving step: h0 and h_last are the carried state.  Calls are asynchronous
  * on cuda_stream (NULL = default), allocate nothing and may be captured into a graph. */
 #define AHT_GLR_SEGMENT 8       /* steps between two checkpoints of the state */
@@ -484,8 +485,10 @@ typedef struct aht_muon_matrix {  /* device arrays of one matrix */
 } aht_muon_matrix;
 typedef struct aht_muon aht_muon; /* opaque, library-owned */
 /* Allocates the workspace for n matrices of these sizes (about 8 bytes per element plus 8
- * per element of the short side's square, sides rounded up to 128); work runs on
- * cuda_stream (NULL = default).  The other calls allocate nothing. */
+ * per element of the short side's square, sides rounded up to 128).  Every later call runs on
+ * cuda_stream (NULL = default), after what was put there before and only that: a caller whose
+ * gradients come from another stream makes this one wait for it.  The other calls allocate
+ * nothing; calls on one handle come from one thread at a time. */
 aht_status aht_muon_create(int32_t n, const int32_t* rows, const int32_t* cols, const aht_muon_config* cfg,
                            void* cuda_stream, aht_muon** out);
 void aht_muon_destroy(aht_muon* s);

@@ -1419,6 +1419,7 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
       !alloc((void**)&s->done, (size_t)n * 3 * kMaxSteps * 4) || !alloc((void**)&s->status, 4) ||
       cudaMemset(s->status, 0, 4) != cudaSuccess)
     return set_last_error(AHT_ENOMEM, "workspace allocation failed");
+  MUON_CUDA(cudaStreamSynchronize(cudaStreamLegacy));  // the tables are there, whatever kind of stream s->stream is
   if (s->cluster) return AHT_OK;
   return make_maps(s, at);
 }

@@ -57,17 +57,24 @@ def gated_step(x, r, i, lam, state, reset=None):
 
 
 class OrthogonalOptimizer:
-    """aht_muon_step over the gradients of a fixed list of f32 matrices."""
+    """aht_muon_step over the gradients of a fixed list of f32 matrices.  The updates run on the
+    stream that is current here; a step under another one is ordered with it both ways."""
 
     def __init__(self, params, lr=0.02, **cfg):
         self.params, self.lr = list(params), lr
         self.momenta = [torch.zeros_like(p) for p in self.params]
-        self.handle = aht.aht_muon_create([tuple(p.shape) for p in self.params], **cfg)
+        self.stream = torch.cuda.current_stream()
+        self.handle = aht.aht_muon_create([tuple(p.shape) for p in self.params], stream=self.stream, **cfg)
 
     @torch.no_grad()
     def step(self):
+        now = torch.cuda.current_stream()
+        if now != self.stream:
+            self.stream.wait_stream(now)
         aht.aht_muon_step(self.handle, [p.detach() for p in self.params], self.momenta, [p.grad for p in self.params],
                           self.lr)
+        if now != self.stream:
+            now.wait_stream(self.stream)
         for p in self.params:
             p.grad = None
 
