@@ -507,8 +507,8 @@ __device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int
 // A phase of few items leaves pairs idle while each item's sum over K runs (1 us per 128).  Where
 // no phase has more items than pairs, clusters are of two pairs and share the items with long
 // sums: each sums half of K, then sends half of its columns to the other, adds what it receives
-// and finishes its half (the exchange costs 1.1 us: 1024 x 1024, 8 blocks of K, 152 us instead of 183;
-// three of 130 x 777, where one product of three is shared, 117 instead of 125).
+// and finishes its half (the exchange costs 1.1 us: 1024 x 1024, 8 blocks of K, 31 us of 183 less; three
+// of 130 x 777, where one product of three is shared, 8 of 125).
 __global__ void __launch_bounds__(kGemmThreads, 1)
     products(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -831,11 +831,6 @@ static_assert(2 * kBlk <= kStaged && kStaged <= kParts, "S hi, lo and a staged m
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-__device__ __forceinline__ float4 peer_load(uint32_t a) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
-  return v;
-}
 __device__ __forceinline__ void peer_store(uint32_t a, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
@@ -1393,8 +1388,8 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
   } else {
     MUON_CUDA(cudaFuncSetAttribute(products, cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * (int)kStage + (int)kParcel));
     // Clusters of two pairs where no phase has more items than pairs and some are shared: 1024 x 1024
-    // 152 us, else 183; with more items the matrices' phases overlap, and 72 pairs (clusters of
-    // four CTAs leave some SMs empty) are fewer than 76: the set of two S5 heads 288 us, else 275.
+    // 31 us of 183 less; with more items the matrices' phases overlap, and 72 pairs (clusters of
+    // four CTAs leave some SMs empty) are fewer than 76: the set of two S5 heads 288 us instead of 275.
     for (int paired = 1; paired >= 0 && items.empty(); --paired) {
       cudaLaunchConfig_t query{};
       cudaLaunchAttribute attr[2];
