@@ -126,7 +126,8 @@ __device__ __forceinline__ float u_of(const Common& c, float g, float mom) {
 
 // ---- momentum and the sum of squares of U ------------------------------------------------
 // Also clears the tile counters of the call.  A thread takes four groups of four columns at a
-// time (their loads in flight together) where the rows allow it, else single elements.
+// time (their loads in flight together) where the rows allow it, else single elements.  Bound by
+// memory latency: 2048 x 4096, bf16 gradient, 20 us from a cold cache, 84 MB.
 __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Common c, const __grid_constant__ Ptrs p) {
   const int k = blockIdx.y;
   const Mat& m = c.mats[k];
@@ -821,7 +822,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 // B) in shared memory.  The CTAs' partial Gram matrices meet in distributed shared memory: each
 // CTA receives everyone's part of its share of the rows, sums them in the order of the CTAs and
 // sends the sum to all (stores only: a remote load waits 0.3 us).  The other two products need no
-// exchange.
+// exchange.  Bound by the chain of a step: Gram product 1.7 us, exchange 2.5, the other two 1.9 each
+// (128 x 196 and 128 x 128, five steps and the update: 55 us; products() takes 82).
 constexpr int kSmallCluster = 8;
 constexpr int kSmallThreads = 256;
 constexpr uint32_t kStaged = 32 * (kB + 1) * 16;  // 128 x 128 fp32, four columns of a row together, padded
