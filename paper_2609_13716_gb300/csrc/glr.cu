@@ -339,12 +339,13 @@ struct Exchange {
 // segment waits in registers.
 //
 // Whole chains are bound by memory (128 x 8192 x 128 fp32 307 us, the rate of a copy; 128 x 16384 x
-// 128 bf16 360 us, 6.0 TB/s, and 61 % of the issue slots); split ones by the hand-over of a window
-// between a cluster's CTAs (65537 x 1 x 896 fp32 172 us, 5.5 TB/s); one step by its launch.
+// 128 bf16 358 us, 6.1 TB/s, and 61 % of the issue slots); split ones by the hand-over of a window
+// between a cluster's CTAs (65537 x 1 x 896 fp32 170 us, 5.5 TB/s); one step by its launch.
 template <typename E, int V, int S, int WT, int kWarps, bool kCluster, int kRing>
 __global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 2 ? 5 : 16 / kWarps)
     glr_fwd(const __grid_constant__ GlrDev a, const float* h0, const __grid_constant__ Seq h, float* h_last,
             float* ckpt, int n_rank) {
+  tc::after_previous();
   using X = Exchange<V, WT, kCluster>;
   __shared__ typename X::Shared sh;
   constexpr int kE = S * V;
@@ -554,6 +555,7 @@ struct GlrGrad {
 template <typename E, int V, int WT, int kWarps, bool kCluster, int kRing>
 __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     glr_bwd(const __grid_constant__ GlrDev a, const __grid_constant__ GlrGrad b, int n_rank) {
+  tc::after_previous();
   using X = Exchange<V, WT, kCluster>;
   __shared__ typename X::Shared sh;
   constexpr int S = kSeg, WL = kWarps / WT, kE = S * V;
@@ -834,6 +836,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
 template <bool kLast>
 __global__ void glr_dlam(const float* __restrict__ part, int64_t rows, int32_t D, const float* __restrict__ lam,
                          float* __restrict__ out) {
+  tc::after_previous();
   __shared__ float sh[32][33];
   const int d = blockIdx.x * 32 + threadIdx.x;
   float sum = 0.0f, comp = 0.0f;
@@ -927,21 +930,24 @@ Split split_bwd(int64_t T, int64_t N, int32_t D, int V) {
 }
 
 template <typename K, typename... Args>
-aht_status launch(K kernel, int64_t blocks, int threads, int cl, int smem, cudaStream_t s, Args... args) {
+aht_status launch(K kernel, dim3 grid, dim3 block, int cl, int smem, cudaStream_t s, Args... args) {
   if (smem > 16 * 1024)  // (with the static part it may pass 48 KB)
     if (aht_status e = launched(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem))) return e;
   if (cl > 8)  // beyond what every device runs
     if (aht_status e = launched(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1))) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(blocks * cl));
-  cfg.blockDim = dim3((unsigned)threads);
+  cfg.gridDim = dim3(grid.x * (unsigned)cl, grid.y);
+  cfg.blockDim = block;
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim = {(unsigned)cl, 1, 1};
+  // (128 x 4096 x 128 bf16 forward + backward 296 us, 303 without; 4096 x 8 x 512 153, 159)
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see tc::after_previous()
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {(unsigned)cl, 1, 1};
   cfg.attrs = attr;
-  cfg.numAttrs = cl > 1 ? 1 : 0;
+  cfg.numAttrs = cl > 1 ? 2 : 1;
   return launched(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
@@ -951,7 +957,7 @@ aht_status forward_wide(const aht_glr_args* a, const float* h0, const Seq& h, fl
   const int64_t four = (split_fwd(a->T, a->N, a->D, V).units + 3) / 4;
   constexpr int kSmem = 4 * kRing * Ring<3, 8, V * (int)sizeof(E), 0>::kStage;
   static_assert(kRing == 0 || S == 8, "");
-  return launch(glr_fwd<E, V, S, 1, 4, false, kRing>, four, 128, 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, S, 1, 4, false, kRing>, dim3((unsigned)four), dim3(128), 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
 }
 // Few lanes: 8 warps and p.cl CTAs along time.
 template <typename E, int V, int S, int kRing>
@@ -959,8 +965,8 @@ aht_status forward_long(const aht_glr_args* a, const Split& p, const float* h0, 
                         cudaStream_t s) {
   constexpr int kSmem = 8 * kRing * Ring<3, S, V * (int)sizeof(E), 0>::kStage;
   if (p.cl == 1)
-    return launch(glr_fwd<E, V, S, 8, 8, false, kRing>, p.units, 256, 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
-  return launch(glr_fwd<E, V, S, 8, 8, true, kRing>, p.units, 256, p.cl, kSmem, s, dev(a), h0, h, h_last, ckpt, p.cl);
+    return launch(glr_fwd<E, V, S, 8, 8, false, kRing>, dim3((unsigned)p.units), dim3(256), 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, S, 8, 8, true, kRing>, dim3((unsigned)p.units), dim3(256), p.cl, kSmem, s, dev(a), h0, h, h_last, ckpt, p.cl);
 }
 
 template <typename E, int V, bool kRows>  // kRows: rows aligned for the ring
@@ -970,10 +976,10 @@ aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStre
   *rows = p.segs();
   constexpr int kStage = Ring<4, kSeg, V * (int)sizeof(E), 128 * V>::kStage, kWide = kRows ? 2 : 0, kLong = kRows ? 3 : 0;
   if (V > 1 || p.wt == 1)
-    return launch(glr_bwd<E, V, 1, 4, false, kWide>, (p.units + 3) / 4, 128, 1, 4 * kWide * kStage, s, d, g, 1);
+    return launch(glr_bwd<E, V, 1, 4, false, kWide>, dim3((unsigned)((p.units + 3) / 4)), dim3(128), 1, 4 * kWide * kStage, s, d, g, 1);
   if constexpr (V == 1) {
-    if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kLong>, p.units, 256, 1, 8 * kLong * kStage, s, d, g, 1);
-    return launch(glr_bwd<E, V, 8, 8, true, kLong>, p.units, 256, p.cl, 8 * kLong * kStage, s, d, g, p.cl);
+    if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kLong>, dim3((unsigned)p.units), dim3(256), 1, 8 * kLong * kStage, s, d, g, 1);
+    return launch(glr_bwd<E, V, 8, 8, true, kLong>, dim3((unsigned)p.units), dim3(256), p.cl, 8 * kLong * kStage, s, d, g, p.cl);
   }
   return AHT_EINVAL;  // (V > 1 is wide)
 }
@@ -1082,15 +1088,10 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
   if (e != AHT_OK || !dlam) return e;
   const int64_t rows = (int64_t)segs * a->N;
   const dim3 grid((a->D + 31) / 32), block(32, 32);
-  if (rows <= 512) {
-    glr_dlam<true><<<grid, block, 0, s>>>(part, rows, a->D, a->lam, dlam);
-    return launched(cudaGetLastError());
-  }
+  if (rows <= 512) return launch(glr_dlam<true>, grid, block, 1, 0, s, part, rows, a->D, a->lam, dlam);
   float* first = part + part_floats(a->T, a->N, a->D);
-  glr_dlam<false><<<dim3(grid.x, kSumRows), block, 0, s>>>(part, rows, a->D, a->lam, first);
-  if (aht_status e2 = launched(cudaGetLastError())) return e2;
-  glr_dlam<true><<<grid, block, 0, s>>>(first, kSumRows, a->D, a->lam, dlam);
-  return launched(cudaGetLastError());
+  if ((e = launch(glr_dlam<false>, dim3(grid.x, kSumRows), block, 1, 0, s, part, rows, a->D, a->lam, first))) return e;
+  return launch(glr_dlam<true>, grid, block, 1, 0, s, first, (int64_t)kSumRows, a->D, a->lam, dlam);
 }
 
 }  // extern "C"

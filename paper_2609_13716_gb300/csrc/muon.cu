@@ -129,6 +129,7 @@ __device__ __forceinline__ float u_of(const Common& c, float g, float mom) {
 // time (their loads in flight together) where the rows allow it, else single elements.  Bound by
 // memory latency: 2048 x 4096, bf16 gradient, 20 us from a cold cache, 84 MB.
 __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Common c, const __grid_constant__ Ptrs p) {
+  tc::after_previous();
   const int k = blockIdx.y;
   const Mat& m = c.mats[k];
   const int blocks = m.norm_blocks;
@@ -245,6 +246,7 @@ __device__ __forceinline__ int64_t chunk_at(int r, int cb) { return ((cb * 16 + 
 // that it reads and writes runs of 128 bytes (an update of the two S5 heads 263 us; 32 rows of a
 // chunk each 275), and 32 rows of a tall one, whose rows are the caller's columns.
 __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common c, const __grid_constant__ Ptrs p) {
+  tc::after_previous();
   const int k = blockIdx.y;
   const Mat m = c.mats[k];
   const int64_t chunks = (int64_t)m.mb * m.nb * 2048;
@@ -844,6 +846,7 @@ __device__ __forceinline__ double peer_load_f64(uint32_t a) {
 
 __global__ void __launch_bounds__(kSmallThreads, 1)
     small_updates(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, int cluster) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ __align__(8) uint64_t done_bar;
   __shared__ uint32_t tmem_slot;
@@ -1113,6 +1116,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       split_to(xs);
     }
   }
+  // (the next call's CTAs from here on: from the start on they cost 2 us of 57 instead of saving 1)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (nb == 2) cluster_wait();
   // the weights, along their rows like the gradient
   if (on && tall && ok) store_result(c, p, k, m, 32 * (warp & 3), lane, j0, f);
@@ -1251,7 +1256,9 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   c.nesterov = s->cfg.nesterov;
   const unsigned n = (unsigned)s->mats.size();
   cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[2], overlap;        // see tc::after_previous()
+  overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  overlap.val.programmaticStreamSerializationAllowed = 1;
   if (s->cluster) {
     cfg.gridDim = dim3(n * (unsigned)s->cluster);
     cfg.blockDim = dim3(kSmallThreads);
@@ -1259,15 +1266,20 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
     cfg.stream = s->stream;
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim = {(unsigned)s->cluster, 1, 1};
+    attr[1] = overlap;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     MUON_CUDA(cudaLaunchKernelEx(&cfg, small_updates, c, p, s->cluster));
     return AHT_OK;
   }
-  momentum_norm<<<dim3((unsigned)s->norm_blocks, n), 256, 0, s->stream>>>(c, p);
-  MUON_CUDA(cudaGetLastError());
-  normalise<<<dim3((unsigned)s->norm_chunks, n), 256, 0, s->stream>>>(c, p);
-  MUON_CUDA(cudaGetLastError());
+  cfg.blockDim = dim3(256);
+  cfg.stream = s->stream;
+  cfg.attrs = &overlap;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3((unsigned)s->norm_blocks, n);
+  MUON_CUDA(cudaLaunchKernelEx(&cfg, momentum_norm, c, p));
+  cfg.gridDim = dim3((unsigned)s->norm_chunks, n);
+  MUON_CUDA(cudaLaunchKernelEx(&cfg, normalise, c, p));
   products_config(cfg, attr, std::min(s->n_items, s->pairs), s->paired, s->stream);
   MUON_CUDA(cudaLaunchKernelEx(&cfg, products, c, p, s->maps));
   return AHT_OK;

@@ -205,6 +205,14 @@ __device__ __forceinline__ bool elect_one() {
   return r != 0;
 }
 
+// First statement of a kernel launched with programmatic stream serialization: it may start while the
+// one before it in the stream drains, lets the next one do so, and reads and writes nothing before
+// all of that one's work is done and visible.
+__device__ __forceinline__ void after_previous() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Named barrier over `count` threads (a multiple of 32).
 __device__ __forceinline__ void bar_sync(int id, int count) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
