@@ -213,7 +213,7 @@ struct Ring {
 // resets.  Loaded with a segment's rows, a window before the ballot waits for it.
 template <int S>
 __device__ __forceinline__ uint8_t reset_byte(const GlrDev& a, const Place& at, int64_t t0, int lane) {
-  return a.reset && lane < S && t0 + lane < at.len ? __ldg(a.reset + (t0 + lane) * a.N + at.n) : (uint8_t)0;
+  return a.reset && lane < S && t0 + lane < at.len ? a.reset[(t0 + lane) * a.N + at.n] : (uint8_t)0;
 }
 
 // The map that reaches segment (rank, wt) of a window, from the maps (A, H) that every
@@ -831,11 +831,12 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
 
 // Sums over rows of part[rows][D] in a fixed order: CTA (x, y) takes 32 channels and the
 // rows y, y + gridDim.y, ... ; 32 row-threads per channel, then a tree.  kLast also applies
-// dlam[d] = -sum sigmoid(lam) / softplus(lam) (the ratio tends to 1 as lam -> -inf).
+// dlam[d] = -sum sigmoid(lam) / softplus(lam) (the ratio tends to 1 as lam -> -inf).  part is
+// written while CTAs of this kernel already wait in after_previous(), so it is read by ordinary
+// loads: no __restrict__, which would let them go through the read-only path.
 // Latency: 6 + 5 us for 4096 rows of 128 in two passes, one alone 24.
 template <bool kLast>
-__global__ void glr_dlam(const float* __restrict__ part, int64_t rows, int32_t D, const float* __restrict__ lam,
-                         float* __restrict__ out) {
+__global__ void glr_dlam(const float* part, int64_t rows, int32_t D, const float* lam, float* out) {
   tc::after_previous();
   __shared__ float sh[32][33];
   const int d = blockIdx.x * 32 + threadIdx.x;

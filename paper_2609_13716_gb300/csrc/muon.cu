@@ -112,10 +112,12 @@ __device__ __forceinline__ bool fours(const Common& c, const Ptrs& p, int k, int
   }
   return low == 0 && (ld & 3) == 0;
 }
+// (An ordinary load: the kernel before may still be writing the input when this one starts, see
+// tc::after_previous(), and the read-only path is for data that nobody writes meanwhile.)
 __device__ __forceinline__ float4 load_in4(const Common& c, const Ptrs& p, int k, int64_t r, int64_t col) {
   const int64_t at = r * p.ld_in[k] + col;
-  if (!c.bf16_in) return __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p.in[k]) + at));
-  const uint2 w = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p.in[k]) + at));
+  if (!c.bf16_in) return *reinterpret_cast<const float4*>(static_cast<const float*>(p.in[k]) + at);
+  const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p.in[k]) + at);
   return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
                      __uint_as_float(w.y & 0xFFFF0000u));
 }

@@ -207,7 +207,8 @@ __device__ __forceinline__ bool elect_one() {
 
 // First statement of a kernel launched with programmatic stream serialization: it may start while the
 // one before it in the stream drains, lets the next one do so, and reads and writes nothing before
-// all of that one's work is done and visible.
+// all of that one's work is done and visible.  Its loads are ordinary ones: the read-only path
+// (__ldg, const __restrict__) is for data that nobody writes from the kernel's start on.
 __device__ __forceinline__ void after_previous() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
