@@ -86,7 +86,7 @@ struct Common {
   const Mat* mats;
   uint8_t* ws;
   double* norm;                                // [n_mats][kNormBlocks]
-  float* inv;                                  // [n_mats] 1 / (||U||_F + eps)
+  float2* inv;                                 // [n_mats] of inverse_norm
   uint32_t* summed;                            // [n_mats] blocks of momentum_norm that are through, 0 between calls
   uint32_t* done;                              // [n_mats][3 phases][kMaxSteps] finished tiles
   uint32_t* status;
@@ -126,6 +126,28 @@ __device__ __forceinline__ float u_of(const Common& c, float g, float mom) {
   return !c.update ? g : c.nesterov ? fmaf(c.mu, mom, g) : mom;
 }
 
+// Squares of a few values (at most 64) are summed in fp32 and added up in fp64.  Outside of 2^-60 to
+// 2^60 their squares would leave fp32's range, or lose bits below it; a group whose largest is there
+// is squared in fp64 (slow, so only there).
+__device__ __forceinline__ bool fp32_squares(float largest) {
+  return largest == 0.0f || (largest >= 0x1p-60f && largest <= 0x1p60f);
+}
+__device__ __forceinline__ float largest4(float m, float4 v) {
+  return fmaxf(fmaxf(m, fmaxf(fabsf(v.x), fabsf(v.y))), fmaxf(fabsf(v.z), fabsf(v.w)));
+}
+__device__ __forceinline__ double square64(float v) { return (double)v * (double)v; }
+__device__ __forceinline__ double squares64(float4 v) {
+  return (square64(v.x) + square64(v.y)) + (square64(v.z) + square64(v.w));
+}
+// kSX / (||U||_F + eps) as a power of two and the rest, x and y with u * x * y in range for every u of
+// U: the norm may lie beyond fp32's largest value, and its inverse too.
+__device__ __forceinline__ float2 inverse_norm(double sum_sq, float eps) {
+  const double d = sqrt(sum_sq) + (double)eps;
+  const int e = min(126, max(-126, (__double2hiint(d) >> 20 & 0x7FF) - 1023));
+  const float x = __int_as_float((127 - e) << 23);
+  return make_float2(x, (float)(1.0 / (d * (double)x)) * kSX);
+}
+
 // ---- momentum and the sum of squares of U ------------------------------------------------
 // Also clears the tile counters of the call.  A thread takes four groups of four columns at a
 // time (their loads in flight together) where the rows allow it, else single elements.  Bound by
@@ -158,7 +180,7 @@ __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Com
           }
         }
       }
-      float part = 0.0f;                       // 16 squares in fp32, the rest in fp64
+      float part = 0.0f, largest = 0.0f;       // 16 squares in fp32, the rest in fp64
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         if (mp[x]) {
@@ -166,11 +188,17 @@ __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Com
                              fmaf(c.mu, o[x].w, g[x].w));
           *reinterpret_cast<float4*>(mp[x]) = o[x];
         }
-        const float ux = u_of(c, g[x].x, o[x].x), uy = u_of(c, g[x].y, o[x].y), uz = u_of(c, g[x].z, o[x].z),
-                    uw = u_of(c, g[x].w, o[x].w);
-        part += (ux * ux + uy * uy) + (uz * uz + uw * uw);
+        g[x] = make_float4(u_of(c, g[x].x, o[x].x), u_of(c, g[x].y, o[x].y), u_of(c, g[x].z, o[x].z),
+                           u_of(c, g[x].w, o[x].w));
+        part += (g[x].x * g[x].x + g[x].y * g[x].y) + (g[x].z * g[x].z + g[x].w * g[x].w);
+        largest = largest4(largest, g[x]);
       }
-      sum += part;
+      if (fp32_squares(largest)) {
+        sum += part;
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) sum += squares64(g[x]);
+      }
     }
   } else {
     const uint32_t total = rows * cols;
@@ -186,7 +214,8 @@ __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Com
         *mp = mom;
       }
       const float u = u_of(c, g, mom);
-      part += u * u;
+      if (fp32_squares(fabsf(u))) part += u * u;
+      else sum += square64(u);
       if (++held == 16) {
         sum += part;
         part = 0.0f;
@@ -220,7 +249,7 @@ __global__ void __launch_bounds__(256) momentum_norm(const __grid_constant__ Com
   for (int i = threadIdx.x; i < blocks; i += 256) all += __ldcg(&c.norm[k * kNormBlocks + i]);
   all = block_sum(all);
   if (threadIdx.x == 0) {
-    c.inv[k] = (float)(1.0 / (sqrt(all) + (double)c.eps));
+    c.inv[k] = inverse_norm(all, c.eps);
     c.summed[k] = 0;
   }
 }
@@ -253,7 +282,7 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
   const Mat m = c.mats[k];
   const int64_t chunks = (int64_t)m.mb * m.nb * 2048;
   if ((int64_t)blockIdx.x * 256 >= chunks) return;
-  const float inv = c.inv[k];
+  const float2 inv = c.inv[k];
   uint8_t* x = c.ws + m.x[0];
   const bool four = !m.tall && fours(c, p, k, m.cols);
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < chunks; q += (int64_t)gridDim.x * 256) {
@@ -274,7 +303,7 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
       const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
       const float o[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (u_of(c, g[e], o[e]) * inv) * kSX;
+      for (int e = 0; e < 8; ++e) v[e] = (u_of(c, g[e], o[e]) * inv.x) * inv.y;
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -283,7 +312,7 @@ __global__ void __launch_bounds__(256) normalise(const __grid_constant__ Common 
         if (i < m.m && j < m.n) {
           const int64_t row = m.tall ? j : i, col = m.tall ? i : j;
           const float mom = c.update ? p.mom[k][row * p.ld_mom[k] + col] : 0.0f;
-          v[e] = (u_of(c, load_in(c, p, k, row, col), mom) * inv) * kSX;
+          v[e] = (u_of(c, load_in(c, p, k, row, col), mom) * inv.x) * inv.y;
         }
       }
     }
@@ -853,7 +882,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   __shared__ __align__(8) uint64_t done_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ double norm_s[kSmallThreads / 32];
-  __shared__ float inv_s;
+  __shared__ float2 inv_s;
   uint8_t *xs = smem, *ss = smem + 2 * kBlk, *parts = ss + kStaged;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int k = (int)blockIdx.x / cluster, rank = (int)blockIdx.x % cluster;
@@ -962,7 +991,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   // Momentum, U and its norm; X = U / (||U||_F + eps).  A wide matrix is read along its rows (a
   // warp 16 rows, a lane 4 columns of each) through a staged copy; a tall one's rows are columns
   // of X, and neighbouring threads, rows of X, read neighbouring elements.
-  float sq = 0.0f;                             // 64 squares a thread, the rest in fp64
+  float sq = 0.0f, largest = 0.0f;             // 64 squares a thread, the rest in fp64
   if (!tall) {
     const bool four = fours(c, p, k, cols);
     const int c0 = rank * kB + 4 * lane;       // first column of this lane
@@ -1008,6 +1037,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         const float4 u = make_float4(u_of(c, g[x].x, o[x].x), u_of(c, g[x].y, o[x].y), u_of(c, g[x].z, o[x].z),
                                      u_of(c, g[x].w, o[x].w));
         sq += (u.x * u.x + u.y * u.y) + (u.z * u.z + u.w * u.w);
+        largest = largest4(largest, u);
         *reinterpret_cast<float4*>(at4(ss, row, lane)) = u;
       }
     }
@@ -1029,10 +1059,21 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
         if (mp && e < left) mp[e * step_m] = mom[e];
         f[b + e] = u_of(c, f[b + e], mom[e]);
         sq += f[b + e] * f[b + e];
+        largest = fmaxf(largest, fabsf(f[b + e]));
       }
     }
   }
   double warp_sq = sq;
+  if (!fp32_squares(largest)) {
+    warp_sq = 0.0;
+    if (!tall) {                               // this thread's own values of the staged copy
+      for (int row = 16 * warp; row < 16 * warp + 16; ++row)
+        warp_sq += squares64(*reinterpret_cast<const float4*>(at4(ss, row, lane)));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 64; ++e) warp_sq += square64(f[e]);
+    }
+  }
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) warp_sq += __shfl_xor_sync(0xFFFFFFFFu, warp_sq, x);
   if (lane == 0) norm_s[warp] = warp_sq;
@@ -1047,13 +1088,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     const double mine = lane < nb ? peer_load_f64(peer_addr(&norm_s[0], lane)) : 0.0;
     double t = 0.0;
     for (int q = 0; q < nb; ++q) t += __shfl_sync(0xFFFFFFFFu, mine, q);
-    if (lane == 0) inv_s = (float)(1.0 / (sqrt(t) + (double)c.eps));  // (once: 64-bit arithmetic is slow)
+    if (lane == 0) inv_s = inverse_norm(t, c.eps);  // (once: 64-bit arithmetic is slow)
   }
   __syncthreads();
   if (!tall) unstage(ss);
-  const float inv = inv_s;
+  const float2 inv = inv_s;
 #pragma unroll
-  for (int e = 0; e < 64; ++e) f[e] = (f[e] * inv) * kSX;
+  for (int e = 0; e < 64; ++e) f[e] = (f[e] * inv.x) * inv.y;
   if (on) split_to(xs);
 
   // rows of the Gram matrix this CTA sums for all
@@ -1212,7 +1253,7 @@ struct aht_muon {
   int paired = 0;                // two of them in a cluster, to share items
   uint8_t* ws = nullptr;
   double* norm = nullptr;
-  float* inv = nullptr;
+  float2* inv = nullptr;
   uint32_t* summed = nullptr;
   uint32_t* status = nullptr;
   std::vector<void*> owned;
@@ -1425,7 +1466,7 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
   s->n_items = (int)items.size();
   if (!up((void**)&s->d_mats, s->mats.data(), s->mats.size() * sizeof(Mat)) || !alloc((void**)&s->ws, (size_t)at) ||
       (s->n_items && !up((void**)&s->items, items.data(), items.size() * sizeof(int4))) ||
-      !alloc((void**)&s->norm, (size_t)n * kNormBlocks * sizeof(double)) || !alloc((void**)&s->inv, (size_t)n * 4) ||
+      !alloc((void**)&s->norm, (size_t)n * kNormBlocks * sizeof(double)) || !alloc((void**)&s->inv, (size_t)n * sizeof(float2)) ||
       !alloc((void**)&s->summed, (size_t)n * 4) || cudaMemset(s->summed, 0, (size_t)n * 4) != cudaSuccess ||
       !alloc((void**)&s->done, (size_t)n * 3 * kMaxSteps * 4) || !alloc((void**)&s->status, 4) ||
       cudaMemset(s->status, 0, 4) != cudaSuccess)
