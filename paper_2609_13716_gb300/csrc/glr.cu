@@ -108,24 +108,50 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t x) {
   tc::f2_unpack(tc::f2_add(tc::f2_pack(tc::ex2_approx(a), tc::ex2_approx(b)), both(1.0f)), a, b);
   return tc::f2_pack(tc::rcp_approx(a), tc::rcp_approx(b));
 }
-// exp(z) - 1 for z <= 0: down to -1/4 its series z (1 + z/2 + z^2/6 + ... + z^6/5040) (the
-// next term is below 2^-26 there), beyond it 2^(z log2 e) - 1 (no cancellation).  kSmall: no
-// z of the warp lies beyond.
+// The decay a = exp(z) for z <= 0, and a - 1.  Down to z = -1/4 a - 1 is its series
+// z (1 + z/2 + z^2/6 + ... + z^6/5040) (the next term is below 2^-26 there) and a the sum; beyond
+// it a is 2^(z log2 e) and a - 1 the difference: rounded the other way round, 1 + (a - 1) would hold
+// a small a to 3e-8 of 1 instead of itself (with lam = 4 dr was off by 2e-6 of its norm).
+// a is never 0, which stands for a reset: at least 2^-149.  kSmall: no z of the warp lies beyond.
+struct Decay {
+  uint64_t a, em;   // a, a - 1
+  uint64_t kept;    // both in one: a - 1 (0 or negative) down to z = -1/4, a (positive) beyond
+};
 template <bool kSmall>
-__device__ __forceinline__ uint64_t decay_m1(uint64_t z) {
+__device__ __forceinline__ Decay decay(uint64_t z) {
   uint64_t s = tc::f2_fma(z, both(1.0f / 5040.0f), both(1.0f / 720.0f));
   s = tc::f2_fma(z, s, both(1.0f / 120.0f));
   s = tc::f2_fma(z, s, both(1.0f / 24.0f));
   s = tc::f2_fma(z, s, both(1.0f / 6.0f));
   s = tc::f2_fma(z, s, both(0.5f));
   s = tc::f2_mul(z, tc::f2_fma(z, s, both(1.0f)));
-  if (kSmall) return s;
-  float z0, z1, s0, s1, a, b;
+  const uint64_t near = tc::f2_add(s, both(1.0f));
+  if (kSmall) return Decay{near, s, s};
+  float z0, z1, s0, s1, n0, n1, a, b, am, bm;
   tc::f2_unpack(z, z0, z1);
   tc::f2_unpack(s, s0, s1);
+  tc::f2_unpack(near, n0, n1);
   tc::f2_unpack(tc::f2_mul(z, both(kLog2e)), a, b);
-  tc::f2_unpack(tc::f2_add(tc::f2_pack(tc::ex2_approx(a), tc::ex2_approx(b)), both(-1.0f)), a, b);
-  return tc::f2_pack(z0 > -0.25f ? s0 : a, z1 > -0.25f ? s1 : b);
+  // (of 0 and positive numbers the integers are in the same order; NaN is above all)
+  a = __int_as_float(max(__float_as_int(tc::ex2_approx(a)), 1));
+  b = __int_as_float(max(__float_as_int(tc::ex2_approx(b)), 1));
+  tc::f2_unpack(tc::f2_add(tc::f2_pack(a, b), both(-1.0f)), am, bm);
+  const bool c0 = z0 > -0.25f, c1 = z1 > -0.25f;
+  return Decay{tc::f2_pack(c0 ? n0 : a, c1 ? n1 : b), tc::f2_pack(c0 ? s0 : am, c1 ? s1 : bm),
+               tc::f2_pack(c0 ? s0 : a, c1 ? s1 : b)};
+}
+// a and a - 1 of what was kept.
+template <bool kSmall>
+__device__ __forceinline__ float kept_a(float k) {
+  return !kSmall && k > 0.0f ? k : k + 1.0f;
+}
+template <bool kSmall>
+__device__ __forceinline__ uint64_t kept_m1(uint64_t k) {
+  if (kSmall) return k;
+  float k0, k1, m0, m1;
+  tc::f2_unpack(k, k0, k1);
+  tc::f2_unpack(tc::f2_add(k, both(-1.0f)), m0, m1);
+  return tc::f2_pack(k0 > 0.0f ? m0 : k0, k1 > 0.0f ? m1 : k1);
 }
 // beta^2 = 1 - a^2 = em (-2 - em)
 __device__ __forceinline__ uint64_t beta_sq(uint64_t em) { return tc::f2_mul(em, tc::f2_fma(em, both(-1.0f), both(-2.0f))); }
@@ -435,13 +461,13 @@ __global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 
       for (int e = 0; e < kE; e += 2) {
         const int k0 = e / V, v0 = e % V, k1 = (e + 1) / V, v1 = (e + 1) % V;
         const uint64_t rho = sigmoid2(tc::f2_pack(nr[k0].get(v0), nr[k1].get(v1)));
-        const uint64_t em = decay_m1<decltype(small_c)::value>(tc::f2_mul(tc::f2_pack(m[v0], m[v1]), rho));
+        const Decay q = decay<decltype(small_c)::value>(tc::f2_mul(tc::f2_pack(m[v0], m[v1]), rho));
         const uint64_t iota = sigmoid2(tc::f2_pack(ni[k0].get(v0), ni[k1].get(v1)));
         float b0, b1;
-        tc::f2_unpack(beta_sq(em), b0, b1);
+        tc::f2_unpack(beta_sq(q.em), b0, b1);
         const uint64_t ix = tc::f2_mul(iota, tc::f2_pack(nx[k0].get(v0), nx[k1].get(v1)));
         tc::f2_unpack(tc::f2_mul(tc::f2_pack(sqrt_q(b0), sqrt_q(b1)), ix), b[e], b[e + 1]);
-        tc::f2_unpack(tc::f2_add(em, both(1.0f)), da[e], da[e + 1]);
+        tc::f2_unpack(q.a, da[e], da[e + 1]);
       }
     };
     if (small) gate(std::true_type());
@@ -670,49 +696,47 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
       if (!b.dh.p) q.zero();
       return q;
     };
-    float em[kE], rho[kE], iota[kE], prev[kE], p[V];
+    float kept[kE], rho[kE], iota[kE], prev[kE], p[V];  // kept: of the decay, see Decay
+    float A[V], P[V];
     const uint32_t rs = __ballot_sync(0xFFFFFFFFu, nrs != 0);
     const bool plain = rs == 0 && t0 + S <= at.len;  // no masks needed
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = nc[v];
-    // gates; prev holds beta iota x until the states are rebuilt
-    auto gate = [&](auto small_c) {
-#pragma unroll
-      for (int e = 0; e < kE; e += 2) {
-        const int k0 = e / V, v0 = e % V, k1 = (e + 1) / V, v1 = (e + 1) % V;
-        const uint64_t rh = sigmoid2(tc::f2_pack(nr[k0].get(v0), nr[k1].get(v1)));
-        const uint64_t z = decay_m1<decltype(small_c)::value>(tc::f2_mul(tc::f2_pack(m[v0], m[v1]), rh));
-        const uint64_t io = sigmoid2(tc::f2_pack(ni[k0].get(v0), ni[k1].get(v1)));
-        float b0, b1;
-        tc::f2_unpack(beta_sq(z), b0, b1);
-        const uint64_t ix = tc::f2_mul(io, tc::f2_pack(x_of(k0).get(v0), x_of(k1).get(v1)));
-        tc::f2_unpack(tc::f2_mul(tc::f2_pack(sqrt_q(b0), sqrt_q(b1)), ix), prev[e], prev[e + 1]);
-        tc::f2_unpack(rh, rho[e], rho[e + 1]);
-        tc::f2_unpack(io, iota[e], iota[e + 1]);
-        tc::f2_unpack(z, em[e], em[e + 1]);
-      }
-    };
-    if (small) gate(std::true_type());
-    else gate(std::false_type());
     auto refill = [&]() {
       __syncwarp();                       // every lane has read the slot
       fetch_ring(t0 - kRing * window, slot);
       slot = slot + 1 == kRing ? 0 : slot + 1;
     };
-    if (kRing) {
-      nrs = w > 1 ? reset_byte<S>(a, at, t0 - window, lane) : (uint8_t)0;
-      if (V == 1) refill();
-    }
+    // gates (prev holds beta iota x until the states are rebuilt), the states, the segment's map
+    auto rebuild = [&](auto small_c) {
+      constexpr bool kSmall = decltype(small_c)::value;
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const int k = e / V, v = e % V;
-      const float in = prev[e];
-      if (!plain && ((rs >> k) & 1u)) p[v] = 0.0f;
-      prev[e] = p[v];
-      p[v] = fmaf(p[v], em[e], p[v]) + in;
-    }
-    if (WT > 1 || kCluster) {
-      float A[V], P[V];
+      for (int e = 0; e < kE; e += 2) {
+        const int k0 = e / V, v0 = e % V, k1 = (e + 1) / V, v1 = (e + 1) % V;
+        const uint64_t rh = sigmoid2(tc::f2_pack(nr[k0].get(v0), nr[k1].get(v1)));
+        const Decay q = decay<kSmall>(tc::f2_mul(tc::f2_pack(m[v0], m[v1]), rh));
+        const uint64_t io = sigmoid2(tc::f2_pack(ni[k0].get(v0), ni[k1].get(v1)));
+        float b0, b1;
+        tc::f2_unpack(beta_sq(q.em), b0, b1);
+        const uint64_t ix = tc::f2_mul(io, tc::f2_pack(x_of(k0).get(v0), x_of(k1).get(v1)));
+        tc::f2_unpack(tc::f2_mul(tc::f2_pack(sqrt_q(b0), sqrt_q(b1)), ix), prev[e], prev[e + 1]);
+        tc::f2_unpack(rh, rho[e], rho[e + 1]);
+        tc::f2_unpack(io, iota[e], iota[e + 1]);
+        tc::f2_unpack(q.kept, kept[e], kept[e + 1]);
+      }
+      if (kRing) {
+        nrs = w > 1 ? reset_byte<S>(a, at, t0 - window, lane) : (uint8_t)0;
+        if (V == 1) refill();
+      }
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const int k = e / V, v = e % V;
+        const float in = prev[e];
+        if (!plain && ((rs >> k) & 1u)) p[v] = 0.0f;
+        prev[e] = p[v];
+        p[v] = fmaf(p[v], kept_a<kSmall>(kept[e]), in);  // (the forward pass's own bits)
+      }
+      if (WT == 1 && !kCluster) return;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         A[v] = 1.0f;
@@ -721,7 +745,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
 #pragma unroll
       for (int e = kE - 1; e >= 0; --e) {
         const int k = e / V, v = e % V;
-        const float d = 1.0f + em[e];
+        const float d = kept_a<kSmall>(kept[e]);
         if (plain) {
           P[v] = d * (g_of(k).get(v) + P[v]);
           A[v] *= d;
@@ -731,6 +755,10 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
           A[v] = cut ? 0.0f : A[v] * d;
         }
       }
+    };
+    if (small) rebuild(std::true_type());
+    else rebuild(std::false_type());
+    if (WT > 1 || kCluster) {
       X::run(sh, n, rank, n_rank, wt, lane, A, P, carry, p);
     } else {
 #pragma unroll
@@ -740,18 +768,19 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
 #pragma unroll
     for (int v = 0; v < V; ++v) part[v] = 0.0f;
     Walk wdx(b.dx, pdx, sizeof(E), t0 + S - 1), wdr(b.dr, pdr, sizeof(E), t0 + S - 1), wdi(b.di, pdi, sizeof(E), t0 + S - 1);
-    auto grads = [&](auto plain_c) {
-      constexpr bool kPlain = decltype(plain_c)::value;
+    auto grads = [&](auto plain_c, auto small_c) {
+      constexpr bool kPlain = decltype(plain_c)::value, kSmall = decltype(small_c)::value;
 #pragma unroll
       for (int e = kE - 2; e >= 0; e -= 2) {
         const int k0 = e / V, v0 = e % V, k1 = (e + 1) / V, v1 = (e + 1) % V;
         // With G = dL/dh: dx = c1 G, di = c2 dx, w = -q a dL/da = c3 G, dr = c4 w, all but G
         // known before the scan.  1 / beta stays finite where beta = 0 (dx is 0 there, and
         // q / beta -> 0 with q).
-        const uint64_t z = tc::f2_pack(em[e], em[e + 1]), rh = tc::f2_pack(rho[e], rho[e + 1]);
+        const float d0 = kept_a<kSmall>(kept[e]), d1 = kept_a<kSmall>(kept[e + 1]);
+        const uint64_t z = kept_m1<kSmall>(tc::f2_pack(kept[e], kept[e + 1])), rh = tc::f2_pack(rho[e], rho[e + 1]);
         const uint64_t io = tc::f2_pack(iota[e], iota[e + 1]), xx = tc::f2_pack(x_of(k0).get(v0), x_of(k1).get(v1));
-        const uint64_t d = tc::f2_add(z, both(1.0f)), b2 = beta_sq(z);
-        float s0, s1, d0, d1;
+        const uint64_t d = tc::f2_pack(d0, d1), b2 = beta_sq(z);
+        float s0, s1;
         tc::f2_unpack(b2, s0, s1);
         const uint64_t inv = tc::f2_pack(rsqrt_q(fmaxf(s0, 1e-37f)), rsqrt_q(fmaxf(s1, 1e-37f)));
         const uint64_t c1 = tc::f2_mul(io, tc::f2_mul(b2, inv)), c2 = tc::f2_mul(xx, tc::f2_fma(io, both(-1.0f), both(1.0f)));
@@ -759,7 +788,6 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         const uint64_t c3 = tc::f2_mul(tc::f2_mul(d, nq),
                                        tc::f2_sub(tc::f2_pack(prev[e], prev[e + 1]), tc::f2_mul(tc::f2_mul(inv, d), tc::f2_mul(io, xx))));
         const uint64_t c4 = tc::f2_fma(rh, both(-1.0f), both(1.0f));
-        tc::f2_unpack(d, d0, d1);
         const bool live0 = kPlain || t0 + k0 < at.len, live1 = kPlain || t0 + k1 < at.len;
         const bool cut0 = !kPlain && ((rs >> k0) & 1u), cut1 = !kPlain && ((rs >> k1) & 1u);
         // the scan: element e + 1 is a later step (V = 1) or another channel
@@ -808,8 +836,13 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         }
       }
     };
-    if (plain) grads(std::true_type());
-    else grads(std::false_type());
+    if (small) {
+      if (plain) grads(std::true_type(), std::true_type());
+      else grads(std::false_type(), std::true_type());
+    } else {
+      if (plain) grads(std::true_type(), std::false_type());
+      else grads(std::false_type(), std::false_type());
+    }
     if (kRing && V > 1) refill();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
