@@ -414,7 +414,8 @@ aht_status aht_s5_sync(aht_s5* s);
  *   s = 8 softplus(lam),  rho = sigmoid(r_t),  iota = sigmoid(i_t),
  *   a_t = exp(-s rho),  beta_t = sqrt(1 - a_t^2),
  *   h_t = a_t h_{t-1} + beta_t iota_t x_t,   without the first term where reset_t is set.
- * A reset drops the earlier state whatever it holds, NaN included.  Env n has lengths[n]
+ * A reset, and nothing else, drops the earlier state whatever it holds, NaN included: what is
+ * not finite comes through any decay, however a call splits the steps.  Env n has lengths[n]
  * steps (clamped to 0..T; NULL: all T): from there on h is written as 0, the inputs are not
  * used (they may hold anything), the state stays and the gradients are 0.
  * x, r, i, h and their gradients are fp32 or bf16, element (t, n, d) of a sequence at

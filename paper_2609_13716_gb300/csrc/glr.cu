@@ -15,8 +15,9 @@
 // receives, p -> A p + P with the same A.
 //
 // State, gates and sums are fp32 whatever the tensors' type; each output is rounded once.
-// Where a segment's map has A = 0 (a reset in it, or a decay that underflowed) it drops what it
-// receives, NaN and infinity included.
+// A = 0 stands for a reset in the segment and for nothing else: it drops what it receives, NaN and
+// infinity included.  A decay, or a product of them, that underflows stays at 2^-149 instead, so
+// that what is not finite comes through whether the steps are split or not.
 //
 // The backward pass needs the state before every step.  The forward pass leaves it as fp32
 // checkpoints every kSeg = 8 steps (0.5 B per element; the rounded h would cost 2-4 B and
@@ -108,11 +109,14 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t x) {
   tc::f2_unpack(tc::f2_add(tc::f2_pack(tc::ex2_approx(a), tc::ex2_approx(b)), both(1.0f)), a, b);
   return tc::f2_pack(tc::rcp_approx(a), tc::rcp_approx(b));
 }
+// A decay or a product of them, which is not to become 0.  (Of 0 and positive numbers the integers are
+// in the same order; NaN is above all.)
+__device__ __forceinline__ float not_zero(float a) { return __int_as_float(max(__float_as_int(a), 1)); }
 // The decay a = exp(z) for z <= 0, and a - 1.  Down to z = -1/4 a - 1 is its series
 // z (1 + z/2 + z^2/6 + ... + z^6/5040) (the next term is below 2^-26 there) and a the sum; beyond
 // it a is 2^(z log2 e) and a - 1 the difference: rounded the other way round, 1 + (a - 1) would hold
 // a small a to 3e-8 of 1 instead of itself (with lam = 4 dr was off by 2e-6 of its norm).
-// a is never 0, which stands for a reset: at least 2^-149.  kSmall: no z of the warp lies beyond.
+// kSmall: no z of the warp lies beyond.
 struct Decay {
   uint64_t a, em;   // a, a - 1
   uint64_t kept;    // both in one: a - 1 (0 or negative) down to z = -1/4, a (positive) beyond
@@ -132,9 +136,8 @@ __device__ __forceinline__ Decay decay(uint64_t z) {
   tc::f2_unpack(s, s0, s1);
   tc::f2_unpack(near, n0, n1);
   tc::f2_unpack(tc::f2_mul(z, both(kLog2e)), a, b);
-  // (of 0 and positive numbers the integers are in the same order; NaN is above all)
-  a = __int_as_float(max(__float_as_int(tc::ex2_approx(a)), 1));
-  b = __int_as_float(max(__float_as_int(tc::ex2_approx(b)), 1));
+  a = not_zero(tc::ex2_approx(a));
+  b = not_zero(tc::ex2_approx(b));
   tc::f2_unpack(tc::f2_add(tc::f2_pack(a, b), both(-1.0f)), am, bm);
   const bool c0 = z0 > -0.25f, c1 = z1 > -0.25f;
   return Decay{tc::f2_pack(c0 ? n0 : a, c1 ? n1 : b), tc::f2_pack(c0 ? s0 : am, c1 ? s1 : bm),
@@ -165,7 +168,7 @@ __device__ __forceinline__ float rsqrt_q(float x) {
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// A y + b, or b alone where A is 0.
+// A y + b, or b alone where A is 0: after a reset.
 __device__ __forceinline__ float apply(float A, float y, float b) { return A == 0.0f ? b : fmaf(A, y, b); }
 
 // Where a warp works: its env, its channels, its segment of a window of steps.
@@ -315,12 +318,23 @@ struct Exchange {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         ch[v] = apply(wa[w][v], ch[v], wh[w][v]);
-        ca[v] = wa[w][v] == 0.0f ? 0.0f : ca[v] * wa[w][v];
+        ca[v] *= wa[w][v];
+      }
+    };
+    // (the product may underflow on its way, or pass NaN on to a reset: 0 where a map has one, not 0 else)
+    auto end = [&](float* ca, int n_w) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        bool cut = false;
+#pragma unroll
+        for (int w = 0; w < WT; ++w) cut = cut || (w < n_w && wa[w][v] == 0.0f);
+        ca[v] = cut ? 0.0f : not_zero(ca[v]);
       }
     };
 #pragma unroll
     for (int w = 0; w < WT; ++w)
       if (w < wt) then(pa, ph, w);
+    end(pa, wt);
     if (kCluster) {
       if (wt == WT - 1) {  // the last warp has the CTA's map: to every CTA of the cluster
         float t[2 * V];
@@ -330,6 +344,7 @@ struct Exchange {
           t[V + v] = ph[v];
         }
         then(t, t + V, WT - 1);
+        end(t, WT);
         if (lane == 0) tc::mbar_expect_tx(&sh.bar[buf], (uint32_t)n_rank * 32u * 2u * V * 4u);
         for (int dst = 0; dst < n_rank; ++dst) send(&sh.c[buf][rank][lane][0], t, &sh.bar[buf], dst);
       }
@@ -506,9 +521,11 @@ __global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 
 #pragma unroll
         for (int e = V; e < kE; ++e) {
           H[e % V] = apply(da[e], H[e % V], b[e]);
-          A[e % V] = da[e] == 0.0f ? 0.0f : A[e % V] * da[e];
+          A[e % V] *= da[e];
         }
       }
+#pragma unroll
+      for (int v = 0; v < V; ++v) A[v] = rs ? 0.0f : not_zero(A[v]);
       X::run(sh, n, rank, n_rank, wt, lane, A, H, carry, y);
     } else {
 #pragma unroll
@@ -752,9 +769,11 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
         } else if (t0 + k < at.len) {
           const bool cut = (rs >> k) & 1u;
           P[v] = cut ? 0.0f : d * (g_of(k).get(v) + P[v]);
-          A[v] = cut ? 0.0f : A[v] * d;
+          A[v] *= d;
         }
       }
+#pragma unroll
+      for (int v = 0; v < V; ++v) A[v] = rs ? 0.0f : not_zero(A[v]);
     };
     if (small) rebuild(std::true_type());
     else rebuild(std::false_type());
