@@ -455,6 +455,17 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
 aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_seq* dh, const float* dh_last,
                             const aht_seq* dx, const aht_seq* dr, const aht_seq* di, float* dlam, float* dh0,
                             void* workspace, int64_t workspace_bytes, void* cuda_stream);
+/* Where few lanes have their steps split over a cluster of CTAs, a CTA waits for the others' (at most
+ * 2 s).  A wait that runs out makes NaN of the state, or of the gradient, that the steps behind it
+ * would receive, up to their next reset, and of h_last or dh0; the pass ends.  aht_glr_sync waits for
+ * the stream and returns AHT_ETIMEOUT if that happened in any pass on the current device since its
+ * last call. */
+aht_status aht_glr_sync(void* cuda_stream);
+/* Failure-detection hook (no paper counterpart), process-wide: in the next pass that is split over a
+ * cluster, CTA 0 of every cluster waits at its window `window` (128 steps or more each) for what nothing
+ * sends, and every wait of the pass is limited to limit_ns (1 .. 10^9).  The hook fires once;
+ * window < 0 clears it.  No fault, no hang. */
+aht_status aht_debug_glr_expire(int32_t window, int64_t limit_ns);
 
 /* ---- Orthogonalised matrix updates (optimiser of a policy's hidden matrices) ------------
  * The Muon update (Jordan et al. 2024) of a fixed set of weight matrices W [rows][cols]:

@@ -29,7 +29,8 @@ EXPORTED = ["aht_create", "aht_destroy", "aht_reset", "aht_rollout", "aht_xplay_
             "aht_ppo_update", "aht_ppo_grad", "aht_learner_get", "aht_learner_set",
             "aht_learner_push", "aht_learner_sync", "aht_rollout_ippo", "aht_rollout_resample",
             "aht_s5_create", "aht_s5_destroy", "aht_s5_step", "aht_s5_sync", "aht_traj_copy",
-            "aht_glr_ckpt_elems", "aht_glr_workspace", "aht_glr_forward", "aht_glr_backward", "aht_muon_create", "aht_muon_destroy",
+            "aht_glr_ckpt_elems", "aht_glr_workspace", "aht_glr_forward", "aht_glr_backward", "aht_glr_sync",
+            "aht_debug_glr_expire", "aht_muon_create", "aht_muon_destroy",
             "aht_muon_step", "aht_muon_orthogonalize", "aht_muon_sync"]
 
 
@@ -132,6 +133,10 @@ def load() -> C.CDLL:
             L.aht_glr_forward.restype = C.c_int
             L.aht_glr_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
             L.aht_glr_backward.restype = C.c_int
+            L.aht_glr_sync.argtypes = [vp]
+            L.aht_glr_sync.restype = C.c_int
+            L.aht_debug_glr_expire.argtypes = [i32, i64]
+            L.aht_debug_glr_expire.restype = C.c_int
             L.aht_muon_create.argtypes = [i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(MuonConfig), vp, C.POINTER(vp)]
             L.aht_muon_destroy.argtypes = [vp]
             L.aht_muon_destroy.restype = None
@@ -782,6 +787,18 @@ def aht_glr_backward(x, r, i, lam, ckpt, dh, dx, dr, di, dlam=None, workspace=No
                                    _ptr(dlam, f32, (D,), "dlam"),
                                    _ptr(dh0, f32, (N, D), "dh0"), ws, 0 if workspace is None else workspace.numel(),
                                    _stream(stream)))
+
+
+def aht_glr_sync(stream=None):
+    """Waits for the stream; raises AhtError with AHT_ETIMEOUT if a bounded wait of a split pass on this
+    device expired since the last call (its results are NaN from there on)."""
+    _check(load().aht_glr_sync(_stream(stream)))
+
+
+def aht_debug_glr_expire(window: int, limit_ns: int):
+    """Failure hook: the next pass split over a cluster waits in vain at its window ``window`` (bounded by
+    limit_ns); ``window < 0`` clears it."""
+    _check(load().aht_debug_glr_expire(window, limit_ns))
 
 
 # ---- orthogonalised matrix updates -------------------------------------------------------

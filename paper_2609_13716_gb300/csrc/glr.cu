@@ -27,6 +27,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "kernels.h"
@@ -44,6 +45,14 @@ namespace {
 constexpr int kSeg = AHT_GLR_SEGMENT;  // steps between two checkpoints
 constexpr float kGateScale = 8.0f;     // s = 8 softplus(lam)
 constexpr int kMaxCluster = 16;
+
+// Limit of a wait for a window's maps, and the window at which the failure hook has CTA 0 of every
+// cluster wait for nothing (none: ~0).
+struct Waits {
+  uint64_t limit_ns;
+  uint32_t expire_at;
+};
+__device__ uint32_t glr_status;        // kStatus* bits since the last aht_glr_sync
 
 struct Seq {
   void* p;
@@ -254,25 +263,37 @@ __device__ __forceinline__ uint8_t reset_byte(const GlrDev& a, const Place& at, 
 // threads have in flight (a sixth of the stalls).  Two buffers suffice: a CTA sends for window
 // w + 2 after it has everyone's maps of w + 1, which each CTA sends after all its warps have
 // read w.
+//
+// A wait that runs out is for good: from that window on the thread takes NaN for the state it would
+// receive, sends nothing (its buffers may still be unread elsewhere) and waits for nothing, so the
+// other CTAs' waits run out in turn and the whole pass ends.  What it computes from its own steps
+// alone (after a reset among them) stays right.
 template <int V, int WT, bool kCluster>
 struct Exchange {
   struct Shared {
     float a[2][WT][32][V], h[2][WT][32][V];   // maps of the CTA's warps
     alignas(16) float c[2][kMaxCluster][32][2 * V];  // maps of the cluster's CTAs: A, then H
     alignas(8) uint64_t bar[2];
+    uint64_t never;
   };
   __device__ __forceinline__ static void init(Shared& sh) {
     if (!kCluster) return;
     if (threadIdx.x == 0) {
       tc::mbar_init(&sh.bar[0], 1);
       tc::mbar_init(&sh.bar[1], 1);
+      tc::mbar_init(&sh.never, 1);
       tc::mbar_init_fence();
     }
     cg::this_cluster().sync();
   }
-  // No CTA leaves while another may send to it.
-  __device__ __forceinline__ static void finish() {
-    if (kCluster) cg::this_cluster().sync();
+  // No CTA leaves while another may send to it, or while what was sent is on its way: a thread that
+  // gave up at window `lost` has not waited for the maps of that window and the next (bounded).
+  __device__ __forceinline__ static void finish(Shared& sh, uint32_t lost) {
+    if (!kCluster) return;
+    cg::this_cluster().sync();
+    if (lost == ~0u) return;
+    atomicOr(&glr_status, kStatusTimeout);
+    for (uint32_t w = lost; w < lost + 2; ++w) tc::mbar_wait(&sh.bar[w & 1u], (w >> 1) & 1u, 1000000ull);
   }
   __device__ __forceinline__ static void send(const float* to, const float* v, const uint64_t* bar, int dst) {
     uint32_t at, mb;
@@ -290,8 +311,8 @@ struct Exchange {
                    : "memory");
   }
   // carry: the state before the window, in; after the window, out.  in: the state before
-  // this segment.  n: windows before this one.
-  __device__ __forceinline__ static void run(Shared& sh, uint32_t n, int rank, int n_rank, int wt, int lane,
+  // this segment.  n: windows before this one.  lost: the window at which this thread gave up.
+  __device__ __forceinline__ static void run(Shared& sh, const Waits& waits, uint32_t& lost, uint32_t n, int rank, int n_rank, int wt, int lane,
                                              const float (&A)[V], const float (&H)[V], float (&carry)[V],
                                              float (&in)[V]) {
     const int buf = (int)(n & 1u);
@@ -336,7 +357,7 @@ struct Exchange {
       if (w < wt) then(pa, ph, w);
     end(pa, wt);
     if (kCluster) {
-      if (wt == WT - 1) {  // the last warp has the CTA's map: to every CTA of the cluster
+      if (wt == WT - 1 && lost == ~0u) {  // the last warp has the CTA's map: to every CTA of the cluster
         float t[2 * V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -348,8 +369,10 @@ struct Exchange {
         if (lane == 0) tc::mbar_expect_tx(&sh.bar[buf], (uint32_t)n_rank * 32u * 2u * V * 4u);
         for (int dst = 0; dst < n_rank; ++dst) send(&sh.c[buf][rank][lane][0], t, &sh.bar[buf], dst);
       }
-      // bounded; a window whose maps did not arrive makes everything after it NaN
-      const bool got = tc::mbar_wait(&sh.bar[buf], (n >> 1) & 1u);
+      if (lost == ~0u) {
+        const bool hook = n == waits.expire_at && rank == 0;
+        if (!tc::mbar_wait(hook ? &sh.never : &sh.bar[buf], hook ? 0u : (n >> 1) & 1u, waits.limit_ns)) lost = n;
+      }
 #pragma unroll
       for (int v = 0; v < V; ++v) in[v] = carry[v];
       for (int c = 0; c < n_rank; ++c)
@@ -358,7 +381,7 @@ struct Exchange {
           if (c == rank) in[v] = carry[v];
           carry[v] = apply(sh.c[buf][c][lane][v], carry[v], sh.c[buf][c][lane][V + v]);
         }
-      if (!got) {
+      if (lost != ~0u) {
 #pragma unroll
         for (int v = 0; v < V; ++v) in[v] = carry[v] = __int_as_float(0x7FC00000);
       }
@@ -385,7 +408,7 @@ struct Exchange {
 template <typename E, int V, int S, int WT, int kWarps, bool kCluster, int kRing>
 __global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 2 ? 5 : 16 / kWarps)
     glr_fwd(const __grid_constant__ GlrDev a, const float* h0, const __grid_constant__ Seq h, float* h_last,
-            float* ckpt, int n_rank) {
+            float* ckpt, int n_rank, Waits waits) {
   tc::after_previous();
   using X = Exchange<V, WT, kCluster>;
   __shared__ typename X::Shared sh;
@@ -453,7 +476,7 @@ __global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 
   } else {
     fetch((int64_t)seg * S);
   }
-  uint32_t n = 0;  // windows so far
+  uint32_t n = 0, lost = ~0u;  // windows so far, see Exchange
   for (int64_t w0 = 0; w0 < a.T; w0 += window, ++n) {
     const int64_t t0 = w0 + (int64_t)seg * S;
     const uint32_t rs = __ballot_sync(0xFFFFFFFFu, nrs != 0);
@@ -526,7 +549,7 @@ __global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) A[v] = rs ? 0.0f : not_zero(A[v]);
-      X::run(sh, n, rank, n_rank, wt, lane, A, H, carry, y);
+      X::run(sh, waits, lost, n, rank, n_rank, wt, lane, A, H, carry, y);
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) y[v] = carry[v];
@@ -575,7 +598,7 @@ __global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 
     }
   }
   if (kRing) R::template wait<0>();
-  X::finish();
+  X::finish(sh, lost);
   if (h_last && at.on && seg == 0) {
 #pragma unroll
     for (int v = 0; v < V; ++v) h_last[me + v] = carry[v];
@@ -597,7 +620,7 @@ struct GlrGrad {
 // 5.1 TB/s); split fp32 passes wait for their windows too (4096 x 8 x 512 102 us, 4.1 TB/s).
 template <typename E, int V, int WT, int kWarps, bool kCluster, int kRing>
 __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
-    glr_bwd(const __grid_constant__ GlrDev a, const __grid_constant__ GlrGrad b, int n_rank) {
+    glr_bwd(const __grid_constant__ GlrDev a, const __grid_constant__ GlrGrad b, int n_rank, Waits waits) {
   tc::after_previous();
   using X = Exchange<V, WT, kCluster>;
   __shared__ typename X::Shared sh;
@@ -677,7 +700,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     for (int w = 0; w < kRing; ++w) fetch_ring(last - w * window, w);
     nrs = reset_byte<S>(a, at, last, lane);
   }
-  uint32_t n = 0;  // windows so far
+  uint32_t n = 0, lost = ~0u;  // windows so far, see Exchange
   for (int64_t t0 = last, w = (a.T + window - 1) / window; w > 0; --w, t0 -= window, ++n) {
     // Ring: one channel a thread has room for the whole segment, and the slot is refilled as soon
     // as it is read; two read x and dh from the slot where they are used, and refill it last.
@@ -778,7 +801,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     if (small) rebuild(std::true_type());
     else rebuild(std::false_type());
     if (WT > 1 || kCluster) {
-      X::run(sh, n, rank, n_rank, wt, lane, A, P, carry, p);
+      X::run(sh, waits, lost, n, rank, n_rank, wt, lane, A, P, carry, p);
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) p[v] = carry[v];
@@ -872,7 +895,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     }
   }
   if (kRing) R::template wait<0>();
-  X::finish();
+  X::finish(sh, lost);
   if (!at.on) return;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
@@ -1004,13 +1027,23 @@ aht_status launch(K kernel, dim3 grid, dim3 block, int cl, int smem, cudaStream_
   return launched(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
+// The failure hook (aht_debug_glr_expire): taken by the next pass that is split over a cluster.
+constexpr uint64_t kWaitNs = 2000000000ull;
+std::atomic<uint64_t> g_expire{0};     // 0: off, else window << 32 | limit_ns
+Waits clustered_waits() {
+  const uint64_t hook = g_expire.exchange(0);
+  return hook ? Waits{hook & 0xFFFFFFFFu, (uint32_t)(hook >> 32)} : Waits{kWaitNs, ~0u};
+}
+constexpr Waits kNoWaits{kWaitNs, ~0u};
+
 // Many lanes (or T = 1): a warp per group of 32 V lanes.
 template <typename E, int V, int S, int kRing>
 aht_status forward_wide(const aht_glr_args* a, const float* h0, const Seq& h, float* h_last, float* ckpt, cudaStream_t s) {
   const int64_t four = (split_fwd(a->T, a->N, a->D, V).units + 3) / 4;
   constexpr int kSmem = 4 * kRing * Ring<3, 8, V * (int)sizeof(E), 0>::kStage;
   static_assert(kRing == 0 || S == 8, "");
-  return launch(glr_fwd<E, V, S, 1, 4, false, kRing>, dim3((unsigned)four), dim3(128), 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
+  return launch(glr_fwd<E, V, S, 1, 4, false, kRing>, dim3((unsigned)four), dim3(128), 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1,
+                kNoWaits);
 }
 // Few lanes: 8 warps and p.cl CTAs along time.
 template <typename E, int V, int S, int kRing>
@@ -1018,8 +1051,10 @@ aht_status forward_long(const aht_glr_args* a, const Split& p, const float* h0, 
                         cudaStream_t s) {
   constexpr int kSmem = 8 * kRing * Ring<3, S, V * (int)sizeof(E), 0>::kStage;
   if (p.cl == 1)
-    return launch(glr_fwd<E, V, S, 8, 8, false, kRing>, dim3((unsigned)p.units), dim3(256), 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1);
-  return launch(glr_fwd<E, V, S, 8, 8, true, kRing>, dim3((unsigned)p.units), dim3(256), p.cl, kSmem, s, dev(a), h0, h, h_last, ckpt, p.cl);
+    return launch(glr_fwd<E, V, S, 8, 8, false, kRing>, dim3((unsigned)p.units), dim3(256), 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1,
+                  kNoWaits);
+  return launch(glr_fwd<E, V, S, 8, 8, true, kRing>, dim3((unsigned)p.units), dim3(256), p.cl, kSmem, s, dev(a), h0, h, h_last, ckpt, p.cl,
+                clustered_waits());
 }
 
 template <typename E, int V, bool kRows>  // kRows: rows aligned for the ring
@@ -1029,10 +1064,12 @@ aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStre
   *rows = p.segs();
   constexpr int kStage = Ring<4, kSeg, V * (int)sizeof(E), 128 * V>::kStage, kWide = kRows ? 2 : 0, kLong = kRows ? 3 : 0;
   if (V > 1 || p.wt == 1)
-    return launch(glr_bwd<E, V, 1, 4, false, kWide>, dim3((unsigned)((p.units + 3) / 4)), dim3(128), 1, 4 * kWide * kStage, s, d, g, 1);
+    return launch(glr_bwd<E, V, 1, 4, false, kWide>, dim3((unsigned)((p.units + 3) / 4)), dim3(128), 1, 4 * kWide * kStage, s, d, g, 1,
+                  kNoWaits);
   if constexpr (V == 1) {
-    if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kLong>, dim3((unsigned)p.units), dim3(256), 1, 8 * kLong * kStage, s, d, g, 1);
-    return launch(glr_bwd<E, V, 8, 8, true, kLong>, dim3((unsigned)p.units), dim3(256), p.cl, 8 * kLong * kStage, s, d, g, p.cl);
+    if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kLong>, dim3((unsigned)p.units), dim3(256), 1, 8 * kLong * kStage, s, d, g, 1, kNoWaits);
+    return launch(glr_bwd<E, V, 8, 8, true, kLong>, dim3((unsigned)p.units), dim3(256), p.cl, 8 * kLong * kStage, s, d, g, p.cl,
+                  clustered_waits());
   }
   return AHT_EINVAL;  // (V > 1 is wide)
 }
@@ -1145,6 +1182,23 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
   float* first = part + part_floats(a->T, a->N, a->D);
   if ((e = launch(glr_dlam<false>, dim3(grid.x, kSumRows), block, 1, 0, s, part, rows, a->D, a->lam, first))) return e;
   return launch(glr_dlam<true>, grid, block, 1, 0, s, first, (int64_t)kSumRows, a->D, a->lam, dlam);
+}
+
+aht_status aht_glr_sync(void* cuda_stream) {
+  if (aht_status e = launched(cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)))) return e;
+  uint32_t st = 0;
+  if (aht_status e = launched(cudaMemcpyFromSymbol(&st, glr_status, sizeof st))) return e;
+  if (!st) return AHT_OK;
+  const uint32_t none = 0;
+  if (aht_status e = launched(cudaMemcpyToSymbol(glr_status, &none, sizeof none))) return e;
+  return set_last_error(AHT_ETIMEOUT, "a bounded wait of a split recurrence expired");
+}
+
+aht_status aht_debug_glr_expire(int32_t window, int64_t limit_ns) {
+  if (window >= 0 && (limit_ns < 1 || limit_ns > 1000000000))
+    return set_last_error(AHT_EINVAL, "limit_ns must be in 1..1e9");
+  g_expire = window < 0 ? 0 : (uint64_t)window << 32 | (uint64_t)limit_ns;
+  return AHT_OK;
 }
 
 }  // extern "C"
