@@ -512,6 +512,13 @@ aht_status aht_muon_step(aht_muon* s, const aht_muon_matrix* mats, int32_t grad_
 aht_status aht_muon_orthogonalize(aht_muon* s, const void* const* in, const int32_t* ld_in, void* const* out,
                                   const int32_t* ld_out, int32_t dtype);
 aht_status aht_muon_sync(aht_muon* s);
+/* What a call that ends in AHT_ETIMEOUT leaves: the momenta are updated; a set on chip (short sides of at
+ * most 128, long ones of at most 1024) has every matrix either updated as a whole or its weights
+ * untouched; of another set weights may be updated in part.  The handle stays usable.
+ * Failure-detection hook (no paper counterpart): in the handle's next call a CTA waits in vain for the
+ * Gram product of matrix `matrix` at step `step` of the iteration, and every wait is limited to limit_ns
+ * (1 .. 10^9).  The hook fires once; matrix < 0 clears it.  No fault, no hang. */
+aht_status aht_debug_muon_expire(aht_muon* s, int32_t matrix, int32_t step, int64_t limit_ns);
 
 /* Stateless GAE (App. C "PPO ego"), time-major [T][n_envs] device arrays:
  *   delta_t = r_t + gamma (1 - d_t) V_{t+1} - V_t,

@@ -31,7 +31,7 @@ EXPORTED = ["aht_create", "aht_destroy", "aht_reset", "aht_rollout", "aht_xplay_
             "aht_s5_create", "aht_s5_destroy", "aht_s5_step", "aht_s5_sync", "aht_traj_copy",
             "aht_glr_ckpt_elems", "aht_glr_workspace", "aht_glr_forward", "aht_glr_backward", "aht_glr_sync",
             "aht_debug_glr_expire", "aht_muon_create", "aht_muon_destroy",
-            "aht_muon_step", "aht_muon_orthogonalize", "aht_muon_sync"]
+            "aht_muon_step", "aht_muon_orthogonalize", "aht_muon_sync", "aht_debug_muon_expire"]
 
 
 class AhtError(RuntimeError):
@@ -143,7 +143,8 @@ def load() -> C.CDLL:
             L.aht_muon_step.argtypes = [vp, C.POINTER(MuonMatrix), i32, C.c_float]
             L.aht_muon_orthogonalize.argtypes = [vp, C.POINTER(vp), C.POINTER(i32), C.POINTER(vp), C.POINTER(i32), i32]
             L.aht_muon_sync.argtypes = [vp]
-            for f in ("aht_muon_create", "aht_muon_step", "aht_muon_orthogonalize", "aht_muon_sync"):
+            L.aht_debug_muon_expire.argtypes = [vp, i32, i32, i64]
+            for f in ("aht_muon_create", "aht_muon_step", "aht_muon_orthogonalize", "aht_muon_sync", "aht_debug_muon_expire"):
                 getattr(L, f).restype = C.c_int
             L.aht_rollout_resample.argtypes = [vp, i32, C.POINTER(i32), i32, i32, C.POINTER(Traj), vp]
             L.aht_xplay_matrix.argtypes = [vp, C.POINTER(i32), i32, C.POINTER(i32), i32, i32, i32, C.POINTER(XplayOut)]
@@ -897,3 +898,9 @@ def aht_muon_orthogonalize(opt: Muon, mats, outs):
 
 def aht_muon_sync(opt: Muon):
     _check(load().aht_muon_sync(opt.handle))
+
+
+def aht_debug_muon_expire(opt: Muon, matrix: int, step: int, limit_ns: int):
+    """Failure hook: the handle's next call waits in vain (bounded by limit_ns) for a product of ``matrix``
+    at iteration ``step``; ``matrix < 0`` clears it."""
+    _check(load().aht_debug_muon_expire(opt.handle, matrix, step, limit_ns))

@@ -95,6 +95,8 @@ struct Common {
   int32_t paired;                              // clusters are of two pairs, else of one
   int32_t bf16_in, bf16_out, update, nesterov;
   float mu, eps, decay, lr;                    // decay = 1 - lr * weight_decay
+  uint64_t wait_ns;                            // limit of a wait
+  int32_t expire_mat, expire_step;             // failure hook: this Gram product is awaited in vain (-1: none)
 };
 
 __device__ __forceinline__ float load_in(const Common& c, const Ptrs& p, int k, int64_t r, int64_t col) {
@@ -547,7 +549,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     products(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, const __grid_constant__ Maps maps) {
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages];
-  __shared__ __align__(8) uint64_t accf_bar[kAcc], acce_bar[kAcc], drain_bar, parcel_bar, read_bar;
+  __shared__ __align__(8) uint64_t accf_bar[kAcc], acce_bar[kAcc], drain_bar, parcel_bar, read_bar, never_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -565,6 +567,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     tc::mbar_init(&drain_bar, 2);
     tc::mbar_init(&parcel_bar, 1);
     tc::mbar_init(&read_bar, 1);
+    tc::mbar_init(&never_bar, 1);
     tc::mbar_init_fence();
     abort_flag = 0;
   }
@@ -583,9 +586,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
   auto wait_or_abort = [&](uint64_t* bar, uint32_t parity) {
     if (tc::mbar_try_wait(bar, parity)) return true;
-    bool ok = false;
-    for (int tries = 0; tries < 1000 && !ok && !abort_flag; ++tries) ok = tc::mbar_wait(bar, parity, 2000000ull);
-    return ok;
+    const uint64_t t0 = tc::globaltimer_ns();
+    for (int tries = 0; tries < 1000 && !abort_flag; ++tries) {
+      if (tc::mbar_wait(bar, parity, min((uint64_t)2000000, c.wait_ns))) return true;
+      if (tc::globaltimer_ns() - t0 > c.wait_ns) break;
+    }
+    return false;
   };
   auto wait_warp = [&](uint64_t* bar, uint32_t parity) {  // by a whole warp, which goes on or gives up together
     return (bool)__all_sync(0xFFFFFFFFu, wait_or_abort(bar, parity));
@@ -600,7 +606,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const uint64_t t0 = tc::globaltimer_ns();
     for (uint32_t i = 0; i < (1u << 30) && !abort_flag; ++i) {
       if (ld_acquire(at) >= want) return true;
-      if ((i & 63u) == 63u && tc::globaltimer_ns() - t0 > 2000000000ull) return false;
+      if ((i & 63u) == 63u && tc::globaltimer_ns() - t0 > c.wait_ns) return false;
     }
     return false;
   };
@@ -754,6 +760,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       float f[64];
 #pragma unroll
       for (int e = 0; e < 64; ++e) f[e] = 0.0f;
+      if (t.mat == c.expire_mat && phase == kGram && t.it == c.expire_step) ok = wait_warp(&never_bar, 0);
       for (int k = 2 * first_k(t.part, K), k_end = 2 * end_k(t.part, K); ok && k < k_end; ++k, ++j) {
         const int acc = j % kAcc;
         // warp-uniform: tensor-memory loads are collective
@@ -832,8 +839,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     tc::mbar_wait(&drain_bar, 0);
   }
   if (warp == 0 && lane == 0 && rank == 0 && abort_flag) {
-    for (int d = max(0, issued - kStages); d < issued; ++d)
-      tc::mbar_wait(&full_bar[d % kStages], (uint32_t)(d / kStages) & 1u);
+    for (int d = max(0, issued - kStages); d < issued; ++d)  // (a stage that was not filled never completes)
+      tc::mbar_wait(&full_bar[d % kStages], (uint32_t)(d / kStages) & 1u, 10000000ull);
   }
   tc::fence_before_sync();
   __syncthreads();
@@ -869,6 +876,9 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void peer_store(uint32_t a, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
+__device__ __forceinline__ void peer_store_u32(uint32_t a, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
 __device__ __forceinline__ double peer_load_f64(uint32_t a) {
   double v;
   asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(a) : "memory");
@@ -879,8 +889,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     small_updates(const __grid_constant__ Common c, const __grid_constant__ Ptrs p, int cluster) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t done_bar;
+  __shared__ __align__(8) uint64_t done_bar, never_bar;
   __shared__ uint32_t tmem_slot;
+  __shared__ uint32_t failed_s;                // a CTA of the cluster gave up
   __shared__ double norm_s[kSmallThreads / 32];
   __shared__ float2 inv_s;
   uint8_t *xs = smem, *ss = smem + 2 * kBlk, *parts = ss + kStaged;
@@ -893,7 +904,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   const int j0 = rank * kB + c_beg;
   if (tid == 0) {
     tc::mbar_init(&done_bar, 1);
+    tc::mbar_init(&never_bar, 1);
     tc::mbar_init_fence();
+    failed_s = 0;
   }
   if (warp == 0) tc::tmem_alloc(&tmem_slot, 256);
   tc::fence_before_sync();
@@ -901,7 +914,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   tc::fence_after_sync();
   const uint32_t tmem = tmem_slot, lane_base = (uint32_t)(32 * (warp & 3)) << 16;
   const bool one = warp == 0 && tc::elect_one();
-  uint32_t parity = 0;
+  uint32_t parity = 0, drain = 2;              // drain: parity of the products that were given up
   bool ok = true;
 
   float f[64];
@@ -918,7 +931,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   };
   // f = a 128 x 128 x 128 product of hi + lo blocks, 64 of K in each of two accumulators (see
   // products()); b_mn: B's block has K along its rows
-  auto product = [&](const uint8_t* a, const uint8_t* b, bool b_mn) {
+  auto product = [&](const uint8_t* a, const uint8_t* b, bool b_mn, bool hook) {
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
@@ -940,11 +953,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     }
     bool got = true;
     if (ok) {
-      got = false;
-      for (int tries = 0; tries < 1000 && !got; ++tries) got = tc::mbar_wait(&done_bar, parity, 2000000ull);
+      got = tc::mbar_wait(hook ? &never_bar : &done_bar, hook ? 0u : parity, c.wait_ns);
+    }
+    if (__syncthreads_or(!got)) {              // all threads of the CTA go on alike
+      ok = false;
+      drain = parity;
     }
     parity ^= 1u;
-    ok = !__syncthreads_or(!got) && ok;        // all threads of the CTA go on alike
     tc::fence_after_sync();
 #pragma unroll
     for (int e = 0; e < 64; ++e) f[e] = 0.0f;
@@ -1100,7 +1115,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   // rows of the Gram matrix this CTA sums for all
   const int r_beg = on ? kB * rank / nb : 0, r_cnt = on ? kB * (rank + 1) / nb - r_beg : 0;
   for (int it = 0; it < c.steps; ++it) {
-    if (on) product(xs, xs, false);
+    if (on) product(xs, xs, false, rank == 0 && k == c.expire_mat && it == c.expire_step);
     if (nb == 2) {                             // each takes the other's part whole: one wait
       if (it > 0) cluster_wait();              // the other has read what it received last
       if (on) {
@@ -1149,11 +1164,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
     scale(kUp * kSA / (kSX * kSX));
     add_diag(kShift * kSA);
     split_to(ss);
-    product(ss, ss, false);
+    product(ss, ss, false, false);
     scale(kUp * kC * kSB / (kSA * kSA));
     add_diag(kDiag * kSB);
     split_to(ss);
-    product(ss, xs, true);
+    product(ss, xs, true, false);
     if (it + 1 < c.steps) {
       scale(kUp / kSB);
       split_to(xs);
@@ -1162,6 +1177,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   // (the next call's CTAs from here on: from the start on they cost 2 us of 57 instead of saving 1)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (nb == 2) cluster_wait();
+  // Nothing is stored of a matrix of which a CTA gave up: the others have summed what it did not send.
+  if (!ok && tid == 0)
+    for (int q = 0; q < cluster; ++q) peer_store_u32(peer_addr(&failed_s, q), 1u);
+  cluster_sync();                              // (no CTA reaches into another from here on)
+  ok = failed_s == 0;
   // the weights, along their rows like the gradient
   if (on && tall && ok) store_result(c, p, k, m, 32 * (warp & 3), lane, j0, f);
   if (on && !tall) {
@@ -1215,9 +1235,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   }
 
   if (tid == 0 && !ok) atomicOr(c.status, kStatusTimeout);
+  if (drain < 2) tc::mbar_wait(&done_bar, drain, 10000000ull);  // before tensor memory goes (bounded)
   tc::fence_before_sync();
   __syncthreads();
-  cluster_sync();                            // no CTA leaves while another may read its sums
   if (warp == 0) {
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem, 256);
@@ -1257,6 +1277,8 @@ struct aht_muon {
   uint32_t* summed = nullptr;
   uint32_t* status = nullptr;
   std::vector<void*> owned;
+  int32_t expire_mat = -1, expire_step = 0;  // failure hook (aht_debug_muon_expire) of the next call
+  uint64_t expire_ns = 0;
 };
 
 namespace {
@@ -1297,6 +1319,10 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   c.eps = s->cfg.eps;
   c.mu = s->cfg.momentum;
   c.nesterov = s->cfg.nesterov;
+  c.wait_ns = s->expire_mat < 0 ? 2000000000ull : s->expire_ns;
+  c.expire_mat = s->expire_mat;
+  c.expire_step = s->expire_step;
+  s->expire_mat = -1;
   const unsigned n = (unsigned)s->mats.size();
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2], overlap;        // see tc::after_previous()
@@ -1561,6 +1587,18 @@ aht_status aht_muon_orthogonalize(aht_muon* s, const void* const* in, const int3
   Common c{};
   c.bf16_in = c.bf16_out = dtype == AHT_BF16;
   return run(s, c, p);
+}
+
+aht_status aht_debug_muon_expire(aht_muon* s, int32_t matrix, int32_t step, int64_t limit_ns) {
+  if (!s) return set_last_error(AHT_EINVAL, "NULL argument");
+  if (matrix >= 0 && (matrix >= (int64_t)s->mats.size() || step < 0 || step >= s->cfg.steps))
+    return set_last_error(AHT_EINVAL, "no such matrix or step");
+  if (matrix >= 0 && (limit_ns < 1 || limit_ns > 1000000000))
+    return set_last_error(AHT_EINVAL, "limit_ns must be in 1..1e9");
+  s->expire_mat = matrix < 0 ? -1 : matrix;
+  s->expire_step = step;
+  s->expire_ns = (uint64_t)limit_ns;
+  return AHT_OK;
 }
 
 aht_status aht_muon_sync(aht_muon* s) {
