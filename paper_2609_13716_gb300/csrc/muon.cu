@@ -54,10 +54,13 @@ constexpr float kA = 3.4445f, kBq = -4.7750f, kC = 2.0315f;  // Jordan et al. 20
 constexpr float kSX = 16384.0f, kSA = 16384.0f, kSB = 8192.0f;
 // The tensor cores round the running sum of a product towards zero.  Over the 12 additions of
 // 64 of K, the small products first, that takes about 2e-7 off a result (a step's two last
-// products together 3e-7 to 5e-7, on full-rank, low-rank and positive matrices of 128 to
-// 2048), always downwards, and five steps multiply a common factor by about 7; every product is
-// scaled back by 2 * 2^-23.
-constexpr float kUp = 1.0f + 2.0f / 8388608.0f;
+// products together 3e-7 to 5e-7), always downwards, and five steps multiply a common factor by 7 to
+// 11; every product is scaled back by 2 * 2^-23.  Where the short side, which two of the three
+// products sum over, ends early, there are fewer additions and half of it is right.  Error of the
+// result in 1e-6, Gaussian matrices, scaled by one and by two 2^-23: 8 x 8 0.8 and 1.3, 16 x 16 0.7
+// and 1.3, 24 x 96 0.7 and 1.5, 32 x 32 0.8 and 1.1, 40 x 40 1.1 and 1.1, 64 x 256 3.2 and 2.0,
+// 128 x 128 3.0 and 1.9, 1024 x 1024 2.7 and 2.0; fp32 products 0.7, 0.8, 1.2, 0.9, 1.0, 1.4, 1.4, 3.1.
+constexpr float up(int short_side) { return short_side <= 32 ? 1.0f + 0x1p-23f : 1.0f + 0x1p-22f; }
 constexpr float kShift = kBq / (2.0f * kC), kDiag = kA - kBq * kBq / (4.0f * kC);
 constexpr int kNormBlocks = 608;               // most partial sums of squares per matrix (one wave)
 constexpr int kMaxSteps = 32;
@@ -67,6 +70,7 @@ constexpr uint32_t kParcel = 32 * kEpiThreads * 4;  // bytes of half a tile in f
 struct Mat {
   int32_t rows, cols, m, n, mb, nb, tall;
   int32_t norm_blocks;                         // partial sums of squares
+  float scale[3];                              // of a phase's accumulated products, up() among it
   int32_t stores[3];                           // a phase's stores of tiles or, where shared, halves of them
   int64_t x[2], a, b;                          // byte offsets of the hi blocks
   int64_t x_lo, s_lo;                          // from a hi block to its lo block
@@ -467,7 +471,7 @@ __device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float* v = f + 4 * (b + e);
-        constexpr float s = kUp / (kSB * kSX);
+        const float s = m.scale[kApply] / kSX;
         o[e] = make_float4(v[0] * s, v[1] * s, v[2] * s, v[3] * s);
         if (c.update) old[e] = w[b + e];
       }
@@ -496,7 +500,7 @@ __device__ __forceinline__ void store_result(const Common& c, const Ptrs& p, int
       const int64_t at = at0 + h * ld;
       float o[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[e] = f[b + h + e] * (kUp / (kSB * kSX));
+      for (int e = 0; e < 16; ++e) o[e] = f[b + h + e] * (m.scale[kApply] / kSX);
       if (c.update) {
         float* w = static_cast<float*>(out) + at;
         float old[16];
@@ -731,7 +735,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       const int64_t blk = (phase == kApply ? (int64_t)I * m.nb : (int64_t)I * m.mb) + J;
       uint8_t* out = c.ws + (phase == kGram ? m.a : phase == kPoly ? m.b : t.it & 1 ? m.x[0] : m.x[1]) + blk * kBlk;
       const int64_t lo_off = phase == kApply ? m.x_lo : m.s_lo;
-      const float scale = kUp * (phase == kGram ? kSA / (kSX * kSX) : phase == kPoly ? kC * kSB / (kSA * kSA) : 1.0f / kSB);
+      const float scale = m.scale[phase];
       const float diag = phase == kApply || I != J ? 0.0f : phase == kGram ? kShift * kSA : kDiag * kSB;
       const bool last = phase == kApply && t.it + 1 == c.steps;
       // the columns c_at.. of row r, complete: to the workspace or, after the last step, the caller
@@ -899,6 +903,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   const int k = (int)blockIdx.x / cluster, rank = (int)blockIdx.x % cluster;
   const Mat& m = c.mats[k];
   const int nb = m.nb, rows = m.m, cols = m.n, tall = m.tall;
+  const float gram_scale = m.scale[kGram], poly_scale = m.scale[kPoly], apply_scale = m.scale[kApply];
   const bool on = rank < nb;                   // (the cluster is as wide as the widest matrix needs)
   const int r = 32 * (warp & 3) + lane, c_beg = 64 * (warp >> 2);  // this thread's row and 64 columns
   const int j0 = rank * kB + c_beg;
@@ -1161,16 +1166,16 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       __syncthreads();                         // (ss is written next)
     }
     if (!on) continue;
-    scale(kUp * kSA / (kSX * kSX));
+    scale(gram_scale);
     add_diag(kShift * kSA);
     split_to(ss);
     product(ss, ss, false, false);
-    scale(kUp * kC * kSB / (kSA * kSA));
+    scale(poly_scale);
     add_diag(kDiag * kSB);
     split_to(ss);
     product(ss, xs, true, false);
     if (it + 1 < c.steps) {
-      scale(kUp / kSB);
+      scale(apply_scale);
       split_to(xs);
     }
   }
@@ -1185,7 +1190,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   // the weights, along their rows like the gradient
   if (on && tall && ok) store_result(c, p, k, m, 32 * (warp & 3), lane, j0, f);
   if (on && !tall) {
-    scale(kUp / (kSB * kSX));
+    scale(apply_scale / kSX);
     stage(parts);
     __syncthreads();
     const float lr = c.update ? c.lr * sqrtf(fmaxf(1.0f, (float)m.rows / (float)m.cols)) : 0.0f;
@@ -1441,6 +1446,9 @@ aht_status create(int32_t n, const int32_t* rows, const int32_t* cols, const aht
     m.x[1] = region((int64_t)m.mb * m.nb);
     m.a = region((int64_t)m.mb * m.mb);
     m.b = region((int64_t)m.mb * m.mb);
+    m.scale[kGram] = up(m.m) * kSA / (kSX * kSX);
+    m.scale[kPoly] = up(m.m) * kC * kSB / (kSA * kSA);
+    m.scale[kApply] = up(m.m) / kSB;
     m.x_lo = (int64_t)m.mb * m.nb * kBlk;
     m.s_lo = (int64_t)m.mb * m.mb * kBlk;
     m.norm_blocks = (int)std::min<int64_t>(((int64_t)m.rows * m.cols + 4095) / 4096, kNormBlocks);
