@@ -223,12 +223,20 @@ def _ptr(t, dtype=None, shape=None, name="tensor"):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream):
+def _stream(stream, device=None):
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(torch.cuda.current_device() if device is None else device)
         return torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
+
+
+def _on_device(t, device, name):
+    """Refuses a tensor that is not on the CUDA device a call runs on."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the call runs on cuda:{device}")
 
 
 class Context:
@@ -715,13 +723,13 @@ _pack_seq = struct.Struct("@Pqq").pack              # Seq
 _pack_glr = struct.Struct("@iiqqPqqPqqPqqPPP").pack  # GlrArgs
 
 
-def _seq(t, shape, dtype, name, written=False):
+def _seq(t, shape, dtype, name, device, written=False):
     """Pointer and strides of a [T][N][D] tensor with contiguous channels and any step and env
     strides."""
     if t is None:
         return 0, 0, 0
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _on_device(t, device, name)
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
@@ -740,17 +748,30 @@ def _seq(t, shape, dtype, name, written=False):
     return t.data_ptr(), st, sn
 
 
+def _glr_ptr(t, dtype, shape, name, device):
+    if t is None:
+        return 0
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _on_device(t, device, name)
+    if t.dtype is not dtype or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        _ptr(t, dtype, shape, name)          # says what is wrong
+    return t.data_ptr()
+
+
 def _glr_args(x, r, i, lam, reset, lengths):
     if not isinstance(x, torch.Tensor) or x.dim() != 3:
         raise ValueError("x must be a [T][N][D] tensor")
     dt, shape = x.dtype, x.shape
     if dt is not torch.float32 and dt is not torch.bfloat16:
         raise TypeError(f"x must be float32 or bfloat16, got {dt}")
+    if not x.is_cuda:
+        raise TypeError("x must be a CUDA tensor")
+    device = torch.cuda.current_device()
     T, N, D = shape
-    return shape, dt, _pack_glr(
-        AHT_FP32 if dt is torch.float32 else AHT_BF16, D, T, N, *_seq(x, shape, dt, "x"), *_seq(r, shape, dt, "r"),
-        *_seq(i, shape, dt, "i"), _ptr(lam, torch.float32, (D,), "lam") or 0,
-        _ptr(reset, torch.uint8, (T, N), "reset") or 0, _ptr(lengths, torch.int32, (N,), "lengths") or 0)
+    return shape, dt, device, _pack_glr(
+        AHT_FP32 if dt is torch.float32 else AHT_BF16, D, T, N, *_seq(x, shape, dt, "x", device),
+        *_seq(r, shape, dt, "r", device), *_seq(i, shape, dt, "i", device), _glr_ptr(lam, torch.float32, (D,), "lam", device),
+        _glr_ptr(reset, torch.uint8, (T, N), "reset", device), _glr_ptr(lengths, torch.int32, (N,), "lengths", device))
 
 
 def aht_glr_ckpt_shape(T, N, D):
@@ -765,29 +786,30 @@ def aht_glr_workspace(T, N, D) -> int:
 
 def aht_glr_forward(x, r, i, lam, h=None, reset=None, lengths=None, h0=None, h_last=None, ckpt=None, stream=None):
     """h_t = a_t h_{t-1} + beta_t sigmoid(i_t) x_t over x, r, i [T][N][D] (see include/aht.h);
-    T = 1 with h0 and h_last the same tensor is the serving step."""
-    shape, dt, a = _glr_args(x, r, i, lam, reset, lengths)
+    T = 1 with h0 and h_last the same tensor is the serving step.  Every tensor is on the current
+    device."""
+    shape, dt, dev, a = _glr_args(x, r, i, lam, reset, lengths)
     T, N, D = shape
     f32 = torch.float32
-    _check(load().aht_glr_forward(a, _ptr(h0, f32, (N, D), "h0"), _pack_seq(*_seq(h, shape, dt, "h", True)),
-                                  _ptr(h_last, f32, (N, D), "h_last"),
-                                  _ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt"), _stream(stream)))
+    _check(load().aht_glr_forward(a, _glr_ptr(h0, f32, (N, D), "h0", dev), _pack_seq(*_seq(h, shape, dt, "h", dev, True)),
+                                  _glr_ptr(h_last, f32, (N, D), "h_last", dev),
+                                  _glr_ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt", dev), _stream(stream, dev)))
 
 
 def aht_glr_backward(x, r, i, lam, ckpt, dh, dx, dr, di, dlam=None, workspace=None, reset=None, lengths=None,
                      dh_last=None, dh0=None, stream=None):
     """Gradients of aht_glr_forward into dx, dr, di (and dlam, dh0) from dh and dh_last."""
-    shape, dt, a = _glr_args(x, r, i, lam, reset, lengths)
+    shape, dt, dev, a = _glr_args(x, r, i, lam, reset, lengths)
     T, N, D = shape
     f32 = torch.float32
-    sdh, sdx, sdr, sdi = (_pack_seq(*_seq(t, shape, dt, k, k != "dh"))
+    sdh, sdx, sdr, sdi = (_pack_seq(*_seq(t, shape, dt, k, dev, k != "dh"))
                           for k, t in (("dh", dh), ("dx", dx), ("dr", dr), ("di", di)))
-    ws = _ptr(workspace, torch.uint8, None, "workspace")
-    _check(load().aht_glr_backward(a, _ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt"), sdh,
-                                   _ptr(dh_last, f32, (N, D), "dh_last"), sdx, sdr, sdi,
-                                   _ptr(dlam, f32, (D,), "dlam"),
-                                   _ptr(dh0, f32, (N, D), "dh0"), ws, 0 if workspace is None else workspace.numel(),
-                                   _stream(stream)))
+    ws = _glr_ptr(workspace, torch.uint8, None, "workspace", dev)
+    _check(load().aht_glr_backward(a, _glr_ptr(ckpt, f32, aht_glr_ckpt_shape(T, N, D), "ckpt", dev), sdh,
+                                   _glr_ptr(dh_last, f32, (N, D), "dh_last", dev), sdx, sdr, sdi,
+                                   _glr_ptr(dlam, f32, (D,), "dlam", dev),
+                                   _glr_ptr(dh0, f32, (N, D), "dh0", dev), ws,
+                                   0 if workspace is None else workspace.numel(), _stream(stream, dev)))
 
 
 def aht_glr_sync(stream=None):
@@ -817,10 +839,11 @@ MUON_DEFAULTS = dict(momentum=0.95, weight_decay=0.01, eps=1e-7, nesterov=1, ste
 
 
 class Muon:
-    """Owns an aht_muon handle (aht_muon_destroy on close / garbage collection)."""
+    """Owns an aht_muon handle (aht_muon_destroy on close / garbage collection); device: the CUDA
+    device it was created on, where its matrices have to be."""
 
-    def __init__(self, handle, shapes):
-        self.handle, self.shapes = handle, shapes
+    def __init__(self, handle, shapes, device):
+        self.handle, self.shapes, self.device = handle, shapes, device
 
     def close(self):
         if self.handle:
@@ -844,7 +867,7 @@ def aht_muon_create(shapes, stream=None, **cfg) -> Muon:
     rows, cols = (C.c_int32 * n)(*[r for r, _ in shapes]), (C.c_int32 * n)(*[k for _, k in shapes])
     h = C.c_void_p()
     _check(load().aht_muon_create(n, rows, cols, C.byref(conf), _stream(stream), C.byref(h)))
-    return Muon(h, shapes)
+    return Muon(h, shapes, torch.cuda.current_device())
 
 
 def _matrices(opt, ts, dtype, name):
@@ -854,8 +877,8 @@ def _matrices(opt, ts, dtype, name):
         raise ValueError(f"{name}: {len(opt.shapes)} matrices expected, got {len(ts)}")
     out = []
     for k, (t, shape) in enumerate(zip(ts, opt.shapes)):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{name}[{k}] must be a CUDA tensor")
+        if not isinstance(t, torch.Tensor) or t.get_device() != opt.device:
+            _on_device(t, opt.device, f"{name}[{k}]")
         if t.dtype != dtype:
             raise TypeError(f"{name}[{k}] must be {dtype}, got {t.dtype}")
         if tuple(t.shape) != shape:

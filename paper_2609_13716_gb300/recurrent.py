@@ -4,9 +4,16 @@ function over the sequence, a serving step and an optimiser, all through the C A
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import aht
+
+
+def _device_of(t):
+    """The device of a CUDA tensor made the current one (other tensors are refused where they are used)."""
+    return torch.cuda.device(t.device) if t.is_cuda else contextlib.nullcontext()
 
 
 class _GatedRecurrence(torch.autograd.Function):
@@ -17,7 +24,8 @@ class _GatedRecurrence(torch.autograd.Function):
         h_last = torch.empty(N, D, dtype=torch.float32, device=x.device)
         need = any(ctx.needs_input_grad)
         ckpt = torch.empty(aht.aht_glr_ckpt_shape(T, N, D), device=x.device) if need else None
-        aht.aht_glr_forward(x, r, i, lam, h, reset=reset, lengths=lengths, h0=h0, h_last=h_last, ckpt=ckpt)
+        with _device_of(x):
+            aht.aht_glr_forward(x, r, i, lam, h, reset=reset, lengths=lengths, h0=h0, h_last=h_last, ckpt=ckpt)
         if need:
             ctx.save_for_backward(x, r, i, lam, ckpt, reset, lengths)
         return h, h_last
@@ -35,8 +43,9 @@ class _GatedRecurrence(torch.autograd.Function):
         ws = torch.empty(aht.aht_glr_workspace(T, N, D), dtype=torch.uint8, device=x.device)
         if dh is not None and dh.stride(2) != 1:
             dh = dh.contiguous()
-        aht.aht_glr_backward(x, r, i, lam, ckpt, dh, dx, dr, di, dlam, ws, reset=reset, lengths=lengths,
-                             dh_last=None if dh_last is None else dh_last.contiguous(), dh0=dh0)
+        with _device_of(x):
+            aht.aht_glr_backward(x, r, i, lam, ckpt, dh, dx, dr, di, dlam, ws, reset=reset, lengths=lengths,
+                                 dh_last=None if dh_last is None else dh_last.contiguous(), dh0=dh0)
         return dx, dr, di, dlam, dh0, None, None
 
 
@@ -51,8 +60,9 @@ def gated_step(x, r, i, lam, state, reset=None):
     """One serving step over x, r, i [N][D]: updates ``state`` (f32 [N][D]) in place and
     returns h [N][D]."""
     h = torch.empty(1, *x.shape, dtype=x.dtype, device=x.device)
-    aht.aht_glr_forward(x[None], r[None], i[None], lam, h, reset=None if reset is None else reset[None], h0=state,
-                        h_last=state)
+    with _device_of(x):
+        aht.aht_glr_forward(x[None], r[None], i[None], lam, h, reset=None if reset is None else reset[None], h0=state,
+                            h_last=state)
     return h[0]
 
 
@@ -63,12 +73,14 @@ class OrthogonalOptimizer:
     def __init__(self, params, lr=0.02, **cfg):
         self.params, self.lr = list(params), lr
         self.momenta = [torch.zeros_like(p) for p in self.params]
-        self.stream = torch.cuda.current_stream()
-        self.handle = aht.aht_muon_create([tuple(p.shape) for p in self.params], stream=self.stream, **cfg)
+        device = self.params[0].device if self.params else None
+        self.stream = torch.cuda.current_stream(device)
+        with torch.cuda.device(device):
+            self.handle = aht.aht_muon_create([tuple(p.shape) for p in self.params], stream=self.stream, **cfg)
 
     @torch.no_grad()
     def step(self):
-        now = torch.cuda.current_stream()
+        now = torch.cuda.current_stream(self.stream.device)
         if now != self.stream:
             self.stream.wait_stream(now)
         aht.aht_muon_step(self.handle, [p.detach() for p in self.params], self.momenta, [p.grad for p in self.params],
