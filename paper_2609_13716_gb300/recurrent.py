@@ -16,6 +16,13 @@ def _device_of(t):
     return torch.cuda.device(t.device) if t.is_cuda else contextlib.nullcontext()
 
 
+def _written(t):
+    """Tells autograd that the library wrote a tensor in place, as torch's own in-place operations do: a
+    graph that saved its earlier value raises instead of using the new one."""
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 class _GatedRecurrence(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, r, i, lam, h0, reset, lengths):
@@ -63,6 +70,7 @@ def gated_step(x, r, i, lam, state, reset=None):
     with _device_of(x):
         aht.aht_glr_forward(x[None], r[None], i[None], lam, h, reset=None if reset is None else reset[None], h0=state,
                             h_last=state)
+    _written(state)
     return h[0]
 
 
@@ -88,6 +96,7 @@ class OrthogonalOptimizer:
         if now != self.stream:
             now.wait_stream(self.stream)
         for p in self.params:
+            _written(p)
             p.grad = None
 
     def sync(self):
