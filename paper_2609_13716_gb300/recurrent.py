@@ -76,7 +76,10 @@ def gated_step(x, r, i, lam, state, reset=None):
 
 class OrthogonalOptimizer:
     """aht_muon_step over the gradients of a fixed list of f32 matrices.  The updates run on the
-    stream that is current here; a step under another one is ordered with it both ways."""
+    stream that is current here; a step under another one is ordered with it both ways.
+
+    step() needs a gradient of every matrix and clears it.  What there is to save and load beside
+    the parameters is ``momenta``, a list of tensors in their order."""
 
     def __init__(self, params, lr=0.02, **cfg):
         self.params, self.lr = list(params), lr
@@ -97,6 +100,7 @@ class OrthogonalOptimizer:
             now.wait_stream(self.stream)
         for p in self.params:
             _written(p)
+            p.grad.record_stream(self.stream)  # wherever it was allocated: its memory is not used again before
             p.grad = None
 
     def sync(self):
