@@ -937,6 +937,14 @@ __global__ void glr_dlam(const float* part, int64_t rows, int32_t D, const float
   }
 }
 
+// Whether every one of these addresses is a multiple of its elements' size (a kernel's access to another
+// faults).
+template <typename... P>
+bool elements_of(uintptr_t size, const P*... p) {
+  return ((reinterpret_cast<uintptr_t>(p) | ... | uintptr_t(0)) & (size - 1)) == 0;
+}
+constexpr char kMisaligned[] = "an address is not a multiple of its elements' size";
+
 aht_status check(const aht_glr_args* a) {
   if (!a) return set_last_error(AHT_EINVAL, "args is NULL");
   if (a->dtype != AHT_FP32 && a->dtype != AHT_BF16)
@@ -949,6 +957,8 @@ aht_status check(const aht_glr_args* a) {
     return set_last_error(AHT_EINVAL, "N * ceil(D / 32) must be at most 2^32");
   if (!a->lam) return set_last_error(AHT_EINVAL, "lam is NULL");
   if (a->T > 0 && (!a->x.data || !a->r.data || !a->i.data)) return set_last_error(AHT_EINVAL, "NULL input sequence");
+  if (!elements_of(a->dtype == AHT_FP32 ? 4 : 2, a->x.data, a->r.data, a->i.data) || !elements_of(4, a->lam, a->lengths))
+    return set_last_error(AHT_EINVAL, kMisaligned);
   return AHT_OK;
 }
 
@@ -1099,6 +1109,7 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
   if (!out.p && !h_last) return set_last_error(AHT_EINVAL, "neither h nor h_last is asked for");
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const int esz = a->dtype == AHT_FP32 ? 4 : 2;
+  if (!elements_of(esz, out.p) || !elements_of(4, h0, h_last, ckpt)) return set_last_error(AHT_EINVAL, kMisaligned);
   auto fits = [&](int V) {
     return a->D % V == 0 && aligned(seq(a->x), esz, V, a->T, a->N) && aligned(seq(a->r), esz, V, a->T, a->N) &&
            aligned(seq(a->i), esz, V, a->T, a->N) && aligned(out, esz, V, a->T, a->N);
@@ -1158,6 +1169,8 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
                   di ? seq(*di) : none, dh0, part};
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const int esz = a->dtype == AHT_FP32 ? 4 : 2;
+  if (!elements_of(esz, g.dh.p, g.dx.p, g.dr.p, g.di.p) || !elements_of(4, ckpt, dh_last, dlam, dh0, part))
+    return set_last_error(AHT_EINVAL, kMisaligned);
   auto fits = [&](int V) {
     bool ok = a->D % V == 0;
     for (const Seq& q : {seq(a->x), seq(a->r), seq(a->i), g.dh, g.dx, g.dr, g.di}) ok = ok && aligned(q, esz, V, a->T, a->N);

@@ -1359,6 +1359,8 @@ aht_status run(aht_muon* s, Common c, const Ptrs& p) {
   return AHT_OK;
 }
 
+constexpr char kMisaligned[] = "an address is not a multiple of its elements' size";
+
 // The boxes that the products copy (see Maps).
 aht_status make_maps(aht_muon* s, int64_t bytes) {
   void* fn = nullptr;
@@ -1563,6 +1565,8 @@ aht_status aht_muon_step(aht_muon* s, const aht_muon_matrix* mats, int32_t grad_
     if (!q.W || !q.M || !q.G) return set_last_error(AHT_EINVAL, "NULL weights, momentum or gradient");
     if (q.ldw < s->mats[k].cols || q.ldm < s->mats[k].cols || q.ldg < s->mats[k].cols)
       return set_last_error(AHT_EINVAL, "a row stride is below the matrix's columns");
+    if ((((uintptr_t)q.W | (uintptr_t)q.M) & 3) || ((uintptr_t)q.G & (grad_dtype == AHT_FP32 ? 3 : 1)))
+      return set_last_error(AHT_EINVAL, kMisaligned);
     p.in[k] = q.G;
     p.out[k] = q.W;
     p.mom[k] = q.M;
@@ -1587,6 +1591,7 @@ aht_status aht_muon_orthogonalize(aht_muon* s, const void* const* in, const int3
     if (!in[k] || !out[k]) return set_last_error(AHT_EINVAL, "NULL matrix");
     if (ld_in[k] < s->mats[k].cols || ld_out[k] < s->mats[k].cols)
       return set_last_error(AHT_EINVAL, "a row stride is below the matrix's columns");
+    if (((uintptr_t)in[k] | (uintptr_t)out[k]) & (dtype == AHT_FP32 ? 3 : 1)) return set_last_error(AHT_EINVAL, kMisaligned);
     p.in[k] = in[k];
     p.out[k] = out[k];
     p.ld_in[k] = ld_in[k];
