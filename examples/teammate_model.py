@@ -79,6 +79,7 @@ def main(updates=40, envs=512, steps=64, dtype="bf16", verbose=True):
         if verbose and k % 10 == 0:
             print(f"update {k}: loss {float(losses[-1]):.4f}")
     muon.sync()
+    aht.aht_glr_sync()
     # the same episodes, one step at a time
     with torch.no_grad():
         whole, last = model.sequence(traj["obs"], reset, state)

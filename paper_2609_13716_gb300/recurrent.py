@@ -11,9 +11,12 @@ import torch
 from . import aht
 
 
+_here = contextlib.nullcontext()
+
+
 def _device_of(t):
     """The device of a CUDA tensor made the current one (other tensors are refused where they are used)."""
-    return torch.cuda.device(t.device) if t.is_cuda else contextlib.nullcontext()
+    return torch.cuda.device(t.device) if t.is_cuda and t.get_device() != torch.cuda.current_device() else _here
 
 
 def _written(t):
@@ -42,7 +45,8 @@ class _GatedRecurrence(torch.autograd.Function):
     def backward(ctx, dh, dh_last):
         x, r, i, lam, ckpt, reset, lengths = ctx.saved_tensors
         T, N, D = x.shape
-        # the three gradients side by side: slices of one projection get one contiguous gradient
+        # the three gradients side by side, one allocation (autograd still concatenates them into a new
+        # tensor where x, r and i are slices of one projection)
         grad = torch.empty(T, N, 3 * D, dtype=x.dtype, device=x.device)
         dx, dr, di = grad.split(D, dim=2)
         dlam = torch.empty(D, device=x.device)

@@ -48,29 +48,34 @@ def test_optimiser_of_another_device():
 
 
 def test_torch_side_makes_the_tensors_device_current(monkeypatch):
-    """The device that is current while the library is called, for tensors of a device that is not."""
+    """With another device current, the tensors' own is while the library is called, and not after."""
     require_gpu()
     x, r, i, lam = sequences()
-    entered = []
+    p = torch.nn.Parameter(torch.ones(8, 16, device="cuda"))
+    current, entered = [1], []
 
     class Guard:
         def __init__(self, device):
-            self.device = device
+            self.index = torch.device(device).index
 
         def __enter__(self):
-            entered.append(torch.device(self.device))
+            entered.append(self.index)
+            self.before, current[0] = current[0], self.index
 
         def __exit__(self, *a):
-            entered.append(None)
+            current[0] = self.before
 
     monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
     x.requires_grad_()
     h, last = recurrent.gated_recurrence(x, r, i, lam)
     h.sum().backward()
-    recurrent.gated_step(x[0].detach(), r[0], i[0], lam, torch.zeros(3, 32, device="cuda"))
-    p = torch.nn.Parameter(torch.ones(8, 16, device="cuda"))
-    recurrent.OrthogonalOptimizer([p])
-    assert entered == [x.device, None] * 4
+    recurrent.gated_step(x[0].detach(), r[0], i[0], lam, torch.zeros(3, 32, device="cuda:0"))
+    opt = recurrent.OrthogonalOptimizer([p])
+    assert entered == [0] * 4 and current == [1] and opt.handle.device == 0
+    current[0] = 0                             # the tensors' device is current: nothing to enter
+    recurrent.gated_step(x[0].detach(), r[0], i[0], lam, torch.zeros(3, 32, device="cuda:0"))
+    assert entered == [0] * 4
 
 
 def test_host_tensors_are_still_a_type_error():
