@@ -423,7 +423,8 @@ aht_status aht_s5_sync(aht_s5* s);
  * all strides.  Gates, state and sums are fp32; each output is rounded once.  Outputs must
  * not overlap inputs or one another (h_last may be h0).  Lanes (n, d) are independent and
  * every sum has a fixed order: the same call gives the same bits.  N * ceil(D / 32) may be up
- * to 2^32, N * D to 2^37 and T * N * D to 2^46.
+ * to 2^32, N * D to 2^37 and T * N * D to 2^46.  Addresses are multiples of their elements' size
+ * (the workspace's of 4).  Every array is on the current device.
  * T = 1 is the serving step: h0 and h_last are the carried state.  Calls are asynchronous
  * on cuda_stream (NULL = default), allocate nothing and may be captured into a graph. */
 #define AHT_GLR_SEGMENT 8       /* steps between two checkpoints of the state */
@@ -478,8 +479,8 @@ aht_status aht_debug_glr_expire(int32_t window, int64_t limit_ns);
  * W and M are fp32, G fp32 or bf16, each output is rounded once.  A zero U gives O = 0; a
  * NaN or infinity in a gradient makes that matrix's update NaN and touches no other.  Every
  * sum has a fixed order: the same call gives the same bits.
- * Matrices are row-major with row strides ld (>= cols, in elements); those of one call must
- * not overlap.  Vectors, embeddings and output layers are the business of another optimiser. */
+ * Matrices are row-major with row strides ld (>= cols, in elements), on the device that was current
+ * at aht_muon_create; those of one call must not overlap.  Vectors, embeddings and output layers are the business of another optimiser. */
 #define AHT_MUON_MAX_MATRICES 48
 #define AHT_MUON_MAX_DIM 16384
 typedef struct aht_muon_config {
@@ -499,7 +500,7 @@ typedef struct aht_muon aht_muon; /* opaque, library-owned */
 /* Allocates the workspace for n matrices of these sizes (about 8 bytes per element plus 8
  * per element of the short side's square, sides rounded up to 128).  Every later call runs on
  * cuda_stream (NULL = default), after what was put there before and only that: a caller whose
- * gradients come from another stream makes this one wait for it.  The other calls allocate
+ * gradients come from another stream makes this one wait for it, and keeps them until it has read them.  The other calls allocate
  * nothing; calls on one handle come from one thread at a time. */
 aht_status aht_muon_create(int32_t n, const int32_t* rows, const int32_t* cols, const aht_muon_config* cfg,
                            void* cuda_stream, aht_muon** out);

@@ -402,9 +402,10 @@ struct Exchange {
 // come through a ring of that many segments (rows of 4-byte lanes, aligned); 0: the next
 // segment waits in registers.
 //
-// Whole chains are bound by memory (128 x 8192 x 128 fp32 307 us, the rate of a copy; 128 x 16384 x
-// 128 bf16 358 us, 6.1 TB/s, and 61 % of the issue slots); split ones by the hand-over of a window
-// between a cluster's CTAs (65537 x 1 x 896 fp32 170 us, 5.5 TB/s); one step by its launch.
+// Whole chains are bound by memory (128 x 8192 x 128 fp32 304 us, the rate of a copy; 128 x 16384 x
+// 128 bf16 356 us, 6.1 TB/s, and 61 % of the issue slots); split ones by the hand-over of a window
+// between a cluster's CTAs (65537 x 1 x 896 fp32 172 us, 5.5 TB/s); one step by its launch.  With
+// decay exponents beyond 1/4 (see Decay) the same three take 307, 392 and 187 us.
 template <typename E, int V, int S, int WT, int kWarps, bool kCluster, int kRing>
 __global__ void __launch_bounds__(32 * kWarps, kRing && WT == 1 && sizeof(E) == 2 ? 5 : 16 / kWarps)
     glr_fwd(const __grid_constant__ GlrDev a, const float* h0, const __grid_constant__ Seq h, float* h_last,
@@ -615,9 +616,10 @@ struct GlrGrad {
 };
 
 // kRing as in glr_fwd; 0: loaded when needed, which other warps cover.
-// Reads x, r, i, dh and a checkpoint, writes dx, dr, di: 14.5 bytes an element in bf16 at about 60
-// instructions, so issue slots (66 %) and memory bound it together (128 x 4096 x 128 bf16 184 us,
-// 5.1 TB/s); split fp32 passes wait for their windows too (4096 x 8 x 512 102 us, 4.1 TB/s).
+// Reads x, r, i, dh and a checkpoint, writes dx, dr, di: 14.5 bytes an element in bf16 at about 67
+// instructions, so issue slots (70 %) and memory bound it together (128 x 4096 x 128 bf16 170 us,
+// 5.5 TB/s); split fp32 passes wait for their windows too (4096 x 8 x 512 100 us, 4.2 TB/s).  With
+// decay exponents beyond 1/4 194 and 106 us.
 template <typename E, int V, int WT, int kWarps, bool kCluster, int kRing>
 __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps)
     glr_bwd(const __grid_constant__ GlrDev a, const __grid_constant__ GlrGrad b, int n_rank, Waits waits) {
@@ -988,7 +990,8 @@ struct Split {
 // steps split, unless it is so short that the windows' hand-overs cost more than the loads gain.
 constexpr int kFill = 152 * 12;
 // Clusters of n CTAs of a split pass that a GB300 holds at once, two CTAs an SM (as the occupancy
-// query answers).  The largest cluster at which every group's is resident is the quickest
+// query answers for the forward kernel; only speed depends on it, so other split kernels, and later
+// ones with other registers or shared memory, go by the same numbers).  The largest cluster at which every group's is resident is the quickest
 // (65537 x 1 x 896 fp32, 28 groups, forward: 8 CTAs 206 us, 9 183, 10 172; 20000 x 2 x 256, 16
 // groups: 8 66 us, 12 53, 16 in two waves 65).
 constexpr int kResident[kMaxCluster + 1] = {0, 304, 152, 97, 74, 58, 46, 38, 36, 30, 28, 23, 23, 19, 14, 14, 14};
@@ -1002,15 +1005,19 @@ Split split_of(int64_t T, int64_t N, int32_t D, int V, int fill) {
   return p;
 }
 
-// Split / whole, us: fp32 100 x 57 x 256 (456 groups) 12 / 15, 100 x 114 x 256 17 / 15, 400 x 150 x 256
-// (1200) 61 / 64, 400 x 200 x 256 77 / 72, 1000 x 200 x 256 146 / 174; bf16, two channels, 300 x 300 x
-// 256 (1200) 56 / 52, 1000 x 300 x 256 144 / 152.
+// Split / whole, us, by groups.  fp32 (groups of two channels; where these are too few, whole passes
+// take one): 100 steps 300 groups 12 / 14, 456 15 / 16, 900 28 / 23; 400 steps 600 62 / 70, 1200 110 / 92;
+// 1000 steps 900 166 / 216, 1824 322 / 298.  bf16, two channels: 100 steps 600 14 / 14, 1200 26 / 25; 400
+// steps 900 58 / 88, 1600 98 / 100; 1000 steps 1200 149 / 227, 2400 289 / 264.  The rule is off by a
+// quarter to a third between its points at 200 to 400 steps of bf16 (200 steps, 900 groups: 33 / 44,
+// whole) and for 1000 steps of fp32 with 1200 to 1824 groups of two (1600: 288 split, 272 whole; its one
+// channel takes 370).
 Split split_fwd(int64_t T, int64_t N, int32_t D, int V) {
   return split_of(T, N, D, V, (int)std::min<int64_t>(std::max<int64_t>(3 * T, kFill / 3), kFill));
 }
-// One channel a thread, split / whole, us: 100 x 57 x 256 (456 groups) fp32 21 / 20, bf16 22 / 20;
-// 400 x 76 x 256 59 / 54, 52 / 58; 1000 x 76 x 256 109 / 117, 97 / 140; 1000 x 150 x 256 199 / 169,
-// 174 / 163.  Two channels are for whole passes that one would not fill (see the dispatch).
+// One channel a thread, split / whole, us without dlam: 100 x 57 x 256 (456 groups) fp32 14 / 13, bf16
+// 14 / 15; 400 x 76 x 256 46 / 44, 41 / 43; 1000 x 76 x 256 100 / 102, 85 / 102; 1000 x 150 x 256 184 / 185,
+// 163 / 185.  Two channels are for whole passes that one would not fill (see the dispatch).
 Split split_bwd(int64_t T, int64_t N, int32_t D, int V) {
   return split_of(T, N, D, V, V > 1 ? kFill : (int)std::min<int64_t>(std::max<int64_t>(T, kFill / 4), kFill / 2));
 }
@@ -1026,7 +1033,7 @@ aht_status launch(K kernel, dim3 grid, dim3 block, int cl, int smem, cudaStream_
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = s;
-  // (128 x 4096 x 128 bf16 forward + backward 296 us, 303 without; 4096 x 8 x 512 153, 159)
+  // (128 x 4096 x 128 bf16 forward + backward 281 us, 288 without; 4096 x 8 x 512 152, 157)
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see tc::after_previous()
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -1119,8 +1126,8 @@ aht_status aht_glr_forward(const aht_glr_args* a, const float* h0, const aht_seq
   const bool rows = fits(16 / esz);      // every row a whole number of aligned 16-byte chunks
   auto wide = [&](int V) { return split_fwd(a->T, a->N, a->D, V).wt == 1; };
   // Wide passes, us for 128 steps (fp32 8192 x 128, bf16 16384 x 128; copies alone take 317): two
-  // channels a thread through the ring 307 / 362, two in registers 332 / 399, four in
-  // registers 333 / 394.  The ring wants aligned rows, two channels a well-filled warp.
+  // channels a thread through the ring 305 / 358, two in registers 312 / 420 (four in registers, of an
+  // earlier form, 333 / 394).  The ring wants aligned rows, two channels a well-filled warp.
   if (a->dtype == AHT_FP32) {
     if (a->T <= 1)
       return fits(4) ? forward_wide<float, 4, 1, 0>(a, h0, out, h_last, ckpt, s)
@@ -1182,8 +1189,8 @@ aht_status aht_glr_backward(const aht_glr_args* a, const float* ckpt, const aht_
   aht_status e;
   if (a->dtype == AHT_FP32)
     e = rows_16 ? backward<float, 1, true>(a, g, &segs, s) : backward<float, 1, false>(a, g, &segs, s);
-  // Two channels a thread while whole groups of them fill the SMs (128 x 16384 x 128: 689 us, one
-  // channel 892), one below (1000 x 300 x 256, 1200 groups of two: 228 against 258).
+  // Two channels a thread while whole groups of them fill the SMs (128 x 16384 x 128: 631 us, one
+  // channel 899), one below (1000 x 300 x 256, 1200 groups of two: 232 against 292).
   else if (fits(2) && split_bwd(a->T, a->N, a->D, 2).wt == 1)
     e = rows_16 ? backward<__nv_bfloat16, 2, true>(a, g, &segs, s) : backward<__nv_bfloat16, 2, false>(a, g, &segs, s);
   else

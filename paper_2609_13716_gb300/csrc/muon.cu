@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 // CTA receives everyone's part of its share of the rows, sums them in the order of the CTAs and
 // sends the sum to all (stores only: a remote load waits 0.3 us).  The other two products need no
 // exchange.  Bound by the chain of a step: Gram product 1.7 us, exchange 2.5, the other two 1.9 each
-// (128 x 196 and 128 x 128, five steps and the update: 55 us; products() takes 82).
+// (128 x 196 and 128 x 128, five steps and the update: 57 us; products() takes 82).
 constexpr int kSmallCluster = 8;
 constexpr int kSmallThreads = 256;
 constexpr uint32_t kStaged = 32 * (kB + 1) * 16;  // 128 x 128 fp32, four columns of a row together, padded
