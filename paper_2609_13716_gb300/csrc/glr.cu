@@ -312,8 +312,9 @@ struct Exchange {
   }
   // carry: the state before the window, in; after the window, out.  in: the state before
   // this segment.  n: windows before this one.  lost: the window at which this thread gave up.
-  __device__ __forceinline__ static void run(Shared& sh, const Waits& waits, uint32_t& lost, uint32_t n, int rank, int n_rank, int wt, int lane,
-                                             const float (&A)[V], const float (&H)[V], float (&carry)[V],
+  __device__ __forceinline__ static void run(Shared& sh, const Waits& waits, uint32_t& lost, uint32_t n, int rank,
+                                             int n_rank, int wt, int lane, const float (&A)[V], const float (&H)[V],
+                                             float (&carry)[V],
                                              float (&in)[V]) {
     const int buf = (int)(n & 1u);
 #pragma unroll
@@ -991,9 +992,9 @@ struct Split {
 constexpr int kFill = 152 * 12;
 // Clusters of n CTAs of a split pass that a GB300 holds at once, two CTAs an SM (as the occupancy
 // query answers for the forward kernel; only speed depends on it, so other split kernels, and later
-// ones with other registers or shared memory, go by the same numbers).  The largest cluster at which every group's is resident is the quickest
-// (65537 x 1 x 896 fp32, 28 groups, forward: 8 CTAs 206 us, 9 183, 10 172; 20000 x 2 x 256, 16
-// groups: 8 66 us, 12 53, 16 in two waves 65).
+// ones with other registers or shared memory, go by the same numbers).  The largest cluster at which
+// every group's is resident is the quickest (65537 x 1 x 896 fp32, 28 groups, forward: 8 CTAs 206 us,
+// 9 183, 10 172; 20000 x 2 x 256, 16 groups: 8 66 us, 12 53, 16 in two waves 65).
 constexpr int kResident[kMaxCluster + 1] = {0, 304, 152, 97, 74, 58, 46, 38, 36, 30, 28, 23, 23, 19, 14, 14, 14};
 
 Split split_of(int64_t T, int64_t N, int32_t D, int V, int fill) {
@@ -1068,10 +1069,10 @@ aht_status forward_long(const aht_glr_args* a, const Split& p, const float* h0, 
                         cudaStream_t s) {
   constexpr int kSmem = 8 * kRing * Ring<3, S, V * (int)sizeof(E), 0>::kStage;
   if (p.cl == 1)
-    return launch(glr_fwd<E, V, S, 8, 8, false, kRing>, dim3((unsigned)p.units), dim3(256), 1, kSmem, s, dev(a), h0, h, h_last, ckpt, 1,
-                  kNoWaits);
-  return launch(glr_fwd<E, V, S, 8, 8, true, kRing>, dim3((unsigned)p.units), dim3(256), p.cl, kSmem, s, dev(a), h0, h, h_last, ckpt, p.cl,
-                clustered_waits());
+    return launch(glr_fwd<E, V, S, 8, 8, false, kRing>, dim3((unsigned)p.units), dim3(256), 1, kSmem, s, dev(a), h0, h, h_last,
+                  ckpt, 1, kNoWaits);
+  return launch(glr_fwd<E, V, S, 8, 8, true, kRing>, dim3((unsigned)p.units), dim3(256), p.cl, kSmem, s, dev(a), h0, h, h_last,
+                ckpt, p.cl, clustered_waits());
 }
 
 template <typename E, int V, bool kRows>  // kRows: rows aligned for the ring
@@ -1081,10 +1082,12 @@ aht_status backward(const aht_glr_args* a, const GlrGrad& g, int* rows, cudaStre
   *rows = p.segs();
   constexpr int kStage = Ring<4, kSeg, V * (int)sizeof(E), 128 * V>::kStage, kWide = kRows ? 2 : 0, kLong = kRows ? 3 : 0;
   if (V > 1 || p.wt == 1)
-    return launch(glr_bwd<E, V, 1, 4, false, kWide>, dim3((unsigned)((p.units + 3) / 4)), dim3(128), 1, 4 * kWide * kStage, s, d, g, 1,
-                  kNoWaits);
+    return launch(glr_bwd<E, V, 1, 4, false, kWide>, dim3((unsigned)((p.units + 3) / 4)), dim3(128), 1, 4 * kWide * kStage, s,
+                  d, g, 1, kNoWaits);
   if constexpr (V == 1) {
-    if (p.cl == 1) return launch(glr_bwd<E, V, 8, 8, false, kLong>, dim3((unsigned)p.units), dim3(256), 1, 8 * kLong * kStage, s, d, g, 1, kNoWaits);
+    if (p.cl == 1)
+      return launch(glr_bwd<E, V, 8, 8, false, kLong>, dim3((unsigned)p.units), dim3(256), 1, 8 * kLong * kStage, s, d, g, 1,
+                    kNoWaits);
     return launch(glr_bwd<E, V, 8, 8, true, kLong>, dim3((unsigned)p.units), dim3(256), p.cl, 8 * kLong * kStage, s, d, g, p.cl,
                   clustered_waits());
   }
