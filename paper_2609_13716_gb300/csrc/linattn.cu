@@ -524,9 +524,10 @@ __global__ void __launch_bounds__(32 * kWarps, KT * COLS > 64 ? 2 : 4) walk(cons
 //   O = ((Q K^T) o D) V + diag(enter) Q S,   S <- g^L S + (diag(leave) K)^T V,
 // with D_ij = g^(i - j) where row j reaches row i (j <= i, the same episode), `enter` the decay from the chunk's
 // beginning to a row and `leave` from a row to its end, each 0 across an episode's beginning.
-//   Roundings to bf16: P = (Q K^T) o D and S, as operands, once each: together as much as the output's own
-// rounding.  Decayed k is hi + mid (2^-17) where the state only feeds bf16 outputs, and + lo, 2^-25, where it is an
-// output itself.  The state stays in fp32 registers, and a chunk's K^T V is summed from 0 before it is added: sums
+//   Operands of bf16: P = (Q K^T) o D and S are hi + lo, off by at most 2^-17 of each element, and so is decayed k
+// (hi + mid) where the state only feeds bf16 outputs; with one more part, 2^-25, where it is an output itself.  (One part,
+// 2^-8, is as much as an output's own rounding, and more where its terms nearly cancel: errors 1.4 times as large for
+// 408 us instead of 472, 128 x 4096 x 4 x 64.)  The state stays in fp32 registers, and a chunk's K^T V is summed from 0 before it is added: sums
 // that grow in the tensor cores' accumulators are truncated at every product.
 //   A CTA of D / 16 warps goes from chunk to chunk and chain to chain, the next chunk's rows on their way while
 // this one is computed.  A warp has 16 rows of O (and 64 of its columns) and 16 rows of S.  P goes from the
@@ -545,8 +546,12 @@ template <int D> struct TcPlan {
   static constexpr int kThreads = 2 * D, kSplit = D / 64;
   static constexpr int kPitch = 2 * D + 16, kPitchV = 2 * kVB + 16;   // bytes of a staged row: 8 rows in 8 bank groups
   static constexpr int kTile = kC * kPitch, kTileV = kC * kPitchV;
-  // one tile of q, two of k and v, S
-  static constexpr int kQ = 0, kK = kTile, kV = 3 * kTile, kS = 3 * kTile + 2 * kTileV, kSmall = kS + D * kPitchV;
+  // One tile of q, two of k and v, S as two operands.  The second one of D = 64 is in v's tile of the next chunk until the
+  // outputs are done: with a plane of its own three CTAs share an SM (128x1024x4x64 with gradients 404 us, this way 374).
+  static constexpr int kPlane = D * kPitchV;
+  static constexpr bool kInV = kPlane == kTileV;
+  static constexpr int kQ = 0, kK = kTile, kV = 3 * kTile, kS = 3 * kTile + 2 * kTileV, kSmall = kS + (kInV ? 1 : 2) * kPlane;
+  __device__ __forceinline__ static int low(int stage) { return kInV ? kV + (stage ^ 1) * kTileV : kS + kPlane; }
   static constexpr int kZeros = 16;        // before the decays of P: rows that do not reach a row
   static constexpr int kDecays = kZeros + 2 * (kC + 4), kBytes = kSmall + 2 * (kDecays + kC) * 4;   // (two sets, by turn)
   static constexpr int kCtas = D == 64 ? 4 : 2;   // an SM
@@ -768,13 +773,18 @@ __global__ void __launch_bounds__(TcPlan<D>::kThreads, TcPlan<D>::kCtas) chunks(
       }
     }
   };
-  auto plane_out = [&]() {      // S as an operand
-    unsigned char* at = sm + P::kS + (16 * warp + tr) * P::kPitchV + 4 * tq;
+  auto plane_out = [&](int stage) {      // S as operands of the chunk in a stage
+    const int at = (16 * warp + tr) * P::kPitchV + 4 * tq;
 #pragma unroll
     for (int j = 0; j < kNV; ++j)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        *reinterpret_cast<uint32_t*>(at + 8 * h * P::kPitchV + 16 * j) = tc::pack_bf16(S[j][2 * h], S[j][2 * h + 1]);
+      for (int h = 0; h < 2; ++h) {
+        const uint64_t f = tc::f2_pack(S[j][2 * h], S[j][2 * h + 1]);
+        const uint32_t hi = bf16_of(f);
+        unsigned char* to = sm + at + 8 * h * P::kPitchV + 16 * j;
+        *reinterpret_cast<uint32_t*>(to + P::kS) = hi;
+        *reinterpret_cast<uint32_t*>(to + P::low(stage)) = bf16_of(tc::f2_sub(f, pair_of(hi)));
+      }
   };
 
   uint32_t u = blockIdx.x;
@@ -823,7 +833,7 @@ __global__ void __launch_bounds__(TcPlan<D>::kThreads, TcPlan<D>::kCtas) chunks(
       }
       __syncthreads();          // (`leave` is made from the decays; nobody reads the chain before any more)
       if (threadIdx.x == 0 && u + gridDim.x < units) of_turn[turn ^ 1] = unit_of(c, u + gridDim.x);
-      if (received) plane_out();
+      if (received) plane_out(stage);
     }
     if (threadIdx.x < kC) leave[threadIdx.x] = (int)threadIdx.x < L && (int)threadIdx.x >= drop_last ? gz[L - 1 + b - threadIdx.x] : 0.f;
     copies_wait<0>();
@@ -859,11 +869,11 @@ __global__ void __launch_bounds__(TcPlan<D>::kThreads, TcPlan<D>::kCtas) chunks(
           uint32_t q[4];
           ldsm(rows_q + 32 * i, q);
 #pragma unroll
-          for (int g = 0; g < kOV / 2; ++g) {
+          for (int g = 0; g < kOV; ++g) {   // (one part of S, then the other: a sum's products far apart)
             uint32_t t[4];
-            ldsm_t(base + P::kS + 16 * i * P::kPitchV + kOB * ch + 32 * g + v_off, t);
-            mma(acc[2 * g], q, t[0], t[1]);
-            mma(acc[2 * g + 1], q, t[2], t[3]);
+            ldsm_t(base + (g < kOV / 2 ? P::kS : P::low(stage)) + 16 * i * P::kPitchV + kOB * ch + 32 * (g % (kOV / 2)) + v_off, t);
+            mma(acc[2 * (g % (kOV / 2))], q, t[0], t[1]);
+            mma(acc[2 * (g % (kOV / 2)) + 1], q, t[2], t[3]);
           }
         }
 #pragma unroll
@@ -913,15 +923,16 @@ __global__ void __launch_bounds__(TcPlan<D>::kThreads, TcPlan<D>::kCtas) chunks(
             f[i] = tc::f2_pack(d > 0 ? 0.f : a0, d > 1 ? 0.f : a1);
           }
         }
-        uint32_t p[4];
+        uint32_t p[4], r[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = bf16_of(f[i]);
+        for (int i = 0; i < 4; ++i) p[i] = bf16_of(f[i]), r[i] = bf16_of(tc::f2_sub(f[i], pair_of(p[i])));
 #pragma unroll
-        for (int g = 0; g < kOV / 2; ++g) {
-          uint32_t v[4];
-          ldsm_t(v_at + (uint32_t)(16 * kb * P::kPitchV) + kOB * ch + 32 * g + v_off, v);
-          mma(acc[2 * g], p, v[0], v[1]);
-          mma(acc[2 * g + 1], p, v[2], v[3]);
+        for (int g = 0; g < kOV / 2; g += 2) {
+          uint32_t v[2][4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) ldsm_t(v_at + (uint32_t)(16 * kb * P::kPitchV) + kOB * ch + 32 * (g + i) + v_off, v[i]);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) mma(acc[2 * g + i % 4], i < 4 ? p : r, v[i / 2 % 2][2 * (i % 2)], v[i / 2 % 2][2 * (i % 2) + 1]);
         }
       }
       // What is not finite: 0 times it is NaN (columns of padding are 0).
@@ -947,7 +958,12 @@ __global__ void __launch_bounds__(TcPlan<D>::kThreads, TcPlan<D>::kCtas) chunks(
             for (int k = 0; k < K; ++k) {
               const float qk = val(q, k) * (h ? e1 : e0);
 #pragma unroll
-              for (int i = 0; i < 2 * kOV; ++i) o[i] += qk * val(sm + P::kS + k * P::kPitchV, 8 * (kOV * ch + i / 2) + 2 * tq + i % 2);
+              for (int i = 0; i < 2 * kOV; ++i) {
+                const unsigned char* s = sm + k * P::kPitchV;
+                const int v = 8 * (kOV * ch + i / 2) + 2 * tq + i % 2;
+                const float hi = val(s + P::kS, v);
+                o[i] += qk * (finite(hi) ? hi + val(s + P::low(stage), v) : hi);
+              }
             }
           for (int j = h ? from1 : from0; j <= r; ++j) {
             float qk = 0.f;
@@ -992,6 +1008,7 @@ __global__ void __launch_bounds__(TcPlan<D>::kThreads, TcPlan<D>::kCtas) chunks(
       if (P::kSplit > 1) asm volatile("bar.sync %0, 64;" ::"r"(1 + rb) : "memory");
       else __syncwarp();        // (the rows of q have been read)
       fetch_q(x2, L2);
+      if (P::kInV && received) __syncthreads();  // (and S)
       fetch_v(x2, L2, stage ^ 1);
     }
     copies_commit();
@@ -1075,7 +1092,7 @@ __global__ void __launch_bounds__(TcPlan<D>::kThreads, TcPlan<D>::kCtas) chunks(
     __syncthreads();            // (S has been read)
     // ---- the end of a chain's segment
     if (!last) {
-      if (!kStates) plane_out();
+      if (!kStates) plane_out(stage ^ 1);
     } else {
       if (!kStates && w.o.p && c.lengths) {  // steps behind the end
         const int64_t lo = (int64_t)x.seg * c.seg_len, hi = min(c.T, lo + c.seg_len);
