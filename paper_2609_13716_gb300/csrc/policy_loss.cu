@@ -72,12 +72,13 @@ struct Sums {
   float mx = -kInf, s = 0.f, u = 0.f, t = 0.f, my = -kInf, sy = 0.f;
 };
 
-// Moves a row's sums to the maximum `to` of x, and by shift_y in y.  Empty ones, and ones that vanish, become 0.
+// Moves a row's sums to the maximum `to` of x, and by shift_y in y.  Empty ones, and ones that vanish, become 0; s that is
+// not a number stays so, whatever the factor.
 __device__ __forceinline__ void move_x(Sums& a, float to, float shift_y) {
   const float d = a.mx - to, r = a.mx == -kInf ? 0.f : exp_of(d);
   a.t = r > 0.f ? r * (a.t + a.s * (d - shift_y)) : 0.f;
   a.u = r > 0.f ? r * (a.u + a.s * d) : 0.f;
-  a.s = r > 0.f ? r * a.s : 0.f;
+  a.s = r * a.s;
   a.mx = to;
 }
 template <bool kRef>
@@ -241,8 +242,10 @@ __device__ __forceinline__ void tile_in(T* dst, const T* src, int64_t ld, int ro
   }
 }
 
-// Beyond this a logit's distance to the maximum may be infinite.
-constexpr float kFar = -1e30f;
+// What stands for a logit that has no part, and the lowest one that is taken as it is: its distance to any other logit is
+// finite, and 2^-100 of it above 0.  A power of two, so that its product with log2 e is exact but for that factor.
+constexpr float kFar = -1.2676506002282294e30f;   // -2^100
+constexpr uint32_t kFarBf16 = 0xF180F180u;        // a pair of them
 
 // Four elements of a row.
 __device__ __forceinline__ void load_4(const float* p, bool whole, int left, float (&v)[4]) {
@@ -519,7 +522,26 @@ __device__ __forceinline__ float greatest(const uint4& a, const float (&)[8]) {
   return fmaxf(__low2float(h), __high2float(h));
 }
 
-// Puts kFar in the place of what is not legal: 2^a of it is 0, and times it as well.
+// Least of V elements (not a number: ignored).
+__device__ __forceinline__ float least(const uint4&, const float (&v)[4]) { return fminf(fminf(v[0], v[1]), fminf(v[2], v[3])); }
+__device__ __forceinline__ float least(const uint4& a, const float (&)[8]) {
+  const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&a);
+  const __nv_bfloat162 h = __hmin2(__hmin2(p[0], p[1]), __hmin2(p[2], p[3]));
+  return fminf(__low2float(h), __high2float(h));
+}
+// Logits below kFar (-inf and the type's lowest value among them) become it; what is not a number stays so.
+__device__ __forceinline__ void lift(uint4& a, const float (&)[4]) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&a);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+r"(w[i]) : "r"(__float_as_uint(kFar)));
+}
+__device__ __forceinline__ void lift(uint4& a, const float (&)[8]) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&a);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(kFarBf16));
+}
+
+// Puts kFar in the place of what is not legal.
 template <int V, bool kRef>
 __device__ __forceinline__ void hide(const uint8_t* legal, float (&x)[V], float (&y)[V]) {
 #pragma unroll
@@ -545,13 +567,16 @@ __device__ __forceinline__ void add_each(Sums& s, const float (&x)[V], const flo
   }
 }
 
-// The sums of a thread over elements that are all legal, as pairs and in units of ln 2: with a = x log2 e - cx, b = y
-// log2 e - cy (cx, cy: the maxima times log2 e, rounded), s = sum 2^a, u = sum 2^a a, v = sum 2^a b, sy = sum 2^b.  Rounding
-// of cx and cy moves all a and b of a row alike and falls out of H, KL and the gradient.  Arithmetic in pairs for an element
-// and its reference, and no element is looked at: of what is infinitely far 0 * inf makes a sum NaN.
+// The sums of a thread, as pairs and in units of ln 2: with a = x log2 e - cx, b = y log2 e - cy (cx, cy: the maxima times
+// log2 e, rounded), s = sum 2^a, u = sum 2^a a, v = sum 2^a b, sy = sum 2^b.  Rounding of cx and cy moves all a and b of a
+// row alike and falls out of H, KL and the gradient.  Arithmetic in pairs for an element and its reference, and no element
+// is looked at.  That is right where x and y are kFar or more: all a and b are finite then, and what stands at kFar adds 0
+// as soon as a maximum lies above it.  x is lifted to that; a lower y, whose KL may be infinite, makes s NaN, as do +inf and
+// what is not a number.  Until a maximum lies above kFar the sums hold what stands for nothing: `raise` takes it to 0, and
+// `sums_of` leaves it out.
 struct Pairs {
   uint64_t s = 0, u = 0, v = 0, sy = 0;
-  float mx = -kInf, my = -kInf;
+  float mx = kFar, my = kFar, low = 0.f;
 };
 __device__ __forceinline__ uint64_t both(float v) { return tc::f2_pack(v, v); }
 __device__ __forceinline__ uint64_t exp2_of(uint64_t v) {
@@ -561,31 +586,34 @@ __device__ __forceinline__ uint64_t exp2_of(uint64_t v) {
 }
 template <bool kRef> __device__ __forceinline__ void raise(Pairs& p, float hx, float hy) {
   const float mx = fmaxf(p.mx, hx), my = fmaxf(p.my, hy);
-  if (p.mx == -kInf) {          // (nothing yet)
-    p.s = p.u = p.v = p.sy = 0;
-  } else {
-    const float dx = p.mx * kLog2e - mx * kLog2e, dy = kRef ? p.my * kLog2e - my * kLog2e : 0.f;
-    const uint64_t r = both(tc::ex2_approx(dx));
-    p.u = tc::f2_mul(r, tc::f2_fma(p.s, both(dx), p.u));
-    if (kRef) {
-      p.v = tc::f2_mul(r, tc::f2_fma(p.s, both(dy), p.v));
-      p.sy = tc::f2_mul(both(tc::ex2_approx(dy)), p.sy);
-    }
-    p.s = tc::f2_mul(r, p.s);
+  const float dx = p.mx * kLog2e - mx * kLog2e, dy = kRef ? p.my * kLog2e - my * kLog2e : 0.f;
+  const uint64_t r = both(tc::ex2_approx(dx));
+  p.u = tc::f2_mul(r, tc::f2_fma(p.s, both(dx), p.u));
+  if (kRef) {
+    p.v = tc::f2_mul(r, tc::f2_fma(p.s, both(dy), p.v));
+    p.sy = tc::f2_mul(both(tc::ex2_approx(dy)), p.sy);
   }
+  p.s = tc::f2_mul(r, p.s);
   p.mx = mx, p.my = my;
 }
 template <int V, bool kRef>
-__device__ __forceinline__ void add_block(Pairs& p, float (&x)[V], float (&y)[V], const uint4& xw, const uint4& yw, const uint8_t* legal) {
+__device__ __forceinline__ void add_block(Pairs& p, uint4 xw, const uint4& yw, const uint8_t* legal) {
+  float x[V], y[V];
+  lift(xw, x);
+  values(xw, x);
+  if (kRef) values(yw, y);
   float hx, hy = 0.f;
   if (legal) {
     hide<V, kRef>(legal, x, y);
     hx = x[0], hy = y[0];
 #pragma unroll
     for (int i = 1; i < V; ++i) hx = fmaxf(hx, x[i]), hy = fmaxf(hy, y[i]);
+    if (kRef)
+#pragma unroll
+      for (int i = 0; i < V; ++i) p.low = fminf(p.low, y[i]);
   } else {
     hx = greatest(xw, x);
-    if (kRef) hy = greatest(yw, y);
+    if (kRef) hy = greatest(yw, y), p.low = fminf(p.low, least(yw, y));
   }
   if (hx > p.mx || (kRef && hy > p.my)) raise<kRef>(p, hx, hy);   // (rare after the first blocks)
   const uint64_t l2 = both(kLog2e), cx = both(-p.mx * kLog2e), cy = both(-p.my * kLog2e);
@@ -604,7 +632,6 @@ __device__ __forceinline__ void add_block(Pairs& p, float (&x)[V], float (&y)[V]
 // As sums about the maxima themselves.
 template <bool kRef> __device__ __forceinline__ Sums sums_of(const Pairs& p) {
   Sums m;
-  if (p.mx == -kInf && !(p.s != 0)) return m;
   constexpr float kLn2 = 0.6931471805599453f;
   float a, b, v = 0.f;
   m.mx = p.mx, m.my = kRef ? p.my : -kInf;
@@ -613,16 +640,18 @@ template <bool kRef> __device__ __forceinline__ Sums sums_of(const Pairs& p) {
   if (kRef) {
     tc::f2_unpack(p.v, a, b), v = a + b;
     tc::f2_unpack(p.sy, a, b), m.sy = a + b;
+    if (p.low < kFar) m.s = kInf - kInf;
   }
   // x log2 e - mx log2 e is a less what cx was rounded by
   const float ox = fmaf(p.mx, kLog2e, -(p.mx * kLog2e)), oy = kRef ? fmaf(p.my, kLog2e, -(p.my * kLog2e)) : 0.f;
   const float rx = tc::ex2_approx(-ox);
   if (kRef) {
     m.t = rx * (m.u - v - m.s * (ox - oy)) * kLn2;
-    m.sy *= tc::ex2_approx(-oy);
+    m.sy = p.my > kFar ? m.sy * tc::ex2_approx(-oy) : 0.f * m.sy;
   }
   m.u = rx * (m.u - m.s * ox) * kLn2;
   m.s *= rx;
+  if (!(p.mx > kFar)) m.mx = -kInf, m.s *= 0.f, m.u = 0.f, m.t = 0.f;
   return m;
 }
 
@@ -666,10 +695,7 @@ __device__ __forceinline__ Sums add_vectors(const uint4* xv, const uint4* yv, co
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
       if (v0 + k * step < n) {
-        float x[V], y[V];
-        values(xw[k], x);
-        if (kRef) values(yw[k], y);
-        add_block<V, kRef>(p, x, y, xw[k], yw[k], legal ? legal + (v0 + k * step) * V : nullptr);
+        add_block<V, kRef>(p, xw[k], yw[k], legal ? legal + (v0 + k * step) * V : nullptr);
       }
   }
   return sums_of<kRef>(p);
@@ -696,8 +722,11 @@ template <bool kRef, int kLanes = 32> __device__ __forceinline__ void join_warp(
 }
 __device__ __forceinline__ void put(float* p, const Sums& t) { p[0] = t.mx, p[1] = t.s, p[2] = t.u, p[3] = t.t, p[4] = t.my, p[5] = t.sy; }
 __device__ __forceinline__ Sums got(const float* p) { return Sums{p[0], p[1], p[2], p[3], p[4], p[5]}; }
-// Whether the pairs' sums of a row that takes part gave no number.
-__device__ __forceinline__ bool lost(const Sums& s) { return !(fabsf(s.s) + fabsf(s.u) + fabsf(s.t) + fabsf(s.sy) < kInf); }
+// Whether the pairs' sums of a row that takes part say nothing of it: no number, or no logit, its own or the reference's,
+// above kFar.
+template <bool kRef> __device__ __forceinline__ bool lost(const Sums& s) {
+  return !(fabsf(s.s) + fabsf(s.u) + fabsf(s.t) + fabsf(s.sy) < kInf) || !(s.mx > kFar) || (kRef && !(s.my > kFar));
+}
 
 // The gradient of a share of a row.  `act`: the action's place in it.
 template <typename E, bool kRef>
@@ -708,7 +737,9 @@ __device__ __forceinline__ void grad_vectors(const Row& r, const uint4* xv, cons
   for (int v = lane; v < n; v += step) {
     float x[V], y[V], g[V];
     if (r.on) {
-      values(load_16(xv + v, first), x);
+      uint4 xw = load_16(xv + v, first);
+      if (!far) lift(xw, x);
+      values(xw, x);
       if (kRef) values(load_16(yv + v, first), y);
       const int k = act - v * V;
       if (far) {
@@ -806,7 +837,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) rows(const __grid_c
         s = Sums{};
         for (int k = 0; k < kParts; ++k) join<kRef>(s, got(set + k * 6));
       }
-      if (far || !on || !lost(s)) break;    // (the same for all threads of the row)
+      if (far || !on || !lost<kRef>(s)) break;    // (the same for all threads of the row)
       far = true, turn ^= 1;
     }
     const Row r = finish<kRef>(l, m, on, xa, s, lane == 0, acc);
