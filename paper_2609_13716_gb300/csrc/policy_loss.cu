@@ -86,7 +86,7 @@ __device__ __forceinline__ void move_to(Sums& a, float mx, float my) {
   const float dy = kRef && a.my != -kInf ? a.my - my : 0.f;
   move_x(a, mx, dy);
   if (kRef) {
-    a.sy = a.my == -kInf ? 0.f : a.sy * exp_of(dy);
+    a.sy *= a.my == -kInf ? 0.f : exp_of(dy);
     a.my = my;
   }
 }
