@@ -563,6 +563,7 @@ aht_status aht_group_norm_backward(const aht_group_norm_args* a, const float* me
  *        probability of the action alone, exp(d) - 1 - d, d = ref_logp - logp; 0 without either,
  *   l = -min(r adv, clamp(r, 1 - clip_low, 1 + clip_high) adv) + kl_coef KL - ent_coef H,
  *   loss = sum_m w_m l_m.
+ * With kl_coef = 0 KL is in stats alone (it may be infinite, where the reference leaves an action out).
  * Of a minimum that the clamped term has alone the gradient is 0.  A row takes no part (its logp and
  * gradient are 0) if its action is not in 0..A-1 or not legal, as for steps behind an episode's end, or if
  * the mask leaves nothing of it: no action legal, or every legal logit -inf.  Logits of actions that are not

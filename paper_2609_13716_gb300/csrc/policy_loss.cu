@@ -102,7 +102,7 @@ struct Acc {
   float hi = 0.f, lo = 0.f;
   __device__ __forceinline__ void add(float v) {
     const float s = hi + v, b = s - hi;
-    lo += (hi - (s - b)) + (v - b);
+    lo += fabsf(s) < kInf ? (hi - (s - b)) + (v - b) : 0.f;   // (an infinite sum stays infinite)
     hi = s;
   }
 };
@@ -138,7 +138,7 @@ __device__ __forceinline__ Row finish(const Loss& l, int64_t m, bool on, float x
   } else if (l.ref_logp) {
     const float d = l.ref_logp[m] - logp;
     kl = excess(d);
-    at -= l.kl * expm1f(d);
+    if (l.kl > 0.f) at -= l.kl * expm1f(d);
   }
   if (first) {
     if (l.logp) l.logp[m] = logp;
@@ -151,7 +151,7 @@ __device__ __forceinline__ Row finish(const Loss& l, int64_t m, bool on, float x
   const float ws = w * inv;
   r.max_x = s.mx;
   r.max_y = s.my;
-  r.c = ws * (l.ent * (H - ls) - (kRef ? l.kl * (ls - lsy + kl) : 0.f) - at);
+  r.c = ws * (l.ent * (H - ls) - (kRef && l.kl > 0.f ? l.kl * (ls - lsy + kl) : 0.f) - at);
   r.cx = ws * (l.ent + (kRef ? l.kl : 0.f));
   r.cy = kRef ? ws * l.kl : 0.f;
   r.at = w * at;
@@ -163,10 +163,13 @@ template <bool kRef>
 __device__ __forceinline__ float slope(const Row& r, float x, float y, bool is_action) {
   const float xm = x - r.max_x, e = exp_of(xm);
   float g = r.c + r.cx * xm;
-  if (kRef) g -= r.cy * (y - r.max_y);
+  if (kRef && r.cy != 0.f) g -= r.cy * (y - r.max_y);   // (without a KL term y may be infinite)
   g = e == 0.f ? 0.f : e * g;   // (0 * inf)
   return is_action ? g + r.at : g;
 }
+
+// kl_coef KL; without a coefficient nothing, whatever KL is.
+__device__ __forceinline__ double kl_term(const Loss& l, double kl) { return l.kl > 0.f ? (double)l.kl * kl : 0.; }
 
 // The CTA's totals: threads in order through shared memory.
 __device__ void totals(const Loss& l, const Acc (&acc)[kSums], double* tmp) {
@@ -188,7 +191,7 @@ __device__ void totals(const Loss& l, const Acc (&acc)[kSums], double* tmp) {
   if (gridDim.x == 1) {
     __syncthreads();
     if (threadIdx.x == 0) {
-      l.stats[0] = (float)(tmp[0] + (double)l.kl * tmp[1] - (double)l.ent * tmp[2]);
+      l.stats[0] = (float)(tmp[0] + kl_term(l, tmp[1]) - (double)l.ent * tmp[2]);
       for (int i = 0; i < kSums; ++i) l.stats[i + 1] = (float)tmp[i];
     }
   }
@@ -216,7 +219,7 @@ __global__ void __launch_bounds__(32 * kSums * kSumWarps) sum_parts(const __grid
     sum[j] = (tmp[0][j] + tmp[1][j]) + (tmp[2][j] + tmp[3][j]);
     l.stats[j + 1] = (float)sum[j];
   }
-  l.stats[0] = (float)(sum[0] + (double)l.kl * sum[1] - (double)l.ent * sum[2]);
+  l.stats[0] = (float)(sum[0] + kl_term(l, sum[1]) - (double)l.ent * sum[2]);
 }
 
 // ---- few actions: dense tiles of rows -------------------------------------------------------
