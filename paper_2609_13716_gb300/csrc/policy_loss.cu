@@ -126,10 +126,11 @@ __device__ __forceinline__ Row finish(const Loss& l, int64_t m, bool on, float x
   }
   const float w = l.weight ? l.weight[m] : l.w, adv = l.adv[m];
   const float ls = logf(s.s), logp = (xa - s.mx) - ls, inv = 1.f / s.s, H = ls - s.u * inv;
-  const float ratio = expf(logp - l.old_logp[m]);
+  const float moved = logp - l.old_logp[m], ratio = expf(moved);
   const bool clipped = adv > 0.f ? ratio > l.hi : adv < 0.f && ratio < l.lo;
   const float inside = ratio < l.lo ? l.lo : ratio > l.hi ? l.hi : ratio;  // (NaN stays)
-  const float a = ratio * adv, b = inside * adv;
+  // (a ratio beyond fp32's range is a number all the same)
+  const float a = adv == 0.f && moved < kInf && ratio == kInf ? 0.f : ratio * adv, b = inside * adv;
   const float pg = -(b < a ? b : a);
   float kl = 0.f, at = clipped ? 0.f : -a, lsy = 0.f;
   if (kRef) {
