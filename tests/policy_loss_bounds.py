@@ -25,6 +25,7 @@ def _sum_rows(x, ok):
     return xm, np.log(np.exp(xm).sum(1))
 
 
+@np.errstate(invalid="ignore", over="ignore")     # (of masked places, which nothing below reads)
 def bounds(x, actions, old_logp, adv, legal=None, weight=None, ref_logits=None, ref_logp=None, clip_low=0.2, clip_high=0.2,
            kl_coef=0.0, ent_coef=0.0, half_step=2.0 ** -24, want=None):
     """want: the reference's (stats, logp, dlogits).  -> tolerances of the three.  Rows take part with finite sums."""

@@ -1,0 +1,55 @@
+"""The clipped policy loss entry by entry: tolerances proportional to each entry of the gradient (policy_loss_bounds.py),
+over the ranges of rows, actions, masks, strides and types."""
+import numpy as np
+import pytest
+import torch
+
+import policy_loss_ref as R
+import test_gpu_policy_loss as L
+from policy_loss_bounds import bounds
+
+pytestmark = pytest.mark.gpu
+
+
+def check(d):
+    got = L.run(d)
+    a = {k: L.to64(v) for k, v in dict(x=d["logits"], actions=d["actions"], old_logp=d["old_logp"], adv=d["advantages"], legal=d["legal"],
+                                       weight=d["weight"], ref_logits=d["ref_logits"], ref_logp=d["ref_logp"]).items()}
+    want = R.loss(**a, **L.COEF)
+    tol = bounds(**a, **L.COEF, want=want, half_step=2.0 ** -8 if d["logits"].dtype is torch.bfloat16 else 2.0 ** -24)
+    for n, ref, t in zip(("stats", "logp", "dlogits"), want, tol):
+        have = L.to64(got[n])
+        bad = ~(np.abs(have - ref) <= t)
+        assert not bad.any(), (n, int(bad.sum()), np.argwhere(bad)[:4].tolist(), have[bad][:4], ref[bad][:4], t[bad][:4])
+
+
+@pytest.mark.parametrize("dtype", L.DTYPES)
+@pytest.mark.parametrize("ref", ["logits", "logp", "none"])
+@pytest.mark.parametrize("M,A", [(1, 1), (1, 6), (64, 6), (127, 5), (128, 8), (129, 17), (300, 20), (257, 21), (257, 32), (200, 33), (131, 64),
+                                 (50, 65), (33, 127), (40, 1000), (9, 1024), (7, 1025), (5, 4099), (3, 8192), (3, 8200),
+                                 (2, 20011), (3, 65536), (1, 300001)])
+def test_entries(M, A, ref, dtype):
+    check(L.make(M, A, dtype, ref, seed=M + A, weight=M % 2 == 1))
+
+
+@pytest.mark.parametrize("dtype", L.DTYPES)
+@pytest.mark.parametrize("spare", [0, 1, 2, 8])
+@pytest.mark.parametrize("M,A", [(300, 6), (300, 20), (130, 64), (64, 100), (33, 512), (20, 1500), (3, 9001), (2, 65536)])
+def test_entries_of_masked_and_strided_rows(M, A, spare, dtype):
+    check(L.make(M, A, dtype, "logits", legal=True, spare=spare, seed=A, weight=True))
+
+
+@pytest.mark.parametrize("dtype", L.DTYPES)
+@pytest.mark.parametrize("M,A", [(50, 100), (20, 1500), (3, 9001)])
+def test_a_reference_that_is_aligned_otherwise(M, A, dtype):
+    """Logits that are slices of a wider output against dense rows."""
+    d = L.make(M, A, dtype, "logits", spare=1, seed=A)
+    d["ref_logits"] = d["ref_logits"].contiguous()
+    check(d)
+
+
+@pytest.mark.parametrize("dtype", L.DTYPES)
+@pytest.mark.parametrize("A", [6, 64, 100, 1500, 9001])
+def test_entries_of_wide_distributions(A, dtype):
+    """Logits of a spread of 40: most probabilities are 0 beside a few."""
+    check(L.make(20, A, dtype, "logits", seed=A, scale=40.0))
