@@ -867,11 +867,12 @@ aht_status run(const Norm& a, const How& h, bool back, int* rows, cudaStream_t s
   const int64_t t = h.threads;
   const int64_t slots = h.vpc <= t ? (p.part + t / h.vpc - 1) / (t / h.vpc) : p.part * ((h.vpc + t - 1) / t);
   const int64_t bytes = slots * t * (int)sizeof(typename Raw<E, V>::T) * (back ? 2 : 1);
-  p.hold = bytes <= (t == kFew ? kHoldFew : kHold);
-  const int64_t most = back ? std::max(1, kCtas / (a.G * h.cl)) : 65536;
-  const dim3 grid((unsigned)(std::min<int64_t>(a.N, most) * h.cl), (unsigned)a.G);
+  const int most = t == kFew ? kHoldFew : kHold;
+  p.hold = bytes <= most;
+  const int64_t samples = back ? std::max(1, kCtas / (a.G * h.cl)) : 65536;
+  const dim3 grid((unsigned)(std::min<int64_t>(a.N, samples) * h.cl), (unsigned)a.G);
   *rows = (int)grid.x;
-  const Shape sh{grid, dim3((unsigned)t), p.hold ? (int)bytes : 0, h.cl};
+  const Shape sh{grid, dim3((unsigned)t), p.hold ? (int)bytes : 0, h.cl, most};
   if (t == kFew) return back ? launch_op(large_bwd<E, V, kFew>, sh, s, a, p) : launch_op(large_fwd<E, V, kFew>, sh, s, a, p);
   return back ? launch_op(large_bwd<E, V, kMany>, sh, s, a, p) : launch_op(large_fwd<E, V, kMany>, sh, s, a, p);
 }

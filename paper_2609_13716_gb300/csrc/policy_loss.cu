@@ -852,12 +852,22 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) rows(const __grid_c
   totals(l, acc, tmp);
 }
 
+// Shared memory of a tile.
+template <typename E> int tile_bytes(int A, bool ref, bool legal) {
+  return (ref ? 2 : 1) * ((kTileRows * A * (int)sizeof(E) + 15) / 16 * 16) + (legal ? (kTileRows * A + 15) / 16 * 16 : 0);
+}
+
+template <typename E, bool kRef, bool kLegal, int kG>
+aht_status launch_tiles(Shape sh, const Loss& l, int64_t n_tiles, cudaStream_t s) {
+  sh.most = tile_bytes<E>(kG > 0 ? 4 * kG : kTileA, kRef, kLegal);
+  return launch_op(tiles<E, kRef, kLegal, kG>, sh, s, l, n_tiles);
+}
 template <typename E, bool kRef, bool kLegal>
 aht_status run_tiles(const Shape& sh, const Loss& l, int64_t n_tiles, cudaStream_t s) {
-  if (l.A <= 8) return launch_op(tiles<E, kRef, kLegal, 2>, sh, s, l, n_tiles);
-  if (l.A <= 20) return launch_op(tiles<E, kRef, kLegal, 5>, sh, s, l, n_tiles);
-  if (l.A <= 32) return launch_op(tiles<E, kRef, kLegal, 8>, sh, s, l, n_tiles);
-  return launch_op(tiles<E, kRef, kLegal, 0>, sh, s, l, n_tiles);
+  if (l.A <= 8) return launch_tiles<E, kRef, kLegal, 2>(sh, l, n_tiles, s);
+  if (l.A <= 20) return launch_tiles<E, kRef, kLegal, 5>(sh, l, n_tiles, s);
+  if (l.A <= 32) return launch_tiles<E, kRef, kLegal, 8>(sh, l, n_tiles, s);
+  return launch_tiles<E, kRef, kLegal, 0>(sh, l, n_tiles, s);
 }
 
 template <typename E, bool kRef>
@@ -866,8 +876,7 @@ aht_status go(const Loss& l, cudaStream_t s) {
   aht_status e;
   if (l.A <= kTileA) {
     const int64_t n_tiles = (l.M + kTileRows - 1) / kTileRows;
-    const int A = (int)l.A, bytes = (kTileRows * A * (int)sizeof(E) + 15) / 16 * 16;
-    const int smem = (kRef ? 2 : 1) * bytes + (l.legal ? (kTileRows * A + 15) / 16 * 16 : 0);
+    const int smem = tile_bytes<E>((int)l.A, kRef, l.legal != nullptr);
     ctas = std::min<int64_t>(n_tiles, 152 * std::max(1, std::min(l.A > 20 ? 4 : kTileCtas, 226 * 1024 / (smem + 2048))));
     const Shape sh{dim3((unsigned)ctas), dim3(kTileRows), smem};
     e = l.legal ? run_tiles<E, kRef, true>(sh, l, n_tiles, s) : run_tiles<E, kRef, false>(sh, l, n_tiles, s);
