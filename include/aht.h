@@ -552,6 +552,9 @@ int64_t aht_group_norm_workspace(int64_t N, int64_t L, int32_t C, int32_t G, int
 aht_status aht_group_norm_backward(const aht_group_norm_args* a, const float* mean, const float* rstd, const aht_seq* dy,
                                    const aht_seq* dx, float* dweight, float* dbias, void* workspace,
                                    int64_t workspace_bytes, void* cuda_stream);
+/* Test hook (no paper counterpart), process-wide: few long instances are laid out as on a device that places clusters of
+ * at most `most` CTAs (8 or 16; 0: what the device says). */
+aht_status aht_debug_group_norm_cluster(int32_t most);
 
 /* ---- Clipped policy loss with a KL term, and its gradient -------------------------------
  * The clipped surrogate (App. C "PPO ego") of any policy's logits, with the distance to a reference

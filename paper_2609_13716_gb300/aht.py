@@ -34,7 +34,7 @@ EXPORTED = ["aht_create", "aht_destroy", "aht_reset", "aht_rollout", "aht_xplay_
             "aht_muon_step", "aht_muon_orthogonalize", "aht_muon_sync", "aht_debug_muon_expire",
             "aht_linattn_workspace", "aht_linattn_forward", "aht_linattn_backward",
             "aht_policy_loss_workspace", "aht_policy_loss", "aht_group_norm_workspace", "aht_group_norm_forward",
-            "aht_group_norm_backward"]
+            "aht_group_norm_backward", "aht_debug_group_norm_cluster"]
 
 
 class AhtError(RuntimeError):
@@ -156,6 +156,8 @@ def load() -> C.CDLL:
             L.aht_group_norm_forward.restype = C.c_int
             L.aht_group_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
             L.aht_group_norm_backward.restype = C.c_int
+            L.aht_debug_group_norm_cluster.argtypes = [i32]
+            L.aht_debug_group_norm_cluster.restype = C.c_int
             L.aht_muon_create.argtypes = [i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(MuonConfig), vp, C.POINTER(vp)]
             L.aht_muon_destroy.argtypes = [vp]
             L.aht_muon_destroy.restype = None
@@ -1020,6 +1022,11 @@ def aht_group_norm_backward(x, groups, mean, rstd, dy, dx, weight=None, bias=Non
                                           _glr_ptr(dweight, f32, (shape[2],), "dweight", dev),
                                           _glr_ptr(dbias, f32, (shape[2],), "dbias", dev), *_workspace(workspace, dev),
                                           _stream(stream, dev)))
+
+
+def aht_debug_group_norm_cluster(most: int):
+    """Test hook: few long instances as on a device that places clusters of at most 8 or 16 CTAs (0: ask it)."""
+    _check(load().aht_debug_group_norm_cluster(most))
 
 
 # ---- clipped policy loss -------------------------------------------------------------------

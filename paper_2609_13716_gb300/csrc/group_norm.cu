@@ -19,6 +19,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "op_launch.cuh"
 
@@ -789,6 +790,33 @@ constexpr int kCtas = 152 * 4;             // of a pass that keeps sums, and row
 constexpr int kMaxCluster = 8, kWideCluster = 16;   // CTAs of a cluster: of any, of few instances (beyond what every device runs)
 constexpr int kHold = 72 * 1024, kHoldFew = 192 * 1024;   // shared memory for an instance's part (else L2 holds it), by threads
 
+// Whether the current device places a cluster of kWideCluster CTAs of kFew threads with all the shared memory that they may
+// hold (no GPC of a part of a GPU need have sixteen SMs).  The kernel with the most static memory answers for all; the
+// answer is asked for once a device.
+std::atomic<int> g_most_ctas{0};           // aht_debug_group_norm_cluster; 0: ask
+bool runs_wide() {
+  if (const int most = g_most_ctas) return most >= kWideCluster;
+  constexpr int kDevices = 64;
+  static std::atomic<signed char> known[kDevices];   // 1: it does, -1: it does not
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  if (dev < kDevices && known[dev]) return known[dev] > 0;
+  const auto kernel = large_bwd<__nv_bfloat16, 8, kFew>;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim = {(unsigned)kWideCluster, 1, 1};
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(kWideCluster), cfg.blockDim = dim3(kFew), cfg.dynamicSmemBytes = kHoldFew;
+  cfg.attrs = &attr, cfg.numAttrs = 1;
+  int n = 0;
+  const bool wide = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldFew) == cudaSuccess &&
+                    cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                    cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0;
+  if (!wide) cudaGetLastError();             // (nothing of the question stays behind)
+  if (dev < kDevices) known[dev] = wide ? 1 : -1;
+  return wide;
+}
+
 // How a call's instances are laid on threads.
 struct How {
   bool small;
@@ -825,9 +853,10 @@ How how(const aht_group_norm_args* a, int V) {
   if (h.cl == kMaxCluster) {
     // Few instances get whole SMs, and clusters of 16 where there are no more of them than run at a time (so, and with 8
     // CTAs of 256 threads, us: 4000000 x 16 bf16 896, 4768; 10000 x 64 bf16 21, 44; 19 x 60000 x 32 bf16 115, 152; but
-    // 16 x 4000 x 64 bf16 30, 21).
-    if (insts <= 8 && vecs >= 4 * kMaxCluster * kFew) h.threads = kFew, h.cl = kWideCluster;
-    else if (insts > 8 && insts * kMaxCluster <= 152 && vecs >= 16 * kMaxCluster * kFew) h.threads = kFew;
+    // 16 x 4000 x 64 bf16 30, 21).  Where the device has no room for such a cluster: 8 CTAs of 256 threads.
+    if (insts <= 8 && vecs >= 4 * kMaxCluster * kFew) {
+      if (runs_wide()) h.threads = kFew, h.cl = kWideCluster;
+    } else if (insts > 8 && insts * kMaxCluster <= 152 && vecs >= 16 * kMaxCluster * kFew) h.threads = kFew;
   }
   return h;
 }
@@ -973,6 +1002,12 @@ aht_status aht_group_norm_backward(const aht_group_norm_args* a, const float* me
   if (aht_status e = pass(a, d, true, &rows, h, s)) return e;
   if (!sums || apart) return AHT_OK;
   return launch_op(fold, Shape{dim3((unsigned)((a->C + 7) / 8), 2), dim3(1024)}, s, (const float*)d.part, rows, a->C, dweight, dbias);
+}
+
+aht_status aht_debug_group_norm_cluster(int32_t most) {
+  if (most != 0 && most != kMaxCluster && most != kWideCluster) return set_last_error(AHT_EINVAL, "most must be 0, 8 or 16");
+  g_most_ctas = most;
+  return AHT_OK;
 }
 
 }  // extern "C"
