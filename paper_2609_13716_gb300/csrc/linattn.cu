@@ -13,8 +13,8 @@
 // reaches exactly the steps that the formulas give it to.  Rows of q, k and v come through a ring of asynchronous
 // copies, eight steps a stage.  Per step and column 2 K multiply-adds (in pairs, an operand of which comes from shared
 // memory once for a thread's columns); at 64x64 they are 128 of a warp's 318 instructions a step, and the issue of all
-// of them bounds it.  Decays cost no instruction: within a window of eight steps the state is kept divided
-// by g^j.
+// of them bounds it.  Decays cost no instruction: within a window of W steps the state is kept times g^(W - 1 - j), never
+// above its own size, so that it overflows where the result itself does.
 //
 // One step, the serving form, is a kernel of its own (`one_step`).
 //
@@ -196,8 +196,9 @@ __global__ void __launch_bounds__(32 * kWarps, KT * COLS > 64 ? 2 : 4) walk(cons
   const int64_t rst = back ? -c.N : c.N;
 
   const float l2 = log2_decay(c.log_decay, h);
-  // The state is kept divided by g^j for the j-th step of `win` steps, where g^-8 is far from overflow.
-  const int win = l2 < -4.0f ? 1 : kWindow;
+  // Behind the j-th step of `win` steps the state is kept times g^(win - 1 - j), at most 2^-8 times itself: below 2^-118,
+  // where fp32 has bits for no more than that, it loses some of its own.
+  const int win = l2 < -4.f ? 1 : l2 < -2.f ? 2 : l2 < -1.f ? 4 : kWindow;
 
   // ---- the state received
   uint64_t S[COLS][KT / 2];
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(32 * kWarps, KT * COLS > 64 ? 2 : 4) walk(cons
 #pragma unroll
   for (int x = 0; x < kStages - 1; ++x) fetch(first + x * kWindow, x);
 
-  // g^j within a window and its inverse
+  // g^j and its inverse
   float* pos = reinterpret_cast<float*>(mine + kStages * P::kStage + P::kConv);
   float* neg = pos + kWindow + 4;
   if (lane <= kWindow) pos[lane] = exp2f(l2 * lane), neg[lane] = exp2f(-l2 * lane);
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(32 * kWarps, KT * COLS > 64 ? 2 : 4) walk(cons
       for (int i = 0; i < KT / 2; ++i) S[y][i] = 0;
   };
   // A step decays what it receives (forward), or passes it on decayed (back).
-  if (!back && steps > 0 && !kStates) scale_by(pos[1]);
+  if (steps > 0 && !kStates) scale_by(pos[back ? win - 1 : win]);
 
   // After the KS threads' sums are joined a thread has kOwn columns of the output, from `oc` on.
   constexpr int kOwn = COLS > KS ? COLS / KS : 1;
@@ -383,11 +384,11 @@ __global__ void __launch_bounds__(32 * kWarps, KT * COLS > 64 ? 2 : 4) walk(cons
     const E* vf = raw + 2 * kWindow * P::kRawRow + col;
     kf += part * (KT + 4);
     qf += part * (KT + 4);
-    // one step, the e-th since the state was last multiplied
+    // one step, the e-th of its window
     auto step = [&](int j, int e) {
       uint64_t vv[COLS];
       {
-        const float down = w.in * neg[e];
+        const float down = w.in * pos[win - 1 - e];
         float a[COLS];
         if constexpr (COLS == 4 && sizeof(E) == 4) {
           const float4 f = *reinterpret_cast<const float4*>(vf + j * P::kVB);
@@ -429,7 +430,7 @@ __global__ void __launch_bounds__(32 * kWarps, KT * COLS > 64 ? 2 : 4) walk(cons
           }
         }
         float y[COLS];
-        const float up = w.out * pos[e];
+        const float up = w.out * neg[win - 1 - e];
 #pragma unroll
         for (int z = 0; z < COLS; ++z) {
           float a, b;
@@ -461,12 +462,13 @@ __global__ void __launch_bounds__(32 * kWarps, KT * COLS > 64 ? 2 : 4) walk(cons
       if (drops >> j & 1u) drop_all();
       step(j, e);
       if (++e == win) {
-        // (the last step of a forward walk hands its state on as it is)
-        scale_by(pos[!back && i0 + j + 1 == steps ? e - 1 : e]);
+        // (the last step of a forward walk hands its state on as it is, that of the other decayed)
+        if (i0 + j + 1 < steps) scale_by(pos[win]);
+        else if (back) scale_by(pos[1]);
         e = 0;
       }
     }
-    if (e > 0) scale_by(pos[!back && i0 + count == steps ? e - 1 : e]);
+    if (e > 0) scale_by(neg[win - e] * (back ? pos[1] : 1.f));   // (the last window of all: `win` divides a stage)
     __syncwarp();
     stage = stage == kStages - 1 ? 0 : stage + 1;
   }
