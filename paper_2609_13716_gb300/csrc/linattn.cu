@@ -1295,11 +1295,12 @@ How how(int64_t T, int64_t N, int H, int K, int V, int walks, bool bf16) {
     want = std::min<int64_t>(152 * (p.D == 64 ? TcPlan<64>::kCtas : TcPlan<128>::kCtas) / p.units, T / kC);
   } else {
     // 33 to 64 rows and columns, two layouts: a warp a head (half the operands from shared memory, 318 instructions a
-    // step for 418) or two warps with half the registers, which fill an SM twice as well.  fp32, first against second:
-    // 65537x1x8 64x64 412 against 606 us; 400x61x3 50x33, which the second runs unsplit, with its gradients 385
-    // against 330.
+    // step for 418) or two warps with half the registers, for so few heads that their steps, 32 at least to a segment,
+    // do not make 304 warps.  fp32 forward 64x64, first against second (us): T = 128, heads 8 48, 38; 64 52, 44; 152 54,
+    // 56; 549 114, 130; 1100 96, 125; 2432 184, 236; T = 1000, 8 58, 48; 64 89, 101; 549 503, 611; T = 61, 152 39, 39;
+    // 549 41, 47.  50x33 backward: T = 61, 150 39, 37; 600 39, 45; T = 400, 402 175, 192; 900 291, 289.
     const int64_t heads = N * H * walks;
-    if (deep > 32 && deep <= 64 && wide > 32 && wide <= 64 && (heads >= 152 * 8 || (T >= 64 && heads <= 456)))
+    if (deep > 32 && deep <= 64 && wide > 32 && wide <= 64 && heads * std::max<int64_t>(1, T / 32) >= 304)
       p.KT = 64, p.KS = 1, p.COLS = 2;
     else
       p.KT = deep > 64 ? 32 : 16, p.KS = deep > 32 ? 4 : deep > 16 ? 2 : 1, p.COLS = deep > 64 ? 2 : deep <= 16 && wide <= 32 ? 1 : 4;
