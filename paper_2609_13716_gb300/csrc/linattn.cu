@@ -1273,18 +1273,21 @@ struct How {
 };
 
 constexpr int kFill = 152 * 16;  // warps of `walk` that keep every SM busy
-// From how many steps on a bf16 pass goes by chunks: a chunk costs the same whatever it holds, a step of `walk` by the
-// size of its state.  Forward passes of 4 heads, chunks against `walk` (us): 256 envs 128x128 T = 2 54, 64; 4096 envs
-// 64x64 T = 8 188, 168, T = 12 189, 210; 32x32 T = 12 152, 128, T = 16 152, 142, T = 32 166, 224; 16x16 T = 32 158, 107,
-// T = 64 187, 190; 64 envs 16x16, which do not fill the GPU, T = 32 11, 17.
+// From how many steps of a chunk on a bf16 pass goes by chunks: one costs the same whatever it holds, a step of `walk` by the
+// size of its state, and few chains wait for steps (`few`: their chunks run at one time).  Forward passes of 4 heads,
+// chunks against `walk` (us): 256 envs 128x128 T = 2 55, 61; 512 envs 96x96 T = 4 98, 86; 4096 envs 64x64 T = 8 205, 164,
+// T = 10 203, 197, T = 12 205, 209; 64 envs 64x64 T = 6 12, 14; 4096 envs 32x32 T = 16 162, 143, T = 20 178, 170, T = 24 180,
+// 184; 150 envs 32x32 T = 12 12, 16; 4096 envs 16x16 T = 64 217, 195, T = 80 328, 238, T = 128 391, 367 (backward, a third of
+// the envs, T = 64 231, 256, T = 128 466, 487); 150 envs 16x16 T = 24 12, 14; 300 envs T = 24 18, 16, T = 48 21, 23.
 int chunk_steps(int deep, int64_t chains) {
-  return deep > 64 ? 2 : deep > 32 ? 10 : deep > 16 ? 20 : chains < kFill ? 32 : 64;
+  const bool few = chains <= 152 * 4;
+  return deep > 64 ? 2 : deep > 32 ? (few ? 6 : 10) : deep > 16 ? (few ? 12 : 20) : few ? 24 : chains <= 2 * 152 * 4 ? 32 : 60;
 }
 
 How how(int64_t T, int64_t N, int H, int K, int V, int walks, bool bf16) {
   How p{};
   const int wide = walks > 1 ? std::max(K, V) : V, deep = walks > 1 ? wide : K;   // (walks may have them exchanged)
-  p.tc = bf16 && T >= chunk_steps(deep, N * H * walks);
+  p.tc = bf16 && T >= chunk_steps(deep, N * H * walks) * ((T + kC - 1) / kC);
   int64_t want, len = std::max<int64_t>(T, 1);
   int step;
   if (p.tc) {
@@ -1306,7 +1309,7 @@ How how(int64_t T, int64_t N, int H, int K, int V, int walks, bool bf16) {
       p.KT = deep > 64 ? 32 : 16, p.KS = deep > 32 ? 4 : deep > 16 ? 2 : 1, p.COLS = deep > 64 ? 2 : deep <= 16 && wide <= 32 ? 1 : 4;
     p.units = heads * ((wide + 32 / p.KS * p.COLS - 1) / (32 / p.KS * p.COLS));
     step = kWindow;
-    want = std::min<int64_t>((p.KT == 64 ? 152 * 8 : kFill) / p.units, T / 32);
+    want = bf16 ? 1 : std::min<int64_t>((p.KT == 64 ? 152 * 8 : kFill) / p.units, T / 32);   // (few bf16 chains go by chunks)
   }
   if (want >= 2) {
     len = (T + want - 1) / want;
@@ -1325,7 +1328,7 @@ int64_t workspace_of(int64_t T, int64_t N, int H, int K, int V, int walks, bool 
 template <typename E, int KT, int KS, int COLS>
 aht_status run(const Chains& c, int64_t units, bool states, cudaStream_t s) {
   const Shape sh{dim3((unsigned)((units + kWarps - 1) / kWarps)), dim3(32 * kWarps), kWarps * Plan<E, KT, KS, COLS>::kBytes};
-  if constexpr (sizeof(E) == 4)   // (a bf16 pass this short is not split)
+  if constexpr (sizeof(E) == 4)   // (a bf16 pass of steps is not split)
     if (states) return launch_op(walk<E, KT, KS, COLS, true>, sh, s, c, units);
   return launch_op(walk<E, KT, KS, COLS, false>, sh, s, c, units);
 }
