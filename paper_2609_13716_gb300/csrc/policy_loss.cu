@@ -102,9 +102,11 @@ struct Acc {
   float hi = 0.f, lo = 0.f;
   __device__ __forceinline__ void add(float v) {
     const float s = hi + v, b = s - hi;
-    lo += fabsf(s) < kInf ? (hi - (s - b)) + (v - b) : 0.f;   // (an infinite sum stays infinite)
+    lo += (hi - (s - b)) + (v - b);
     hi = s;
   }
+  // (of an infinite sum the error is not a number, and the sum says all)
+  __device__ __forceinline__ double sum() const { return fabsf(hi) < kInf ? (double)hi + (double)lo : (double)hi; }
 };
 
 // e^d - 1 - d.  Near 0, where the difference cancels, its series (to 2^-27 of it for |d| < 1/4).
@@ -149,10 +151,11 @@ __device__ __forceinline__ Row finish(const Loss& l, int64_t m, bool on, float x
     acc[3].add(clipped ? w : 0.f);
     acc[4].add(w);
   }
-  const float ws = w * inv;
+  // (formed in any case and selected: a branch around it made 2097152 x 20 fp32 148 us of 134)
+  const float ws = w * inv, past = kRef ? ls - lsy + kl : 0.f;
   r.max_x = s.mx;
   r.max_y = s.my;
-  r.c = ws * (l.ent * (H - ls) - (kRef && l.kl > 0.f ? l.kl * (ls - lsy + kl) : 0.f) - at);
+  r.c = ws * (l.ent * (H - ls) - l.kl * (l.kl > 0.f ? past : 0.f) - at);
   r.cx = ws * (l.ent + (kRef ? l.kl : 0.f));
   r.cy = kRef ? ws * l.kl : 0.f;
   r.at = w * at;
@@ -178,7 +181,7 @@ __device__ void totals(const Loss& l, const Acc (&acc)[kSums], double* tmp) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
   for (int i = 0; i < kSums; ++i) {
-    double v = (double)acc[i].hi + (double)acc[i].lo;
+    double v = acc[i].sum();
     for (int o = 16; o > 0; o >>= 1) v += __shfl_down_sync(~0u, v, o);
     if (lane == 0) tmp[warp * kSums + i] = v;
   }
