@@ -865,12 +865,28 @@ aht_status launch_tiles(Shape sh, const Loss& l, int64_t n_tiles, cudaStream_t s
   sh.most = tile_bytes<E>(kG > 0 ? 4 * kG : kTileA, kRef, kLegal);
   return launch_op(tiles<E, kRef, kLegal, kG>, sh, s, l, n_tiles);
 }
+// Groups of four actions in registers, and CTAs an SM: times (us) of 40 M logits with a reference, fp32 / bf16.  8 actions: 2
+// groups 168 / 160, 5 176 / 180.  20: 5 groups 113 / 104, 8 172 / 164; 6 CTAs 111 / 104, 4 135 / 131.  21: 8 groups 147 / 141, none
+// 166 / 158; 4 CTAs 145 / 141, 6 182 / 180.  32: 8 groups 113 / 102, none 123 / 115.  64, half legal: tiles 131 / 111, a warp a row
+// 612 / 717.
 template <typename E, bool kRef, bool kLegal>
 aht_status run_tiles(const Shape& sh, const Loss& l, int64_t n_tiles, cudaStream_t s) {
   if (l.A <= 8) return launch_tiles<E, kRef, kLegal, 2>(sh, l, n_tiles, s);
   if (l.A <= 20) return launch_tiles<E, kRef, kLegal, 5>(sh, l, n_tiles, s);
   if (l.A <= 32) return launch_tiles<E, kRef, kLegal, 8>(sh, l, n_tiles, s);
   return launch_tiles<E, kRef, kLegal, 0>(sh, l, n_tiles, s);
+}
+
+// Threads of a row of more than kTileA actions, by its bytes and the number of rows: a warp, whose sums are joined without a
+// barrier, where there are enough of them, else a CTA.  32, 256 and 512 threads a row, with a reference (us): fp32 1024
+// actions x 9728 rows 47, 109, 238, x 64 18, 14, 21; 2048 x 304 23, 21, 27, x 608 23, 27, 33, x 4864 49, 70, 139; 4096 x 1216 41,
+// 39, 51, x 2432 53, 53, 86, x 9728 135, 160, 291; 8192 x 4864 152, 127, 193; 16384 x 64 96, 23, 25, x 4864 277, 223, 272; 32768 x
+// 64 178, 37, 31, x 2432 354, 254, 236.  bf16 2048 x 4864 37, 66, 135; 8192 x 2432 59, 57, 96, x 4864 84, 100, 172; 32768 x 1216
+// 170, 80, 94; 65536 x 64 211, 39, 35, x 1216 334, 141, 145.
+int threads_of_row(int64_t A, int64_t M, int bytes) {
+  const int64_t row = A * bytes;
+  if (A <= 1024 || (row <= 8192 && M >= 608) || (row <= 16384 && M >= 2432)) return 32;
+  return row <= 65536 ? 256 : 512;
 }
 
 template <typename E, bool kRef>
@@ -883,10 +899,10 @@ aht_status go(const Loss& l, cudaStream_t s) {
     ctas = std::min<int64_t>(n_tiles, 152 * std::max(1, std::min(l.A > 20 ? 4 : kTileCtas, 226 * 1024 / (smem + 2048))));
     const Shape sh{dim3((unsigned)ctas), dim3(kTileRows), smem};
     e = l.legal ? run_tiles<E, kRef, true>(sh, l, n_tiles, s) : run_tiles<E, kRef, false>(sh, l, n_tiles, s);
-  } else if (l.A <= 1024) {
+  } else if (const int threads = threads_of_row(l.A, l.M, (int)sizeof(E)); threads == 32) {
     ctas = std::min<int64_t>((l.M + 7) / 8, 152 * 4);
     e = launch_op(rows<E, 32, 256, kRef>, Shape{dim3((unsigned)ctas), dim3(256)}, s, l);
-  } else if (l.A <= 8192) {
+  } else if (threads == 256) {
     ctas = std::min<int64_t>(l.M, 152 * 4);
     e = launch_op(rows<E, 256, 256, kRef>, Shape{dim3((unsigned)ctas), dim3(256)}, s, l);
   } else {

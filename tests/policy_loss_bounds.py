@@ -1,8 +1,8 @@
 """How far the fp32 policy loss may be from the 64-bit reference, entry by entry.
 
 With e = 2^-24, p the row's softmax, xm = x - max x, ym = y - max y, Ex = sum p |xm|, Ey = sum p |ym|:
-- A sum over the row goes through n additions: a thread's own, one after the other (A / 32 of a row of up to 1024
-  actions, A / 256 to 8192, A / 512 beyond, A up to 64), and those that join 32 lanes and 16 warps.  An exponential is off
+- A sum over the row goes through n additions: a thread's own, one after the other (A / 32 of a row of up to 8192
+  actions, which a warp may have, A / 256 beyond, A up to 64), and those that join 32 lanes and 16 warps.  An exponential is off
   by 2^-22 of itself (2 ulp) and 2 e |xm| from its argument; moving a sum to a new maximum is one more factor of that kind,
   16 of them at most for rows in random order.  Sums of one sign are therefore off, relative to themselves, by
       d = (n + 64 + 4 (Ex + Ey)) 2^-24 + 2^-22,   with 16 2^-22 = 64 2^-24.
@@ -53,7 +53,7 @@ def bounds(x, actions, old_logp, adv, legal=None, weight=None, ref_logits=None, 
         KL = (p * np.where(live & (ym > -np.inf), (xm - ls[:, None]) - (ym - lsy[:, None]), 0.0)).sum(1)
     else:
         kl = 0.0
-    n = A if A <= 64 else A / 32 + 6 if A <= 1024 else A / 256 + 16 if A <= 8192 else A / 512 + 24
+    n = A if A <= 64 else A / 32 + 6 if A <= 8192 else A / 256 + 24
     e = 2.0 ** -24
     d = (n + 64 + 4 * (Ex + Ey)) * e + 2.0 ** -22
     xa = np.where(live[rows, a], ax[rows, a], 0.0)

@@ -53,3 +53,20 @@ def test_a_reference_that_is_aligned_otherwise(M, A, dtype):
 def test_entries_of_wide_distributions(A, dtype):
     """Logits of a spread of 40: most probabilities are 0 beside a few."""
     check(L.make(20, A, dtype, "logits", seed=A, scale=40.0))
+
+
+@pytest.mark.parametrize("dtype", L.DTYPES)
+@pytest.mark.parametrize("M,A", [(607, 1500), (608, 1500), (608, 2048), (610, 2049), (608, 4096), (610, 4097), (2432, 4096), (2433, 1100)])
+def test_rows_of_a_warp_or_a_cta(M, A, dtype):
+    """Both sides of where a long row goes to a warp; some rows are compared."""
+    d = L.make(M, A, dtype, "logits", legal=M % 2 == 0, seed=A, actions=torch.int64, weight=True)
+    got = L.run(d)
+    some = torch.tensor([0, 1, 303, M // 2, M - 9, M - 1], device="cuda")
+    part = {k: v[some].contiguous() if isinstance(v, torch.Tensor) else v for k, v in d.items()}
+    a = {k: L.to64(v) for k, v in dict(x=part["logits"], actions=part["actions"], old_logp=part["old_logp"], adv=part["advantages"],
+                                       legal=part["legal"], weight=part["weight"], ref_logits=part["ref_logits"]).items()}
+    want = R.loss(**a, **L.COEF)
+    tol = bounds(**a, **L.COEF, want=want, half_step=2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -24)
+    for n, ref, t in zip(("logp", "dlogits"), want[1:], tol[1:]):
+        assert (np.abs(L.to64(got[n][some]) - ref) <= t).all(), n
+    assert abs(float(got["stats"][5]) - float(d["weight"].double()[got["logp"] != 0].sum())) <= 1e-6 * M
