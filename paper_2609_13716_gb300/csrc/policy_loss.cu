@@ -12,7 +12,7 @@
 //     reads fall into all banks.
 //   rows: more.  A warp, or a CTA, takes a row, and reads it a second time from L1 or L2.  What a CTA reads first stays
 //     in L2 until then (evict_last), what it reads again and writes goes first: without that, 304 rows of 256 KB at a
-//     time found 14 % of themselves there (4096 x 65536 bf16: 484 us, 438 with it, every logit from memory once; a
+//     time found 14 % of themselves there (4096 x 65536 bf16: 484 us, 440 with it, every logit from memory once; a
 //     cluster of CTAs a row that keeps it in shared memory 1144, the clusters' barriers).
 // Sums over rows: two fp32 a thread (value and rounding error), fp64 from there, in a fixed order.
 #include <cuda_bf16.h>
@@ -109,7 +109,7 @@ struct Acc {
   __device__ __forceinline__ double sum() const { return fabsf(hi) < kInf ? (double)hi + (double)lo : (double)hi; }
 };
 
-// e^d - 1 - d.  Near 0, where the difference cancels, its series (to 2^-27 of it for |d| < 1/4).
+// e^d - 1 - d.  Near 0, where the difference cancels, its series (to 2^-26.3 of it for |d| < 1/4).
 __device__ __forceinline__ float excess(float d) {
   if (fabsf(d) < 0.25f)
     return d * d * (0.5f + d * (1.f / 6 + d * (1.f / 24 + d * (1.f / 120 + d * (1.f / 720 + d * (1.f / 5040))))));
@@ -675,8 +675,7 @@ __device__ __forceinline__ uint4 load_16(const uint4* p, uint64_t policy) {
 }
 
 // Adds a row's vectors [0, n) from `lane` on, `step` apart, as pairs, or (`far`) an element at a time.
-// kAhead loads are on their way at a time.
-template <typename E, bool kRef, int kAhead>
+template <typename E, bool kRef>
 __device__ __forceinline__ Sums add_vectors(const uint4* xv, const uint4* yv, const uint8_t* legal, int n, int lane, int step, bool far) {
   const uint64_t stays = tc::l2_evict_last();
   constexpr int V = 16 / (int)sizeof(E);
@@ -690,6 +689,7 @@ __device__ __forceinline__ Sums add_vectors(const uint4* xv, const uint4* yv, co
     }
     return s;
   }
+  constexpr int kAhead = 2;     // vectors on their way at a time
   Pairs p;
   for (int v0 = lane; v0 < n; v0 += kAhead * step) {
     uint4 xw[kAhead], yw[kAhead];
@@ -711,17 +711,17 @@ template <typename E, bool kRef> __device__ __forceinline__ void add_one(Sums& s
   const float xv[1] = {f32(x[j])}, yv[1] = {kRef ? f32(y[j]) : 0.f};
   add_each<1, kRef>(s, xv, yv, legal ? legal + j : nullptr);
 }
-// The sums of a warp's lanes (or of groups of kLanes), for each of them.
-template <bool kRef, int kLanes = 32> __device__ __forceinline__ void join_warp(Sums& s) {
+// The sums of a warp's lanes, for each of them.
+template <bool kRef> __device__ __forceinline__ void join_warp(Sums& s) {
   float mx = s.mx, my = s.my;
 #pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) {
+  for (int o = 16; o > 0; o >>= 1) {
     mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
     if (kRef) my = fmaxf(my, __shfl_xor_sync(~0u, my, o));
   }
   move_to<kRef>(s, mx, my);
 #pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) {
+  for (int o = 16; o > 0; o >>= 1) {
     s.s += __shfl_xor_sync(~0u, s.s, o);
     s.u += __shfl_xor_sync(~0u, s.u, o);
     if (kRef) s.t += __shfl_xor_sync(~0u, s.t, o), s.sy += __shfl_xor_sync(~0u, s.sy, o);
@@ -833,10 +833,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) rows(const __grid_c
     while (true) {
       s = Sums{};
       if (on) {
-        s = add_vectors<E, kRef, 2>(row.xv(0), row.yv(0), legal, row.vecs, lane, TPR, far);
+        s = add_vectors<E, kRef>(row.xv(0), row.yv(0), legal, row.vecs, lane, TPR, far);
         row.odd(A, lane, TPR, [&](int j) { add_one<E, kRef>(s, row.x, row.y, row.legal, j); });
       }
       join_warp<kRef>(s);
+      __syncwarp();             // (the lanes have read the action's logit, which the gradient may replace)
       if constexpr (TPR > 32) {
         float* set = red + turn * kParts * 6;
         if ((lane & 31) == 0) put(set + lane / 32 * 6, s);

@@ -70,3 +70,15 @@ def test_rows_of_a_warp_or_a_cta(M, A, dtype):
     for n, ref, t in zip(("logp", "dlogits"), want[1:], tol[1:]):
         assert (np.abs(L.to64(got[n][some]) - ref) <= t).all(), n
     assert abs(float(got["stats"][5]) - float(d["weight"].double()[got["logp"] != 0].sum())) <= 1e-6 * M
+
+
+@pytest.mark.parametrize("dtype", L.DTYPES)
+@pytest.mark.parametrize("M,A", [(700, 65), (3000, 100), (700, 1501), (2500, 4096)])
+def test_gradient_in_place_of_rows_of_a_warp(M, A, dtype):
+    d = L.make(M, A, dtype, "logits", legal=True, seed=6)
+    want = L.run(d)
+    for _ in range(3):
+        e = dict(d, logits=d["logits"].clone())
+        got = L.run(e, dlogits=e["logits"])
+        for n in ("stats", "logp", "dlogits"):
+            assert torch.equal(got[n], want[n]), n
