@@ -529,15 +529,17 @@ __global__ void __launch_bounds__(32 * kWarps, KT * COLS > 64 ? 2 : 4) walk(cons
 //   Operands of bf16: P = (Q K^T) o D and S are hi + lo, off by at most 2^-17 of each element, and so is decayed k
 // (hi + mid) where the state only feeds bf16 outputs; with one more part, 2^-25, where it is an output itself.  (One part,
 // 2^-8, is as much as an output's own rounding, and more where its terms nearly cancel: errors 1.4 times as large for
-// 408 us instead of 472, 128 x 4096 x 4 x 64.)  The state stays in fp32 registers, and a chunk's K^T V is summed from 0 before it is added: sums
-// that grow in the tensor cores' accumulators are truncated at every product.
+// 408 us instead of 472, 128 x 4096 x 4 x 64.)  The state stays in fp32 registers, and a chunk's K^T V is summed from 0
+// before it is added: sums that grow in the tensor cores' accumulators are truncated at every product.
 //   A CTA of D / 16 warps goes from chunk to chunk and chain to chain, the next chunk's rows on their way while
 // this one is computed.  A warp has 16 rows of O (and 64 of its columns) and 16 rows of S.  P goes from the
 // accumulators of Q K^T to the operand of P V in registers, as does decayed k from its rows; a block of v is
 // loaded once for P V and K^T V.  These are warp-wide products (mma.sync): a chunk is a chain of small products
-// with work on registers between them, and what bounds it is that work and its latency, not the products.  (The
-// same pass on tcgen05, chunks of 128 with P and results through tensor memory, took 1035 us for 128 x 4096 x 4 x 64;
-// this one takes 409, 58 % of the measured copy rate.)
+// with work on registers between them, and what bounds it is that work and its latency, not the products: 1775
+// instructions a warp and chunk, 48 % of the issue slots, 35 % of the products' pipe; 128 x 4096 x 4 x 64 with both states
+// 472 us, 50 % of the measured copy rate.  (A form on tcgen05, chunks of 128 with P and results through tensor memory,
+// took 1035 us for that pass as it was first built, and this one 1045 as it was: the steps from there were taken for this
+// one alone, so which of the two ends faster is not known.)
 //   Masked products are products with 0.  Where anything of a warp's result is not finite, they may have spread it:
 // those elements are then computed again from the rows that reach them.
 constexpr int kC = 64;                     // steps of a chunk
