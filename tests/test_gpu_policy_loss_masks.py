@@ -29,6 +29,7 @@ def check(d):
 def masked(M, A, dtype, spans, value, ref="logits", seed=0, both=False):
     """Logits of ``value`` over spans of columns, another span for each row; actions elsewhere."""
     d = L.make(M, A, dtype, ref, seed=seed, actions=torch.int64)
+    torch.manual_seed(0)
     d["actions"] = torch.randint(0, A, (M,), device="cuda")
     x = d["logits"].clone()
     y = d["ref_logits"].clone() if ref == "logits" else None
@@ -83,6 +84,7 @@ def test_rows_of_very_low_logits(A, level, with_mask, dtype):
     reference's as low.  The probabilities are those of the logits at the level, 1 / their number."""
     M = 6
     d = L.make(M, A, dtype, "logits", seed=3, actions=torch.int64)
+    torch.manual_seed(0)
     x, y = torch.full((M, A), 2 * level, device="cuda"), torch.full((M, A), 2 * level, device="cuda")
     top = torch.rand(M, A, device="cuda") < 0.4
     d["actions"] = torch.randint(0, A, (M,), device="cuda")
@@ -104,6 +106,7 @@ def test_rows_of_very_low_logits(A, level, with_mask, dtype):
 @pytest.mark.parametrize("A", [100, 256, 1500, 9001])
 def test_contiguous_ranges_that_are_not_legal(A, dtype):
     d = L.make(16, A, dtype, "logits", legal=True, seed=4, actions=torch.int64)
+    torch.manual_seed(0)
     d["legal"][:] = 0
     d["actions"] = torch.randint(0, A, (16,), device="cuda")
     for m in range(16):

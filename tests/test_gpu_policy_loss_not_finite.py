@@ -31,6 +31,7 @@ def shows(d, clean, row, where):
 def test_logits_that_are_no_numbers(A, ref, dtype, spare):
     """A whole row (a diverged network's), whole vectors at its head, middle and tail, every other vector, one element."""
     d = L.make(9, A, dtype, ref, seed=A, spare=spare, actions=torch.uint8 if A < 256 else torch.int64)
+    torch.manual_seed(0)
     d["actions"] = torch.randint(0, A, (9,), device="cuda")
     clean = L.run(d)
     j = torch.arange(A, device="cuda")
@@ -48,6 +49,7 @@ def test_logits_that_are_no_numbers(A, ref, dtype, spare):
 def test_a_reference_of_no_numbers(A, dtype, spare):
     """Also beside reference logits of -inf, and where the policy's own logit is -inf."""
     d = L.make(9, A, dtype, "logits", seed=A, spare=spare, actions=torch.int64)
+    torch.manual_seed(0)
     d["actions"] = torch.randint(0, A, (9,), device="cuda")
     clean = L.run(d)
     j = torch.arange(A, device="cuda")
@@ -67,6 +69,7 @@ def test_a_reference_of_no_numbers(A, dtype, spare):
 @pytest.mark.parametrize("A", [48, 100, 256, 1500, 9001])
 def test_infinite_logits(A, dtype):
     d = L.make(9, A, dtype, "logits", seed=A, actions=torch.int64)
+    torch.manual_seed(0)
     d["actions"] = torch.randint(0, A, (9,), device="cuda")
     clean = L.run(d)
     for name in ("logits", "ref_logits"):

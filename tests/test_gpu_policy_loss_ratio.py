@@ -15,6 +15,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("A", [6, 48, 100, 1500, 9001])
 def test_actions_that_the_collecting_policy_hardly_took(A, ref, dtype):
     d = L.make(8, A, dtype, ref, seed=A, actions=torch.int64)
+    torch.manual_seed(0)
     d["actions"] = torch.randint(0, A, (8,), device="cuda")
     lp = torch.log_softmax(d["logits"].double(), 1).gather(1, d["actions"][:, None])[:, 0]
     d["old_logp"] = (lp + 0.1).float()
