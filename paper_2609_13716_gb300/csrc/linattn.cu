@@ -1057,13 +1057,13 @@ __global__ void __launch_bounds__(TcPlan<D>::kThreads, TcPlan<D>::kCtas) chunks(
             }
           }
         }
-        // (without a drop no product is masked)
+        // What is not finite: masked rows are 0 times it, and so are parts that are 0.
         uint64_t zero = 0;
 #pragma unroll
         for (int j = 0; j < kNV; ++j) zero = tc::f2_fma(tc::f2_pack(U[j][0], U[j][1]), 0, tc::f2_fma(tc::f2_pack(U[j][2], U[j][3]), 0, zero));
         float z0, z1;
         tc::f2_unpack(zero, z0, z1);
-        if (!keeps && __any_sync(~0u, !(z0 + z1 == 0.f))) {
+        if (__any_sync(~0u, !(z0 + z1 == 0.f))) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float n[2 * kNV] = {};
