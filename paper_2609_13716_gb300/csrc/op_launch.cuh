@@ -24,8 +24,8 @@ bool on_boundary(int bytes, const P*... p) {
 }
 
 // Grid, block, dynamic shared memory and CTAs of a cluster of a launch; `most`: the most that any launch of the kernel has.
-// (A kernel's limit belongs to the device, not to a call: every call sets the same one, or a call of another thread
-// could lower it between this one's setting and its launch.)
+// (A kernel's limit belongs to the device, not to a call: every call that sets it sets the same one, or a call of another
+// thread could lower it between this one's setting and its launch.)
 struct Shape {
   dim3 grid, block;
   int smem = 0, cluster = 1, most = smem;
@@ -33,7 +33,7 @@ struct Shape {
 
 template <typename K, typename... Args>
 aht_status launch_op(K kernel, const Shape& sh, cudaStream_t s, const Args&... args) {
-  if (sh.most > 16 * 1024)  // (with the static part it may pass 48 KB)
+  if (sh.smem > 16 * 1024)  // (with the static part it may pass 48 KB)
     if (aht_status e = launched(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sh.most))) return e;
   if (sh.cluster > 8)  // beyond what every device runs
     if (aht_status e = launched(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1))) return e;
